@@ -456,6 +456,136 @@ SPEC_API spec_status spec_mla_sparse_decode_attn(const spec_mla_dims* dm, const 
  * the partial results of split selections).                                 */
 SPEC_API spec_status spec_mla_workspace_size(const spec_mla_dims* dm, size_t* bytes);
 
+/* ---- caches read in full ---------------------------------------------------
+ * Attention over every cached token a query may see, without a selection: a
+ * sliding window with sinks, a prefix shared by the batch, and a cache kept
+ * bounded by evicting the tokens of least accumulated attention weight.  The
+ * conventions above hold (layouts, lengths on the device and clamped, ownership,
+ * alignment, errors, SPEC_DEBUG), with these differences: H_q / H_kv = G may be
+ * any number up to 128, H_kv any number, and the workspace must be of the size
+ * that spec_dense_workspace_size() gives.                                     */
+typedef struct spec_dense_dims {
+  int32_t B;         /* sequences in the batch                                 */
+  int32_t L_cap;     /* token capacity of every cache row                      */
+  int32_t n_layers;  /* layers of the call                                     */
+  int32_t H_q;       /* query heads (not used by spec_evict)                   */
+  int32_t H_kv;      /* KV heads; query head h reads KV head h / (H_q / H_kv)  */
+  int32_t d;         /* head dimension (128)                                   */
+  int32_t T;         /* spec_window_attn: query tokens per sequence (row length
+                        of q), > 0; spec_evict: new rows per sequence, >= 0    */
+  int32_t window;    /* window entry points: tokens that a query sees, itself
+                        included, > 0 (L_cap or more: all before it)           */
+  int32_t n_sink;    /* first tokens that stay visible (window) or are not
+                        evicted (spec_evict), >= 0                             */
+  int32_t P_cap;     /* spec_prefix_decode_attn: token capacity of the prefix  */
+  int32_t n_sets;    /* spec_accum_decode_attn, spec_evict: weight sums per token:
+                        1 (all heads) or H_kv (one per KV head)                */
+  int32_t n_recent;  /* spec_evict: last tokens that are not evicted, >= 0     */
+  int64_t kv_stride_layer;     /* elements between layers of K/V; 0 = B*kv_stride_b */
+  int64_t kv_stride_b;         /* elements between sequences; 0 = L_cap*H_kv*d */
+  int64_t prefix_stride_layer; /* elements between layers of the prefix;
+                                  0 = P_cap*H_kv*d                             */
+  float scale;       /* softmax scale; 0 = 1/sqrt(d)                           */
+  int32_t reserved;  /* must be 0                                              */
+} spec_dense_dims;
+
+typedef enum spec_dense_op {
+  SPEC_DENSE_WINDOW_DECODE = 0,
+  SPEC_DENSE_WINDOW = 1,
+  SPEC_DENSE_PREFIX_DECODE = 2,
+  SPEC_DENSE_ACCUM_DECODE = 3,
+  SPEC_DENSE_EVICT = 4
+} spec_dense_op;
+
+/* Workspace bytes of a dense entry point (0 where it takes none).  Returns the
+ * same validation status as the entry point itself.                           */
+SPEC_API spec_status spec_dense_workspace_size(const spec_dense_dims* dm, spec_dense_op op,
+                                size_t* bytes);
+
+/* Decode attention with a sliding window and sinks: one query token per
+ * sequence, at position p = L_b - 1 of its L_b = seq_lens[b] cached tokens.  It
+ * sees token t if
+ *     t <= p  and  (t < n_sink  or  t > p - window),
+ * and out, lse are Eq. 1 over those tokens, as for spec_sparse_decode_attn.
+ * Layouts: q [n_layers][B][H_q][d], K/V [n_layers][B][L_cap][H_kv][d], out
+ * [n_layers][B][H_q][d] fp32, lse [n_layers][B][H_q] fp32 (nullable).  A sequence
+ * of no tokens gives out = 0 and lse = -inf, and so does a query all of whose
+ * visible logits are -inf.  Rows that no query sees are not read for values.    */
+SPEC_API spec_status spec_window_decode_attn(const spec_dense_dims* dm, const uint16_t* q,
+                                const uint16_t* k_cache, const uint16_t* v_cache,
+                                const int32_t* seq_lens, float* out, float* lse, void* ws,
+                                size_t ws_bytes, spec_stream stream);
+
+/* Window attention of a chunk of query tokens per sequence (prefill, or several
+ * tokens at once): the last n_b = q_lens[b] (NULL: T) of the L_b = seq_lens[b]
+ * tokens, which the cache holds already; query i < n_b is at position
+ * p = L_b - n_b + i and sees tokens as above (none where p < 0).  q and out are
+ * bf16 [n_layers][B][T][H_q][d], lse fp32 [n_layers][B][T][H_q] (nullable).
+ * Queries i >= n_b leave out and lse as they were; a query that sees nothing
+ * gives 0 and -inf.  fp32 accumulation; the softmax weights enter the matrix
+ * cores rounded to bf16, as the output is.  A cached row that holds a NaN or an
+ * infinity reaches only the queries that see it.                               */
+SPEC_API spec_status spec_window_attn(const spec_dense_dims* dm, const uint16_t* q,
+                                const uint16_t* k_cache, const uint16_t* v_cache,
+                                const int32_t* seq_lens, const int32_t* q_lens,
+                                uint16_t* out, float* lse, void* ws, size_t ws_bytes,
+                                spec_stream stream);
+
+/* Decode attention of a batch whose sequences share a prefix: query token of
+ * sequence b over the P = prefix_len[0] (NULL: P_cap) rows of k_prefix/v_prefix
+ * [n_layers][P_cap][H_kv][d] and then the L_b = seq_lens[b] rows of its own cache,
+ * one softmax over both.  The prefix is read once for the whole batch.  q, out,
+ * lse and the own caches as for spec_window_decode_attn.  P = L_b = 0 gives out
+ * = 0 and lse = -inf.                                                          */
+SPEC_API spec_status spec_prefix_decode_attn(const spec_dense_dims* dm, const uint16_t* q,
+                                const uint16_t* k_prefix, const uint16_t* v_prefix,
+                                const int32_t* prefix_len, const uint16_t* k_cache,
+                                const uint16_t* v_cache, const int32_t* seq_lens, float* out,
+                                float* lse, void* ws, size_t ws_bytes, spec_stream stream);
+
+/* Decode attention over the rows [0, counts[b]) of every cache (in any token
+ * order), which adds the softmax weights up per token:
+ *     weights[l,b,s,t] += sum over the heads h of set s of p[l,b,h,t]
+ * with set 0 = all heads (n_sets = 1) or set g = KV head g's query heads (n_sets =
+ * H_kv); weights [n_layers][B][n_sets][L_cap] fp32, rows t >= counts[b] left as they
+ * were.  out and lse (nullable) as for spec_window_decode_attn.  The sums are
+ * deterministic (fixed order).                                                 */
+SPEC_API spec_status spec_accum_decode_attn(const spec_dense_dims* dm, const uint16_t* q,
+                                const uint16_t* k_cache, const uint16_t* v_cache,
+                                const int32_t* counts, float* weights, float* out, float* lse,
+                                void* ws, size_t ws_bytes, spec_stream stream);
+
+/* Device-resident state of bounded caches (host struct of device pointers).
+ *   k, v     [n_layers][B][L_cap][H_kv][d] bf16: the rows held, in any order;
+ *   weights  [n_layers][B][n_sets][L_cap] fp32: their accumulated weights;
+ *   tokens   [n_layers][B][n_sets][L_cap] int32: their token positions;
+ *   counts   [B] int32: rows held, slots [0, counts[b]) of every layer and set.  */
+typedef struct spec_bounded {
+  uint16_t* k;
+  uint16_t* v;
+  float* weights;
+  int32_t* tokens;
+  int32_t* counts;
+} spec_bounded;
+
+/* Insertion of n_b = n_new[b] (NULL: T) new rows into bounded caches, evicting by
+ * accumulated weight.  With c = counts[b] and a budget k = keep[b] (clamped into
+ * [0, L_cap]), C' = min(k, c + n_b) rows are held afterwards: the last n' = min(n_b,
+ * C') new rows, and of the rows held, per layer and set, the C' - n' that come
+ * first by weight (largest first; ties to the lower slot; NaN ranks with -inf),
+ * where the weight of a protected row (token < n_sink, or token >= pos[b] + n_b -
+ * n_recent) counts as +inf.  pos[b]: the position of the first new row, i.e. the
+ * tokens seen so far.  Rows that stay keep their slot; the other slots below C'
+ * are filled, ascending, first by the kept rows of slots >= C' (ascending, with
+ * their weights and tokens), then by the new rows in order, with weight 0 and
+ * token pos[b] + i.  counts[b] = C'.  Slots >= C' are left as they were.  T = 0
+ * (k_new, v_new may be NULL) only brings the caches down to their budgets.
+ * k_new, v_new [n_layers][B][T][H_kv][d] bf16, keep, pos, n_new [B] int32.      */
+SPEC_API spec_status spec_evict(const spec_dense_dims* dm, const spec_bounded* cache,
+                                const int32_t* keep, const int32_t* pos, const uint16_t* k_new,
+                                const uint16_t* v_new, const int32_t* n_new, void* ws,
+                                size_t ws_bytes, spec_stream stream);
+
 /* Workspace bytes needed by `op` for dimensions `dm` (0 for SPEC_OP_GATHER).
  * Returns the same validation status as the op itself.                      */
 SPEC_API spec_status spec_workspace_size(const spec_dims* dm, spec_op op,

@@ -29,6 +29,9 @@ __all__ = [
     "retrieval_qk", "MlaDims", "mla_workspace_size", "mla_sparse_decode_attn",
     "OP_SCORE", "OP_TOPK", "OP_GATHER", "OP_ATTN", "OP_DELTA", "OP_STEP", "OP_FRONTEND",
     "OP_OFFLOAD", "OP_STEP_NOALLOC", "HostKv", "OffloadEvents", "offload_load", "step_offload",
+    "DenseDims", "dense_workspace_size", "window_decode_attn", "window_attn",
+    "prefix_decode_attn", "accum_decode_attn", "evict", "DENSE_WINDOW_DECODE", "DENSE_WINDOW",
+    "DENSE_PREFIX_DECODE", "DENSE_ACCUM_DECODE", "DENSE_EVICT",
     "EXPORTED_SYMBOLS",
 ]
 
@@ -37,6 +40,8 @@ lib_path = os.path.join(_PKG, "libspecctx.so")
 
 (OP_SCORE, OP_TOPK, OP_GATHER, OP_ATTN, OP_DELTA, OP_STEP, OP_FRONTEND, OP_OFFLOAD,
  OP_STEP_NOALLOC) = range(9)
+(DENSE_WINDOW_DECODE, DENSE_WINDOW, DENSE_PREFIX_DECODE, DENSE_ACCUM_DECODE,
+ DENSE_EVICT) = range(5)
 STATUS = {0: "SPEC_OK", 1: "SPEC_ERR_INVALID", 2: "SPEC_ERR_UNSUPPORTED",
           3: "SPEC_ERR_WORKSPACE", 4: "SPEC_ERR_HIP", 5: "SPEC_ERR_TOO_LARGE"}
 
@@ -45,6 +50,8 @@ EXPORTED_SYMBOLS = ["spec_score", "spec_topk", "spec_gather", "spec_sparse_decod
                     "spec_step_noalloc_max_bytes", "spec_offload_load", "spec_step_offload",
                     "spec_retrieval_qk",
                     "spec_mla_sparse_decode_attn", "spec_mla_workspace_size", "spec_workspace_size",
+                    "spec_dense_workspace_size", "spec_window_decode_attn", "spec_window_attn",
+                    "spec_prefix_decode_attn", "spec_accum_decode_attn", "spec_evict",
                     "spec_status_string", "spec_last_hip_error", "spec_version"]
 
 
@@ -117,6 +124,29 @@ class MlaDims(ctypes.Structure):
                    ckv_stride_b, scale, 0)
 
 
+class DenseDims(ctypes.Structure):
+    """Mirror of `spec_dense_dims`."""
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("B", "L_cap", "n_layers", "H_q", "H_kv", "d", "T", "window", "n_sink", "P_cap",
+                 "n_sets", "n_recent")] + [
+        ("kv_stride_layer", ctypes.c_int64), ("kv_stride_b", ctypes.c_int64),
+        ("prefix_stride_layer", ctypes.c_int64), ("scale", ctypes.c_float),
+        ("reserved", ctypes.c_int32)]
+
+    @classmethod
+    def make(cls, B, L_cap, n_layers=1, H_q=8, H_kv=8, d=128, T=1, window=0, n_sink=0, P_cap=0,
+             n_sets=1, n_recent=0, kv_stride_layer=0, kv_stride_b=0, prefix_stride_layer=0,
+             scale=0.0):
+        return cls(B, L_cap, n_layers, H_q, H_kv, d, T, window, n_sink, P_cap, n_sets, n_recent,
+                   kv_stride_layer, kv_stride_b, prefix_stride_layer, scale, 0)
+
+
+class Bounded(ctypes.Structure):
+    """Mirror of `spec_bounded`."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+                ("tokens", ctypes.c_void_p), ("counts", ctypes.c_void_p)]
+
+
 _lib = None
 _fast = None  # native marshalling (binding/fast.cpp), loaded with the library if built
 # its entry points, in the order its init() takes their addresses
@@ -139,6 +169,7 @@ def load_library(path: Optional[str] = None):
     E = ctypes.POINTER(Elastic)
     F = ctypes.POINTER(Frontend)
     M = ctypes.POINTER(MlaDims)
+    N = ctypes.POINTER(DenseDims)
     sig = {
         "spec_score": [D, P, P, P, P, P, S, P],
         "spec_topk": [D, P, P, P, P, P, P, S, P],
@@ -155,6 +186,12 @@ def load_library(path: Optional[str] = None):
         "spec_mla_sparse_decode_attn": [M, P, P, P, P, P, P, P, P, P, S, P],
         "spec_mla_workspace_size": [M, ctypes.POINTER(S)],
         "spec_workspace_size": [D, I, ctypes.POINTER(S)],
+        "spec_dense_workspace_size": [N, I, ctypes.POINTER(S)],
+        "spec_window_decode_attn": [N, P, P, P, P, P, P, P, S, P],
+        "spec_window_attn": [N, P, P, P, P, P, P, P, P, S, P],
+        "spec_prefix_decode_attn": [N, P, P, P, P, P, P, P, P, P, P, S, P],
+        "spec_accum_decode_attn": [N, P, P, P, P, P, P, P, P, S, P],
+        "spec_evict": [N, ctypes.POINTER(Bounded), P, P, P, P, P, P, S, P],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -831,3 +868,235 @@ def mla_sparse_decode_attn(q: torch.Tensor, ckv: torch.Tensor, w_uk: torch.Tenso
                                            _p(ws), ws.numel() * ws.element_size(), _stream(q)),
            "spec_mla_sparse_decode_attn")
     return out, lse
+
+
+# ------------------------------------------------------------------ caches read in full
+
+def dense_workspace_size(dims: DenseDims, op: int) -> int:
+    lib = load_library()
+    n = ctypes.c_size_t(0)
+    _check(lib.spec_dense_workspace_size(ctypes.byref(dims), op, ctypes.byref(n)),
+           "spec_dense_workspace_size")
+    return int(n.value)
+
+
+def _dense_workspace(dims: DenseDims, op: int, device, ws: Optional[torch.Tensor]):
+    if ws is not None:
+        return ws, ws.numel() * ws.element_size()
+    need = dense_workspace_size(dims, op)
+    return torch.empty(max(need, 16), dtype=torch.uint8, device=device), need
+
+
+def _same_device(where: torch.Tensor, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != where.device:
+            raise ValueError(f"{name} must be on {where.device}, is on {t.device}")
+
+
+def _output(t: Optional[torch.Tensor], name: str, shape, dtype, device) -> torch.Tensor:
+    """The caller's output, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _need(t, name, dtype, len(shape))
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous {tuple(shape)}")
+    return t
+
+
+def _dense_q(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, chunk: bool):
+    _need(q, "q", torch.bfloat16, 5 if chunk else 4)
+    _check_cache(K, V)
+    n_layers, B, _, _, d = K.shape
+    if q.shape[0] != n_layers or q.shape[1] != B or q.shape[-1] != d or not q.is_contiguous():
+        raise ValueError("q must be contiguous [n_layers, B, " + ("T, " if chunk else "")
+                         + "H_q, d]")
+
+
+def _int32(n: int) -> int:
+    """A count whose size beyond any cache's does not matter, as the C ABI takes it."""
+    return max(-1, min(int(n), 2 ** 31 - 1))
+
+
+def _dense_dims(K: torch.Tensor, **kw) -> DenseDims:
+    n_layers, B, L_cap, H_kv, d = K.shape
+    return DenseDims.make(B=B, L_cap=L_cap, n_layers=n_layers, H_kv=H_kv, d=d,
+                          kv_stride_layer=K.stride(0), kv_stride_b=K.stride(1), **kw)
+
+
+def window_decode_attn(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, seq_lens: torch.Tensor,
+                       window: int, n_sink: int = 0, scale: float = 0.0,
+                       out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                       with_lse: bool = True, ws: Optional[torch.Tensor] = None):
+    """Decode attention with a sliding window and sinks: the query token at
+    position seq_lens[b] - 1 sees the first n_sink tokens and the last `window`
+    of the cache (itself included).  q [n_layers, B, H_q, d]; K/V [n_layers, B,
+    L_cap, H_kv, d].  Returns (out fp32 [n_layers, B, H_q, d], lse fp32
+    [n_layers, B, H_q] or None); no tokens: 0 and -inf."""
+    lib = load_library()
+    _dense_q(q, K, V, False)
+    _i32(seq_lens, "seq_lens", K.shape[1])
+    _same_device(q, K=K, V=V, seq_lens=seq_lens, out=out, lse=lse, ws=ws)
+    dims = _dense_dims(K, H_q=q.shape[2], window=_int32(window), n_sink=_int32(n_sink), scale=scale)
+    ws, nws = _dense_workspace(dims, DENSE_WINDOW_DECODE, q.device, ws)
+    out = _output(out, "out", q.shape, torch.float32, q.device)
+    if lse is not None or with_lse:
+        lse = _output(lse, "lse", q.shape[:-1], torch.float32, q.device)
+    with torch.cuda.device(q.device):
+        _check(lib.spec_window_decode_attn(ctypes.byref(dims), _p(q), _p(K), _p(V), _p(seq_lens),
+                                           _p(out), _p(lse), _p(ws), nws, _stream(q)),
+               "spec_window_decode_attn")
+    return out, lse
+
+
+def window_attn(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, seq_lens: torch.Tensor,
+                window: int, n_sink: int = 0, q_lens: Optional[torch.Tensor] = None,
+                scale: float = 0.0, out: Optional[torch.Tensor] = None,
+                lse: Optional[torch.Tensor] = None, with_lse: bool = True,
+                ws: Optional[torch.Tensor] = None):
+    """Window attention of a chunk of query tokens per sequence, the last q_lens[b]
+    (None: T) of its seq_lens[b] cached tokens.  q [n_layers, B, T, H_q, d]; K/V
+    as above.  Returns (out bf16 like q, lse fp32 [n_layers, B, T, H_q] or
+    None); queries behind a sequence's last are left as they are (zero when the
+    outputs are allocated here)."""
+    lib = load_library()
+    _dense_q(q, K, V, True)
+    B = K.shape[1]
+    _i32(seq_lens, "seq_lens", B)
+    if q_lens is not None:
+        _i32(q_lens, "q_lens", B)
+    _same_device(q, K=K, V=V, seq_lens=seq_lens, q_lens=q_lens, out=out, lse=lse, ws=ws)
+    dims = _dense_dims(K, H_q=q.shape[3], T=q.shape[2], window=_int32(window), n_sink=_int32(n_sink),
+                       scale=scale)
+    ws, nws = _dense_workspace(dims, DENSE_WINDOW, q.device, ws)
+    if out is None:
+        out = torch.zeros_like(q) if q_lens is not None else torch.empty_like(q)
+    _output(out, "out", q.shape, torch.bfloat16, q.device)
+    if lse is None and with_lse:
+        lse = torch.zeros(q.shape[:-1], dtype=torch.float32, device=q.device)
+    if lse is not None:
+        _output(lse, "lse", q.shape[:-1], torch.float32, q.device)
+    with torch.cuda.device(q.device):
+        _check(lib.spec_window_attn(ctypes.byref(dims), _p(q), _p(K), _p(V), _p(seq_lens),
+                                    _p(q_lens), _p(out), _p(lse), _p(ws), nws, _stream(q)),
+               "spec_window_attn")
+    return out, lse
+
+
+def prefix_decode_attn(q: torch.Tensor, K_prefix: torch.Tensor, V_prefix: torch.Tensor,
+                       K: torch.Tensor, V: torch.Tensor, seq_lens: torch.Tensor,
+                       prefix_len: Optional[torch.Tensor] = None, scale: float = 0.0,
+                       out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                       with_lse: bool = True, ws: Optional[torch.Tensor] = None):
+    """Decode attention of a batch that shares a prefix, one softmax over the
+    prefix's rows (K_prefix/V_prefix [n_layers, P_cap, H_kv, d]; prefix_len: int32
+    [1] on the device, None: P_cap) and the sequence's own seq_lens[b] rows of K/V
+    [n_layers, B, L_cap, H_kv, d].  q [n_layers, B, H_q, d].  Returns (out fp32,
+    lse fp32 or None) as window_decode_attn."""
+    lib = load_library()
+    _dense_q(q, K, V, False)
+    n_layers, B, _, H_kv, d = K.shape
+    for t, nm in ((K_prefix, "K_prefix"), (V_prefix, "V_prefix")):
+        _need(t, nm, torch.bfloat16, 4)
+        if t.shape[0] != n_layers or tuple(t.shape[2:]) != (H_kv, d):
+            raise ValueError(f"{nm} must be [n_layers, P_cap, H_kv, d]")
+        _inner_contig(t, nm, 3)
+    if K_prefix.shape != V_prefix.shape or K_prefix.stride() != V_prefix.stride():
+        raise ValueError("K_prefix and V_prefix must have the same shape and strides")
+    _i32(seq_lens, "seq_lens", B)
+    if prefix_len is not None:
+        _i32(prefix_len, "prefix_len", 1)
+    _same_device(q, K=K, V=V, K_prefix=K_prefix, V_prefix=V_prefix, seq_lens=seq_lens,
+                 prefix_len=prefix_len, out=out, lse=lse, ws=ws)
+    dims = _dense_dims(K, H_q=q.shape[2], P_cap=K_prefix.shape[1], scale=scale,
+                       prefix_stride_layer=K_prefix.stride(0))
+    ws, nws = _dense_workspace(dims, DENSE_PREFIX_DECODE, q.device, ws)
+    out = _output(out, "out", q.shape, torch.float32, q.device)
+    if lse is not None or with_lse:
+        lse = _output(lse, "lse", q.shape[:-1], torch.float32, q.device)
+    with torch.cuda.device(q.device):
+        _check(lib.spec_prefix_decode_attn(ctypes.byref(dims), _p(q), _p(K_prefix), _p(V_prefix),
+                                           _p(prefix_len), _p(K), _p(V), _p(seq_lens), _p(out),
+                                           _p(lse), _p(ws), nws, _stream(q)),
+               "spec_prefix_decode_attn")
+    return out, lse
+
+
+def _sets_of_weights(weights: torch.Tensor, K: torch.Tensor) -> int:
+    n_layers, B, L_cap, H_kv, _ = K.shape
+    _need(weights, "weights", torch.float32, 4)
+    n_sets = weights.shape[2]
+    if n_sets not in (1, H_kv) or tuple(weights.shape) != (n_layers, B, n_sets, L_cap) \
+            or not weights.is_contiguous():
+        raise ValueError("weights must be contiguous [n_layers, B, 1 or H_kv, L_cap]")
+    return n_sets
+
+
+def accum_decode_attn(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, counts: torch.Tensor,
+                      weights: torch.Tensor, scale: float = 0.0,
+                      out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                      with_lse: bool = True, ws: Optional[torch.Tensor] = None):
+    """Decode attention over the rows [0, counts[b]) of K/V [n_layers, B, L_cap,
+    H_kv, d] that adds each row's softmax weights, summed over all query heads
+    (weights [n_layers, B, 1, L_cap] fp32) or over each KV head's (weights
+    [n_layers, B, H_kv, L_cap]), to `weights` in place.  Returns (out, lse) as
+    window_decode_attn."""
+    lib = load_library()
+    _dense_q(q, K, V, False)
+    _i32(counts, "counts", K.shape[1])
+    n_sets = _sets_of_weights(weights, K)
+    _same_device(q, K=K, V=V, counts=counts, weights=weights, out=out, lse=lse, ws=ws)
+    dims = _dense_dims(K, H_q=q.shape[2], n_sets=n_sets, scale=scale)
+    ws, nws = _dense_workspace(dims, DENSE_ACCUM_DECODE, q.device, ws)
+    out = _output(out, "out", q.shape, torch.float32, q.device)
+    if lse is not None or with_lse:
+        lse = _output(lse, "lse", q.shape[:-1], torch.float32, q.device)
+    with torch.cuda.device(q.device):
+        _check(lib.spec_accum_decode_attn(ctypes.byref(dims), _p(q), _p(K), _p(V), _p(counts),
+                                          _p(weights), _p(out), _p(lse), _p(ws), nws, _stream(q)),
+               "spec_accum_decode_attn")
+    return out, lse
+
+
+def evict(K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, tokens: torch.Tensor,
+          counts: torch.Tensor, keep: torch.Tensor, pos: torch.Tensor,
+          k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
+          n_new: Optional[torch.Tensor] = None, n_recent: int = 0, n_sink: int = 0,
+          ws: Optional[torch.Tensor] = None):
+    """Inserts new rows into bounded caches, evicting by accumulated weight, all
+    in place: K/V [n_layers, B, L_cap, H_kv, d], weights fp32 and tokens int32
+    [n_layers, B, 1 or H_kv, L_cap], counts int32 [B].  keep int32 [B]: rows to
+    hold at most; pos int32 [B]: the position of the first new row; k_new/v_new
+    [n_layers, B, T, H_kv, d] (None: no new rows); n_new int32 [B] (None: T).  Of
+    the rows held, the last n_recent tokens and the first n_sink stay before all
+    others, then the largest weights, ties to the lower slot."""
+    lib = load_library()
+    _check_cache(K, V)
+    n_layers, B, L_cap, H_kv, d = K.shape
+    n_sets = _sets_of_weights(weights, K)
+    _need(tokens, "tokens", torch.int32, 4)
+    if tokens.shape != weights.shape or not tokens.is_contiguous():
+        raise ValueError("tokens must be contiguous and of the shape of weights")
+    for t, nm in ((counts, "counts"), (keep, "keep"), (pos, "pos")):
+        _i32(t, nm, B)
+    T = 0
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new go together")
+    if k_new is not None:
+        T = k_new.shape[2] if k_new.dim() == 5 else 0
+        for t, nm in ((k_new, "k_new"), (v_new, "v_new")):
+            _need(t, nm, torch.bfloat16, 5)
+            if tuple(t.shape) != (n_layers, B, T, H_kv, d) or not t.is_contiguous():
+                raise ValueError(f"{nm} must be contiguous [n_layers, B, T, H_kv, d]")
+    if n_new is not None:
+        _i32(n_new, "n_new", B)
+    _same_device(K, V=V, weights=weights, tokens=tokens, counts=counts, keep=keep, pos=pos,
+                 k_new=k_new, v_new=v_new, n_new=n_new, ws=ws)
+    dims = _dense_dims(K, H_q=H_kv, T=T, n_sets=n_sets, n_sink=_int32(n_sink),
+                       n_recent=_int32(n_recent))
+    ws, nws = _dense_workspace(dims, DENSE_EVICT, K.device, ws)
+    cache = Bounded(K.data_ptr(), V.data_ptr(), weights.data_ptr(), tokens.data_ptr(),
+                    counts.data_ptr())
+    with torch.cuda.device(K.device):
+        _check(lib.spec_evict(ctypes.byref(dims), ctypes.byref(cache), _p(keep), _p(pos),
+                              _p(k_new), _p(v_new), _p(n_new), _p(ws), nws, _stream(K)),
+               "spec_evict")

@@ -236,6 +236,70 @@ hipError_t launch_attn_elastic(const Dims& d, const uint16_t* q, const uint16_t*
                                const int32_t* slot_src, const int32_t* counts, float* out,
                                float* lse, void* ws, hipStream_t s,
                                const int32_t* fused = nullptr);
+// ---- attention without a selection, bounded caches ----------------------
+// Dimensions of the dense entry points after validation.
+struct DenseDims {
+  int B, L_cap, n_layers, H_q, H_kv, G, T, window, n_sink, P_cap, n_sets, n_recent;
+  int64_t kv_stride_layer, kv_stride_b, prefix_stride_layer;
+  float scale;
+};
+constexpr int kHeadDim = 128;
+
+// Where a launch whose results another kernel finishes left them:
+// acc [n_layers*B][n_split][H_q][d], (max, sum) [n_layers*B][n_split][H_q].  A
+// sequence of c tokens has min(n_split, ceil(c / split)) of them.
+struct AttnParts {
+  const float* acc;
+  const float* ml;
+  int n_split, split;
+};
+// One query token per sequence over its cache: d.k_max tokens at most are
+// visible, the first n_sink and the last of the rest.
+struct DenseAttn {
+  int n_sink;
+  float* logits;         // nullable: keep the logits, [n_layers*B][H_q][logit_stride], log2 units
+  int64_t logit_stride;  // of d.k_max rounded up to whole chunks of 32
+  bool partials;         // leave partial results, described in *parts
+  AttnParts* parts;
+};
+size_t attn_dense_ws_bytes(const Dims& d, bool partials);
+hipError_t launch_attn_dense(const Dims& d, const DenseAttn& m, const uint16_t* q,
+                             const uint16_t* k, const uint16_t* v, const int32_t* lens,
+                             float* out, float* lse, void* ws, hipStream_t s);
+
+size_t window_ws_bytes(const DenseDims& d);
+hipError_t launch_window(const DenseDims& d, const uint16_t* q, const uint16_t* k,
+                         const uint16_t* v, const int32_t* lens, const int32_t* q_lens,
+                         uint16_t* out, float* lse, void* ws, hipStream_t s);
+size_t window_decode_ws_bytes(const DenseDims& d);
+hipError_t launch_window_decode(const DenseDims& d, const uint16_t* q, const uint16_t* k,
+                                const uint16_t* v, const int32_t* lens, float* out, float* lse,
+                                void* ws, hipStream_t s);
+size_t prefix_decode_ws_bytes(const DenseDims& d);
+hipError_t launch_prefix_decode(const DenseDims& d, const uint16_t* q, const uint16_t* k_prefix,
+                                const uint16_t* v_prefix, const int32_t* prefix_len,
+                                const uint16_t* k, const uint16_t* v, const int32_t* lens,
+                                float* out, float* lse, void* ws, hipStream_t s);
+size_t accum_decode_ws_bytes(const DenseDims& d);
+hipError_t launch_accum_decode(const DenseDims& d, const uint16_t* q, const uint16_t* k,
+                               const uint16_t* v, const int32_t* counts, float* weights,
+                               float* out, float* lse, void* ws, hipStream_t s);
+size_t evict_ws_bytes(const DenseDims& d);
+// The rows of an eviction: the caches, the new rows and what is kept per slot.
+struct EvictArgs {
+  uint16_t* k;
+  uint16_t* v;
+  float* weights;
+  int32_t* tokens;
+  int32_t* counts;
+  const int32_t* keep;
+  const int32_t* pos;
+  const uint16_t* k_new;
+  const uint16_t* v_new;
+  const int32_t* n_new;
+};
+hipError_t launch_evict(const DenseDims& d, const EvictArgs& x, void* ws, hipStream_t s);
+
 hipError_t launch_delta(const Dims& d, const int32_t* idx_now, const int32_t* counts,
                         const uint16_t* k_cache, const uint16_t* v_cache,
                         int32_t* slot_tok, int32_t* slot_src, uint16_t* kbuf, uint16_t* vbuf,

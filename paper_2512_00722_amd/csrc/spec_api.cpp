@@ -351,8 +351,95 @@ spec_status resolve_mla(const spec_mla_dims* dm, spec::MlaDims* o) {
   return SPEC_OK;
 }
 
+spec_status resolve_dense(const spec_dense_dims* dm, spec_dense_op op, spec::DenseDims* o) {
+  if (!dm || dm->reserved != 0) return SPEC_ERR_INVALID;
+  const bool evict = op == SPEC_DENSE_EVICT;
+  const bool window = op == SPEC_DENSE_WINDOW || op == SPEC_DENSE_WINDOW_DECODE;
+  if (dm->B <= 0 || dm->L_cap <= 0 || dm->n_layers <= 0 || dm->H_kv <= 0 || dm->d <= 0)
+    return SPEC_ERR_INVALID;
+  if (!evict && (dm->H_q <= 0 || dm->H_q % dm->H_kv != 0)) return SPEC_ERR_INVALID;
+  if (dm->kv_stride_layer < 0 || dm->kv_stride_b < 0 || dm->prefix_stride_layer < 0)
+    return SPEC_ERR_INVALID;
+  if (!isfinite(dm->scale) || dm->scale < 0.f) return SPEC_ERR_INVALID;
+  if (window && (dm->window <= 0 || dm->n_sink < 0)) return SPEC_ERR_INVALID;
+  if (op == SPEC_DENSE_WINDOW && dm->T <= 0) return SPEC_ERR_INVALID;
+  if (op == SPEC_DENSE_PREFIX_DECODE && dm->P_cap <= 0) return SPEC_ERR_INVALID;
+  if (evict && (dm->T < 0 || dm->n_sink < 0 || dm->n_recent < 0)) return SPEC_ERR_INVALID;
 
-// Host checks shared by the two step entry points (before any HIP call).
+  if (dm->d != spec::kHeadDim) return SPEC_ERR_UNSUPPORTED;
+  if (!evict && dm->H_q / dm->H_kv > 128) return SPEC_ERR_UNSUPPORTED;
+  if ((evict || op == SPEC_DENSE_ACCUM_DECODE) && dm->n_sets != 1 && dm->n_sets != dm->H_kv)
+    return SPEC_ERR_UNSUPPORTED;
+  if (dm->B > 65535 || dm->n_layers > 65535 || dm->H_kv > 65535) return SPEC_ERR_UNSUPPORTED;
+  // Launch grids: at most 2^26 query rows, 2^21 KV heads or token sets, and
+  // 2^23 workgroups over the weights.
+  const int64_t lb = (int64_t)dm->n_layers * dm->B;
+  if (lb * dm->H_kv > 1 << 21) return SPEC_ERR_UNSUPPORTED;
+  if (!evict && lb * dm->H_q > 1 << 26) return SPEC_ERR_UNSUPPORTED;
+  if (op == SPEC_DENSE_WINDOW && (lb * dm->H_q * dm->T > 1 << 26)) return SPEC_ERR_UNSUPPORTED;
+  if (op == SPEC_DENSE_ACCUM_DECODE && lb * dm->n_sets * (dm->L_cap / 1024 + 1) > 1 << 23)
+    return SPEC_ERR_UNSUPPORTED;
+  if ((int64_t)dm->L_cap + dm->T > INT32_MAX - 4096 || dm->P_cap > INT32_MAX - 4096)
+    return SPEC_ERR_UNSUPPORTED;
+
+  const int64_t row = (int64_t)dm->L_cap * dm->H_kv * dm->d;
+  o->B = dm->B;
+  o->L_cap = dm->L_cap;
+  o->n_layers = dm->n_layers;
+  o->H_q = evict ? dm->H_kv : dm->H_q;
+  o->H_kv = dm->H_kv;
+  o->G = o->H_q / dm->H_kv;
+  o->T = dm->T;
+  o->window = dm->window < dm->L_cap ? dm->window : dm->L_cap;
+  o->n_sink = dm->n_sink < dm->L_cap || evict ? dm->n_sink : dm->L_cap;
+  o->P_cap = dm->P_cap;
+  o->n_sets = dm->n_sets;
+  o->n_recent = dm->n_recent;
+  o->kv_stride_b = dm->kv_stride_b ? dm->kv_stride_b : row;
+  o->kv_stride_layer = dm->kv_stride_layer ? dm->kv_stride_layer : (int64_t)dm->B * o->kv_stride_b;
+  if (o->kv_stride_b < row || o->kv_stride_b % 8 || o->kv_stride_layer < row ||
+      o->kv_stride_layer % 8)
+    return SPEC_ERR_INVALID;
+  o->prefix_stride_layer = 0;
+  if (op == SPEC_DENSE_PREFIX_DECODE) {
+    const int64_t prow = (int64_t)dm->P_cap * dm->H_kv * dm->d;
+    o->prefix_stride_layer = dm->prefix_stride_layer ? dm->prefix_stride_layer : prow;
+    if (o->prefix_stride_layer < prow || o->prefix_stride_layer % 8) return SPEC_ERR_INVALID;
+  }
+  o->scale = dm->scale > 0.f ? dm->scale : 1.0f / sqrtf((float)dm->d);
+  return SPEC_OK;
+}
+
+size_t dense_ws_bytes(const spec::DenseDims& d, spec_dense_op op) {
+  switch (op) {
+    case SPEC_DENSE_WINDOW_DECODE: return spec::window_decode_ws_bytes(d);
+    case SPEC_DENSE_WINDOW: return spec::window_ws_bytes(d);
+    case SPEC_DENSE_PREFIX_DECODE: return spec::prefix_decode_ws_bytes(d);
+    case SPEC_DENSE_ACCUM_DECODE: return spec::accum_decode_ws_bytes(d);
+    case SPEC_DENSE_EVICT: return spec::evict_ws_bytes(d);
+  }
+  return 0;
+}
+
+spec_status check_dense_ws(const spec::DenseDims& d, spec_dense_op op, const void* ws,
+                           size_t ws_bytes) {
+  const size_t need = dense_ws_bytes(d, op);
+  if (need == 0) return SPEC_OK;
+  if (!ws || ws_bytes < need) return SPEC_ERR_WORKSPACE;
+  return aligned16(ws) ? SPEC_OK : SPEC_ERR_INVALID;
+}
+
+// Device-resident int32 values in [lo, hi] (null: none to check).
+spec_status debug_range(const int32_t* p, size_t n, int32_t lo, int32_t hi, hipStream_t s) {
+  if (!p) return SPEC_OK;
+  std::vector<int32_t> h;
+  if (!d2h(h, p, n, s)) return SPEC_ERR_HIP;
+  for (int32_t v : h)
+    if (v < lo || v > hi) return SPEC_ERR_INVALID;
+  return SPEC_OK;
+}
+
+// Host checks shared by the step entry points (before any HIP call).
 spec_status check_step(const spec_dims* dm, spec::Dims* d, const uint16_t* q_r,
                        const uint16_t* k_r, const int32_t* seq_lens, const int32_t* ks,
                        const uint16_t* q, const uint16_t* k_cache, const uint16_t* v_cache,
@@ -457,6 +544,125 @@ spec_status spec_mla_sparse_decode_attn(const spec_mla_dims* dm, const uint16_t*
   return finish(hip_status(spec::launch_mla(d, q, ckv, w_uk, w_uv, idx, counts, out, lse, ws,
                                             as_stream(stream))),
                 as_stream(stream));
+}
+
+spec_status spec_dense_workspace_size(const spec_dense_dims* dm, spec_dense_op op,
+                                      size_t* bytes) {
+  if (!bytes) return SPEC_ERR_INVALID;
+  if ((int)op < SPEC_DENSE_WINDOW_DECODE || (int)op > SPEC_DENSE_EVICT) return SPEC_ERR_INVALID;
+  spec::DenseDims d;
+  const spec_status st = resolve_dense(dm, op, &d);
+  if (st != SPEC_OK) return st;
+  *bytes = dense_ws_bytes(d, op);
+  return SPEC_OK;
+}
+
+spec_status spec_window_decode_attn(const spec_dense_dims* dm, const uint16_t* q,
+                                    const uint16_t* k_cache, const uint16_t* v_cache,
+                                    const int32_t* seq_lens, float* out, float* lse, void* ws,
+                                    size_t ws_bytes, spec_stream stream) {
+  spec::DenseDims d;
+  spec_status st = resolve_dense(dm, SPEC_DENSE_WINDOW_DECODE, &d);
+  if (st != SPEC_OK) return st;
+  if (!q || !k_cache || !v_cache || !seq_lens || !out) return SPEC_ERR_INVALID;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned4(seq_lens) ||
+      !aligned16(out) || (lse && !aligned4(lse)))
+    return SPEC_ERR_INVALID;
+  if ((st = check_dense_ws(d, SPEC_DENSE_WINDOW_DECODE, ws, ws_bytes)) != SPEC_OK) return st;
+  const hipStream_t s = as_stream(stream);
+  if (debug_on() && (st = debug_range(seq_lens, d.B, 0, d.L_cap, s)) != SPEC_OK) return st;
+  return finish(
+      hip_status(spec::launch_window_decode(d, q, k_cache, v_cache, seq_lens, out, lse, ws, s)),
+      s);
+}
+
+spec_status spec_window_attn(const spec_dense_dims* dm, const uint16_t* q,
+                             const uint16_t* k_cache, const uint16_t* v_cache,
+                             const int32_t* seq_lens, const int32_t* q_lens, uint16_t* out,
+                             float* lse, void* ws, size_t ws_bytes, spec_stream stream) {
+  spec::DenseDims d;
+  spec_status st = resolve_dense(dm, SPEC_DENSE_WINDOW, &d);
+  if (st != SPEC_OK) return st;
+  if (!q || !k_cache || !v_cache || !seq_lens || !out) return SPEC_ERR_INVALID;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned4(seq_lens) ||
+      (q_lens && !aligned4(q_lens)) || !aligned16(out) || (lse && !aligned4(lse)))
+    return SPEC_ERR_INVALID;
+  if ((st = check_dense_ws(d, SPEC_DENSE_WINDOW, ws, ws_bytes)) != SPEC_OK) return st;
+  const hipStream_t s = as_stream(stream);
+  if (debug_on() && ((st = debug_range(seq_lens, d.B, 0, d.L_cap, s)) != SPEC_OK ||
+                     (st = debug_range(q_lens, d.B, 0, d.T, s)) != SPEC_OK))
+    return st;
+  return finish(hip_status(spec::launch_window(d, q, k_cache, v_cache, seq_lens, q_lens, out, lse,
+                                               ws, s)),
+                s);
+}
+
+spec_status spec_prefix_decode_attn(const spec_dense_dims* dm, const uint16_t* q,
+                                    const uint16_t* k_prefix, const uint16_t* v_prefix,
+                                    const int32_t* prefix_len, const uint16_t* k_cache,
+                                    const uint16_t* v_cache, const int32_t* seq_lens, float* out,
+                                    float* lse, void* ws, size_t ws_bytes, spec_stream stream) {
+  spec::DenseDims d;
+  spec_status st = resolve_dense(dm, SPEC_DENSE_PREFIX_DECODE, &d);
+  if (st != SPEC_OK) return st;
+  if (!q || !k_prefix || !v_prefix || !k_cache || !v_cache || !seq_lens || !out)
+    return SPEC_ERR_INVALID;
+  if (!aligned16(q) || !aligned16(k_prefix) || !aligned16(v_prefix) ||
+      (prefix_len && !aligned4(prefix_len)) || !aligned16(k_cache) || !aligned16(v_cache) ||
+      !aligned4(seq_lens) || !aligned16(out) || (lse && !aligned4(lse)))
+    return SPEC_ERR_INVALID;
+  if ((st = check_dense_ws(d, SPEC_DENSE_PREFIX_DECODE, ws, ws_bytes)) != SPEC_OK) return st;
+  const hipStream_t s = as_stream(stream);
+  if (debug_on() && ((st = debug_range(seq_lens, d.B, 0, d.L_cap, s)) != SPEC_OK ||
+                     (st = debug_range(prefix_len, 1, 0, d.P_cap, s)) != SPEC_OK))
+    return st;
+  return finish(hip_status(spec::launch_prefix_decode(d, q, k_prefix, v_prefix, prefix_len,
+                                                      k_cache, v_cache, seq_lens, out, lse, ws,
+                                                      s)),
+                s);
+}
+
+spec_status spec_accum_decode_attn(const spec_dense_dims* dm, const uint16_t* q,
+                                   const uint16_t* k_cache, const uint16_t* v_cache,
+                                   const int32_t* counts, float* weights, float* out, float* lse,
+                                   void* ws, size_t ws_bytes, spec_stream stream) {
+  spec::DenseDims d;
+  spec_status st = resolve_dense(dm, SPEC_DENSE_ACCUM_DECODE, &d);
+  if (st != SPEC_OK) return st;
+  if (!q || !k_cache || !v_cache || !counts || !weights || !out) return SPEC_ERR_INVALID;
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned4(counts) ||
+      !aligned4(weights) || !aligned16(out) || (lse && !aligned4(lse)))
+    return SPEC_ERR_INVALID;
+  if ((st = check_dense_ws(d, SPEC_DENSE_ACCUM_DECODE, ws, ws_bytes)) != SPEC_OK) return st;
+  const hipStream_t s = as_stream(stream);
+  if (debug_on() && (st = debug_range(counts, d.B, 0, d.L_cap, s)) != SPEC_OK) return st;
+  return finish(hip_status(spec::launch_accum_decode(d, q, k_cache, v_cache, counts, weights, out,
+                                                     lse, ws, s)),
+                s);
+}
+
+spec_status spec_evict(const spec_dense_dims* dm, const spec_bounded* cache, const int32_t* keep,
+                       const int32_t* pos, const uint16_t* k_new, const uint16_t* v_new,
+                       const int32_t* n_new, void* ws, size_t ws_bytes, spec_stream stream) {
+  spec::DenseDims d;
+  spec_status st = resolve_dense(dm, SPEC_DENSE_EVICT, &d);
+  if (st != SPEC_OK) return st;
+  if (!cache || !cache->k || !cache->v || !cache->weights || !cache->tokens || !cache->counts ||
+      !keep || !pos || (d.T > 0 && (!k_new || !v_new)))
+    return SPEC_ERR_INVALID;
+  if (!aligned16(cache->k) || !aligned16(cache->v) || !aligned4(cache->weights) ||
+      !aligned4(cache->tokens) || !aligned4(cache->counts) || !aligned4(keep) || !aligned4(pos) ||
+      (k_new && !aligned16(k_new)) || (v_new && !aligned16(v_new)) || (n_new && !aligned4(n_new)))
+    return SPEC_ERR_INVALID;
+  if ((st = check_dense_ws(d, SPEC_DENSE_EVICT, ws, ws_bytes)) != SPEC_OK) return st;
+  const hipStream_t s = as_stream(stream);
+  if (debug_on() && ((st = debug_range(cache->counts, d.B, 0, d.L_cap, s)) != SPEC_OK ||
+                     (st = debug_range(keep, d.B, 0, d.L_cap, s)) != SPEC_OK ||
+                     (st = debug_range(n_new, d.B, 0, d.T, s)) != SPEC_OK))
+    return st;
+  const spec::EvictArgs x{cache->k, cache->v, cache->weights, cache->tokens, cache->counts,
+                          keep,     pos,      k_new,          v_new,         n_new};
+  return finish(hip_status(spec::launch_evict(d, x, ws, s)), s);
 }
 
 spec_status spec_workspace_size(const spec_dims* dm, spec_op op, size_t* bytes) {

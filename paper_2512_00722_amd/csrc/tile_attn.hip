@@ -1,0 +1,744 @@
+// Attention of many query rows over one range of cached tokens, on gfx950: the
+// chunks of window attention (Sec. 4.3's GQA layout; the rows are the query
+// tokens of a sequence times the query heads of a KV head), and the shared part
+// of prefix attention (the rows are the sequences of the batch times the heads).
+//
+// One pass over the tokens with a running maximum and sum per row:
+//     m' = max(m, max_t s_t),  l' = l 2^(m-m') + sum_t 2^(s_t-m'),
+//     O' = O 2^(m-m') + sum_t 2^(s_t-m') v_t,     s_t = scale log2(e) q.k_t
+// Tiles of TOK tokens go through LDS (two buffers; the next tile's loads are in
+// flight in registers while this one is multiplied).  A wavefront owns 32 rows:
+//  * S^T = K Q^T with v_mfma_f32_32x32x16_bf16 leaves a row's logits in one lane
+//    (and its partner 32 lanes on), so that the softmax needs one lane swap;
+//  * O^T += V^T P^T takes P from those registers as they are: the token order
+//    inside a multiplication is free, and V is read transposed from LDS
+//    (ds_read_b64_tr_b16) in the same order.
+#include <float.h>
+
+#include "device_common.h"
+#include "internal.h"
+
+namespace spec {
+namespace {
+
+constexpr int kD = kHeadDim;
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// The running maximum before the first logit: finite, so that logits of -inf
+// weigh nothing from the first tile on.
+constexpr float kNoMax = -FLT_MAX;
+// The maximum is moved, and what has been added up rescaled, only once a logit
+// is 2^8 above it: until then weights are up to 2^8, which neither the fp32 sums
+// nor the bf16 weights (whose precision is relative) notice.
+constexpr float kSlack = 8.f;
+
+struct TileArgs {
+  const uint16_t* q;      // [units / H_kv][T][H_q][d]
+  const uint16_t* k;
+  const uint16_t* v;
+  const int32_t* lens;    // window: cached tokens [B]; prefix: [1] or null (L_cap)
+  const int32_t* q_lens;  // window: [B] or null (T)
+  uint16_t* out;          // window, one split: [units / H_kv][T][H_q][d] bf16
+  float* lse;             // [units / H_kv][T][H_q] or null
+  float* part_acc;        // [units][n_rt][n_split][ROWS][d]
+  float* part_ml;         // [units][n_rt][n_split][ROWS][2]
+  int64_t stride_layer, stride_b;  // elements between layers / sequences of K and V
+  int B, T, H_q, H_kv, G, L_cap, window, n_sink;
+  int n_units, n_rt, n_split, split_tok;
+  float scale_log2;
+};
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The value of the lane 32 on (each row lives in two lanes).
+__device__ __forceinline__ float pair_max(float v) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+__device__ __forceinline__ float pair_sum(float v) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+
+__device__ __forceinline__ bf16x4 lds_read_tr(const uint16_t* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+      (__attribute__((address_space(3))) bf16x4*)(p));
+}
+
+__device__ __forceinline__ bf16x8 to_bf16x8(const float* p) {  // round to nearest even
+  bf16x8 r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const bf16x2 h = __builtin_convertvector(floatx2{p[2 * j], p[2 * j + 1]}, bf16x2);
+    r[2 * j] = h[0];
+    r[2 * j + 1] = h[1];
+  }
+  return r;
+}
+
+// The 16-byte pieces of a 256-byte row stand at piece ^ swizzle(token): the 16
+// rows that a quarter of a K read touches then lie in different banks, and so do
+// the four rows of a transposing V read.
+__device__ __forceinline__ int swizzle(int token) {
+  return ((token & 3) << 2) | ((token >> 2) & 3);
+}
+
+// Visible tokens of the query items i0..i1 of one sequence (len cached tokens, n
+// query tokens, item i at position len - n + i), numbered 0 .. count-1: the first
+// n_sink are themselves, the others stand `shift` further on.
+struct Range {
+  int count, n_sink, shift;
+};
+__device__ __forceinline__ Range window_range(const TileArgs& a, int p0, int i0, int i1) {
+  const int hi = p0 + i1 + 1;  // behind the last visible token
+  if (hi <= 0) return {0, 0, 0};
+  const int s = min(a.n_sink, hi);
+  const int lo = max(p0 + i0 - a.window + 1, s);
+  return {s + hi - lo, s, lo - s};
+}
+
+// Two bf16 values: is one an infinity or a NaN; both with those replaced by 0.
+__device__ __forceinline__ bool odd2(uint32_t x) {
+  return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+}
+__device__ __forceinline__ uint32_t finite2(uint32_t x) {
+  if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+  if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+  return x;
+}
+
+// RW x TW wavefronts: RW groups of 32 rows, TW parts of each tile's tokens.
+// WINDOW: masked rows of a sequence; else every row sees all tokens.  SPLITP:
+// weights as a bf16 pair (~2^-18 relative) for fp32 results; else rounded to
+// bf16 once (2^-9), which the rounding of a bf16 result hides.
+template <int RW, int TW, int TOK, bool WINDOW, bool SPLITP>
+__global__ __launch_bounds__(RW* TW * 64) __attribute__((amdgpu_waves_per_eu(TOK == 64 ? 2 : 1)))
+void tile_attn_kernel(TileArgs a) {
+  constexpr int NT = RW * TW * 64;
+  constexpr int ROWS = 32 * RW;
+  constexpr int NB = TOK / (32 * TW);      // 32-token blocks of a wavefront
+  constexpr int LD = TOK * 16 / NT;        // 16-byte loads of a thread for K, and for V
+  __shared__ __align__(16) uint16_t lds[2][2][TOK * kD];
+  __shared__ int odd_tile[2];  // the last tile in the buffer that holds an odd value (see below)
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int rw = wave % RW, tw = wave / RW;
+  const int c32 = lane & 31, kg = lane >> 5;
+
+  // Units run fastest over the workgroups: those of one KV head keep to one XCD
+  // where the units are a multiple of 8, and share its L2.  The last rows, which
+  // see the most tokens, go first.
+  const int u = blockIdx.x % a.n_units;
+  const int rest = blockIdx.x / a.n_units;
+  const int split = rest % a.n_split;
+  const int rt = a.n_rt - 1 - rest / a.n_split;
+  const int lb = u / a.H_kv, g = u % a.H_kv;
+  const int b = lb % a.B;
+
+  int n_items = a.T, p0 = 0;
+  Range rg;
+  const int r0 = rt * ROWS;
+  if (WINDOW) {
+    const int len = clampi(a.lens[b], 0, a.L_cap);
+    if (a.q_lens) n_items = clampi(a.q_lens[b], 0, a.T);
+    p0 = len - n_items;
+  }
+  const int n_rows = n_items * a.G;
+  if (r0 >= n_rows) return;  // uniform
+  const int i0 = r0 / a.G, i1 = (min(r0 + ROWS, n_rows) - 1) / a.G;
+  if (WINDOW) rg = window_range(a, p0, i0, i1);
+  else rg = {a.lens ? clampi(a.lens[0], 0, a.L_cap) : a.L_cap, 0, 0};
+  const int v0 = split * a.split_tok;
+  const int v1 = min(v0 + a.split_tok, rg.count);
+  const int n_tiles = v1 > v0 ? (v1 - v0 + TOK - 1) / TOK : 0;
+
+  // this lane's row
+  const int row = r0 + rw * 32 + c32;
+  const bool row_ok = row < n_rows;
+  const int rc = min(row, n_rows - 1);
+  const int item = rc / a.G;
+  const int pos = p0 + item;
+  const size_t orow = ((size_t)lb * a.T + item) * a.H_q + (size_t)g * a.G + (rc - item * a.G);
+
+  bf16x8 qf[8];
+  {
+    const uint16_t* qp = a.q + orow * kD + 8 * kg;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) qf[s] = __builtin_bit_cast(bf16x8, ldg16(qp + 16 * s));
+  }
+
+  const int64_t rs = (int64_t)a.H_kv * kD;
+  const int64_t base = (int64_t)(lb / a.B) * a.stride_layer + (int64_t)b * a.stride_b + g * kD;
+  const uint16_t* kb = a.k + base + (tid & 15) * 8;
+  const uint16_t* vb = a.v + base + (tid & 15) * 8;
+
+  uint4 kr[LD], vr[LD];
+  auto token_of = [&](int j) { return j + (j < rg.n_sink ? 0 : rg.shift); };
+  auto issue = [&](int it) {  // tokens past the range read its last one
+#pragma unroll
+    for (int p = 0; p < LD; ++p) {
+      const int j = min(v0 + it * TOK + (tid >> 4) + p * (NT / 16), v1 - 1);
+      const int64_t off = (int64_t)token_of(j) * rs;
+      kr[p] = ldg16(kb + off);
+      vr[p] = ldg16(vb + off);
+    }
+  };
+  // Tiles that every row sees whole need no mask (uniform).
+  auto needs_mask = [&](int it) {
+    const int j0 = v0 + it * TOK, jl = j0 + TOK - 1;
+    if (!WINDOW) return jl >= v1;
+    const int first = j0 < rg.n_sink ? rg.n_sink + rg.shift : token_of(j0);  // behind the sinks
+    return jl >= v1 || token_of(jl) > p0 + i0 ||
+           (jl >= rg.n_sink && first <= p0 + i1 - a.window);
+  };
+  auto put = [&](int it) {
+    const int buf = it & 1;
+#pragma unroll
+    for (int p = 0; p < LD; ++p) {
+      const int r = (tid >> 4) + p * (NT / 16);
+      const int o = r * kD + (((tid & 15) ^ swizzle(r)) * 8);
+      *reinterpret_cast<uint4*>(&lds[buf][0][o]) = kr[p];
+      *reinterpret_cast<uint4*>(&lds[buf][1][o]) = vr[p];
+    }
+    // A weight of 0 does not keep an infinity or a NaN of a row that is masked
+    // for this query but not for another out of the sums: such tiles are marked.
+    if (WINDOW && needs_mask(it)) {
+      bool odd = false;
+#pragma unroll
+      for (int p = 0; p < LD; ++p)
+        odd = odd || odd2(vr[p].x) || odd2(vr[p].y) || odd2(vr[p].z) || odd2(vr[p].w);
+      if (odd) odd_tile[buf] = it;
+    }
+  };
+
+  float m_run = kNoMax, l_run = 0.f;
+  floatx16 acc[4];  // O^T[32 db + 8 (i / 4) + 4 kg + i % 4][row]
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[db][i] = 0.f;
+
+  // LDS offsets of this lane: K rows c32 of a block, V rows of a transposing read
+  const int ksw = kg ^ swizzle(c32);
+  const int a16 = lane & 15, half16 = (lane >> 4) & 1;
+
+  if (tid < 2) odd_tile[tid] = -1;
+  __syncthreads();
+  if (n_tiles > 0) {
+    issue(0);
+    put(0);
+    if (n_tiles > 1) issue(1);
+  }
+  __syncthreads();
+
+  for (int it = 0; it < n_tiles; ++it) {
+    const uint16_t* Kt = lds[it & 1][0];
+    const uint16_t* Vt = lds[it & 1][1];
+    const int j0 = v0 + it * TOK;
+
+    // S^T of this wavefront's blocks: token 32 blk + 8 (i / 4) + 4 kg + i % 4
+    floatx16 s[NB];
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[blk][i] = 0.f;
+      const uint16_t* kp = Kt + ((tw * NB + blk) * 32 + c32) * kD;
+#pragma unroll
+      for (int st = 0; st < 8; ++st) {
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kp + (((2 * st) ^ ksw) * 8));
+        s[blk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[blk], 0, 0, 0);
+      }
+    }
+
+    const bool masked = needs_mask(it);
+    const bool odd = WINDOW && masked && odd_tile[it & 1] == it;  // uniform
+    if (masked) {
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = j0 + (tw * NB + blk) * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
+          bool see = j < v1;
+          if (WINDOW) {
+            const int t = token_of(j);
+            see = see && t <= pos && (t < a.n_sink || t > pos - a.window);
+          }
+          s[blk][i] = see ? s[blk][i] : -INFINITY;
+        }
+    }
+
+    float mx = -INFINITY;
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[blk][i]);
+    mx = pair_max(mx) * a.scale_log2;
+    if (__any(mx > m_run + kSlack)) {
+      const float mn = fmaxf(m_run, mx);
+      const float alpha = exp2_fast(m_run - mn);
+      m_run = mn;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < 4; ++db) acc[db] *= alpha;
+    }
+
+    bf16x8 ph[2 * NB], pl[SPLITP ? 2 * NB : 1];
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
+      float p[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[i] = exp2_fast(fmaf(s[blk][i], a.scale_log2, -m_run));
+        l_run += p[i];
+      }
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        ph[2 * blk + m] = to_bf16x8(p + 8 * m);
+        if constexpr (SPLITP) {
+          float lo[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) lo[e] = p[8 * m + e] - (float)ph[2 * blk + m][e];
+          pl[2 * blk + m] = to_bf16x8(lo);
+        }
+      }
+    }
+
+    // O^T += V^T P^T: slots 8 kg .. 8 kg + 7 of a multiplication are tokens
+    // 16 m + 4 kg + 0..3 and 16 m + 8 + 4 kg + 0..3, as this lane holds P.
+    auto add_pv = [&](auto&& values) {
+#pragma unroll
+      for (int m = 0; m < 2 * NB; ++m) {
+        const uint16_t* vp =
+            Vt + ((tw * NB) * 32 + 16 * m + 4 * kg + (a16 >> 2)) * kD + 4 * (a16 & 1);
+        const int lo0 = (2 * half16 + ((a16 >> 1) & 1)) ^ kg;
+#pragma unroll
+        for (int db = 0; db < 4; ++db) {
+          const int hi4 = 4 * (db ^ (a16 >> 2));
+          const bf16x4 x = lds_read_tr(vp + (hi4 + lo0) * 8);
+          const bf16x4 y = lds_read_tr(vp + 8 * kD + (hi4 + (lo0 ^ 2)) * 8);
+          const bf16x8 vf = values(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, ph[m], acc[db], 0, 0, 0);
+          if constexpr (SPLITP)
+            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl[m], acc[db], 0, 0, 0);
+        }
+      }
+    };
+    if (!(WINDOW && odd)) {
+      add_pv([](bf16x8 x) { return x; });
+    } else {
+      // Infinities and NaNs as 0, and then each row that holds one, for the
+      // queries that see it.
+      add_pv([](bf16x8 x) {
+        const uint4 w = __builtin_bit_cast(uint4, x);
+        return __builtin_bit_cast(
+            bf16x8, make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w)));
+      });
+      for (int r = 0; r < 32 * NB; ++r) {
+        const int tr = tw * NB * 32 + r;  // row of the tile
+        const uint16_t* vp = Vt + tr * kD;
+        if (!__any(odd2(reinterpret_cast<const uint32_t*>(vp)[lane]))) continue;
+        const int j = j0 + tr, t = token_of(j);
+        const bool see = j < v1 && t <= pos && (t < a.n_sink || t > pos - a.window);
+        float sv = 0.f;  // the logit: register (r / 8, r % 4) of block r / 32, half (r / 4) % 2
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (r >> 5 == blk && ((r >> 3) & 3) * 4 + (r & 3) == i) sv = s[blk][i];
+        sv = __shfl(sv, c32 + 32 * ((r >> 2) & 1));
+        const float w = exp2_fast(fmaf(sv, a.scale_log2, -m_run));
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int piece = (4 * db + e) ^ swizzle(tr);  // dims 32 db + 8 e ..
+            const uint2 x = *reinterpret_cast<const uint2*>(vp + piece * 8 + 4 * kg);
+            const float f[4] = {bf16lo(x.x), bf16hi(x.x), bf16lo(x.y), bf16hi(x.y)};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              acc[db][4 * e + i] += see && !(fabsf(f[i]) <= FLT_MAX) ? w * f[i] : 0.f;
+          }
+      }
+    }
+
+    // The other buffer was last read before the previous barrier.
+    if (it + 1 < n_tiles) put(it + 1);
+    if (it + 2 < n_tiles) issue(it + 2);
+    __syncthreads();
+  }
+  l_run = pair_sum(l_run);
+
+  // The parts of a row group, joined by its first wavefront: accumulators stand
+  // in the same lanes of each.
+  if constexpr (TW > 1) {
+    static_assert((TW - 1) * RW * 64 * (64 + 2) * 4 <= sizeof(lds), "merge area");
+    float* mem = reinterpret_cast<float*>(lds);
+    constexpr int kPer = 64 * 66;  // floats of a wavefront: 16 x 64 float4, 64 x (m, l)
+    if (tw > 0) {
+      float* w = mem + ((tw - 1) * RW + rw) * kPer;
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<float4*>(w + ((db * 4 + e) * 64 + lane) * 4) = make_float4(
+              acc[db][4 * e], acc[db][4 * e + 1], acc[db][4 * e + 2], acc[db][4 * e + 3]);
+      *reinterpret_cast<float2*>(w + 64 * 64 + lane * 2) = make_float2(m_run, l_run);
+    }
+    __syncthreads();
+    if (tw > 0) return;
+#pragma unroll
+    for (int o = 1; o < TW; ++o) {
+      const float* w = mem + ((o - 1) * RW + rw) * kPer;
+      const float2 ml = *reinterpret_cast<const float2*>(w + 64 * 64 + lane * 2);
+      const float mn = fmaxf(m_run, ml.x);
+      const float f0 = exp2_fast(m_run - mn), f1 = exp2_fast(ml.x - mn);
+      m_run = mn;
+      l_run = l_run * f0 + ml.y * f1;
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 x = *reinterpret_cast<const float4*>(w + ((db * 4 + e) * 64 + lane) * 4);
+          acc[db][4 * e] = acc[db][4 * e] * f0 + x.x * f1;
+          acc[db][4 * e + 1] = acc[db][4 * e + 1] * f0 + x.y * f1;
+          acc[db][4 * e + 2] = acc[db][4 * e + 2] * f0 + x.z * f1;
+          acc[db][4 * e + 3] = acc[db][4 * e + 3] * f0 + x.w * f1;
+        }
+    }
+  }
+
+  if (!row_ok) return;
+  if (WINDOW && a.n_split == 1) {
+    const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+    uint16_t* dst = a.out + orow * kD + 4 * kg;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        typedef float floatx4v __attribute__((ext_vector_type(4)));
+        const bf16x4 h = __builtin_convertvector(
+            floatx4v{acc[db][4 * e] * inv, acc[db][4 * e + 1] * inv, acc[db][4 * e + 2] * inv,
+                     acc[db][4 * e + 3] * inv}, bf16x4);
+        *reinterpret_cast<uint2*>(dst + 32 * db + 8 * e) = __builtin_bit_cast(uint2, h);
+      }
+    if (a.lse && kg == 0) a.lse[orow] = (m_run + log2f(l_run)) * kLn2;
+    return;
+  }
+  // a part without tokens leaves a sum of 0, and no accumulators
+  const size_t prow = (((size_t)u * a.n_rt + rt) * a.n_split + split) * ROWS + rw * 32 + c32;
+  if (kg == 0) reinterpret_cast<float2*>(a.part_ml)[prow] = make_float2(m_run, l_run);
+  if (n_tiles == 0) return;
+  float* dst = a.part_acc + prow * kD + 4 * kg;
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<float4*>(dst + 32 * db + 8 * e) = make_float4(
+          acc[db][4 * e], acc[db][4 * e + 1], acc[db][4 * e + 2], acc[db][4 * e + 3]);
+}
+
+// Joins partial results: weights 2^(m - M), parts whose sum is 0 left out (their
+// accumulators may never have been written).
+struct Join {
+  float M = kNoMax, L = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  __device__ __forceinline__ void add(const float2 ml, const float* acc, int d4) {
+    if (ml.y == 0.f) return;
+    const float4 x = reinterpret_cast<const float4*>(acc)[d4];
+    const float mn = fmaxf(M, ml.x);
+    const float f0 = exp2f(M - mn), f1 = exp2f(ml.x - mn);
+    M = mn;
+    L = L * f0 + ml.y * f1;
+    o.x = o.x * f0 + x.x * f1;
+    o.y = o.y * f0 + x.y * f1;
+    o.z = o.z * f0 + x.z * f1;
+    o.w = o.w * f0 + x.w * f1;
+  }
+  __device__ __forceinline__ float inv() const { return L == 0.f ? 0.f : 1.f / L; }
+  __device__ __forceinline__ float lse() const { return (M + log2f(L)) * kLn2; }
+};
+
+// One output row per 32 lanes (4 dimensions each), 8 per workgroup.
+__global__ __launch_bounds__(256) void window_merge_kernel(TileArgs a, int rows_per_tile,
+                                                           int64_t n_out) {
+  const int64_t orow = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int d4 = threadIdx.x & 31;
+  if (orow >= n_out) return;
+  const int h = (int)(orow % a.H_q);
+  const int64_t rest = orow / a.H_q;
+  const int i = (int)(rest % a.T), lb = (int)(rest / a.T);
+  if (a.q_lens && i >= clampi(a.q_lens[lb % a.B], 0, a.T)) return;
+  const int g = h / a.G;
+  const int r = i * a.G + (h - g * a.G);
+  const size_t part = ((size_t)lb * a.H_kv + g) * a.n_rt + r / rows_per_tile;
+  Join j;
+  for (int s = 0; s < a.n_split; ++s) {
+    const size_t prow = (part * a.n_split + s) * rows_per_tile + r % rows_per_tile;
+    j.add(reinterpret_cast<const float2*>(a.part_ml)[prow], a.part_acc + prow * kD, d4);
+  }
+  const float inv = j.inv();
+  typedef float floatx4v __attribute__((ext_vector_type(4)));
+  const bf16x4 o = __builtin_convertvector(
+      floatx4v{j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv}, bf16x4);
+  reinterpret_cast<uint2*>(a.out + orow * kD)[d4] = __builtin_bit_cast(uint2, o);
+  if (a.lse && d4 == 0) a.lse[orow] = j.lse();
+}
+
+// The prefix's partial results and those of the sequence's own tokens.
+__global__ __launch_bounds__(256) void prefix_merge_kernel(TileArgs a, int rows_per_tile,
+                                                           AttnParts own, const int32_t* own_lens,
+                                                           int own_cap, float* out, float* lse,
+                                                           int64_t n_out) {
+  const int64_t orow = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int d4 = threadIdx.x & 31;
+  if (orow >= n_out) return;
+  const int h = (int)(orow % a.H_q);
+  const int64_t lb = orow / a.H_q;                       // layer * batch + sequence
+  const int b = (int)(lb % a.T), layer = (int)(lb / a.T);  // T: the batch
+  const int g = h / a.G;
+  const int r = b * a.G + (h - g * a.G);
+  const size_t part = ((size_t)layer * a.H_kv + g) * a.n_rt + r / rows_per_tile;
+  Join j;
+  for (int s = 0; s < a.n_split; ++s) {
+    const size_t prow = (part * a.n_split + s) * rows_per_tile + r % rows_per_tile;
+    j.add(reinterpret_cast<const float2*>(a.part_ml)[prow], a.part_acc + prow * kD, d4);
+  }
+  const int count = clampi(own_lens[b], 0, own_cap);
+  const int ns = min(own.n_split, (count + own.split - 1) / own.split);
+  for (int s = 0; s < ns; ++s) {
+    const size_t prow = ((size_t)lb * own.n_split + s) * a.H_q + h;
+    j.add(reinterpret_cast<const float2*>(own.ml)[prow], own.acc + prow * kD, d4);
+  }
+  const float inv = j.inv();
+  reinterpret_cast<float4*>(out + orow * kD)[d4] =
+      make_float4(j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv);
+  if (lse && d4 == 0) lse[orow] = j.lse();
+}
+
+// Rows of a workgroup, tokens of a tile, and how the tokens are split.
+struct TilePlan {
+  int rows, tok, n_rt, n_split, split_tok;
+};
+
+constexpr int kMinSplit = 256;
+
+// units: (layer, sequence, KV head); rows: query rows of a unit; most: the most
+// tokens that a row tile of `rows` sees.
+TilePlan tile_plan(int64_t units, int64_t rows, int64_t most) {
+  TilePlan p;
+  p.rows = rows > 128 ? 256 : rows > 64 ? 128 : rows > 32 ? 64 : 32;
+  while (p.rows > 64 && units * ((rows + p.rows - 1) / p.rows) < kCUs) p.rows /= 2;
+  p.tok = p.rows == 32 ? 128 : 64;
+  p.n_rt = (int)((rows + p.rows - 1) / p.rows);
+  const int64_t wgs = units * p.n_rt;
+  const int64_t target = p.rows == 256 || p.rows == 32 ? kCUs : 2 * kCUs;
+  int64_t ns = (target + wgs - 1) / wgs;
+  const int64_t cap = (most + kMinSplit - 1) / kMinSplit;
+  if (ns > cap) ns = cap;
+  if (ns < 1) ns = 1;
+  const int64_t per = ((most + ns - 1) / ns + p.tok - 1) / p.tok * p.tok;
+  p.split_tok = (int)(per < p.tok ? p.tok : per);
+  p.n_split = (int)((most + p.split_tok - 1) / p.split_tok);
+  if (p.n_split < 1) p.n_split = 1;
+  return p;
+}
+
+size_t tile_acc_bytes(int64_t units, const TilePlan& p) {
+  return align_up(sizeof(float) * kD * (size_t)units * p.n_rt * p.n_split * p.rows);
+}
+size_t tile_ml_bytes(int64_t units, const TilePlan& p) {
+  return align_up(sizeof(float) * 2 * (size_t)units * p.n_rt * p.n_split * p.rows);
+}
+
+template <bool WINDOW, bool SPLITP>
+hipError_t launch_tiles(const TilePlan& p, const TileArgs& a, hipStream_t s) {
+  const int64_t n = (int64_t)a.n_units * a.n_rt * a.n_split;
+  if (n > INT32_MAX) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)n);
+  if (p.rows == 256) tile_attn_kernel<8, 1, 64, WINDOW, SPLITP><<<grid, 512, 0, s>>>(a);
+  else if (p.rows == 128) tile_attn_kernel<4, 1, 64, WINDOW, SPLITP><<<grid, 256, 0, s>>>(a);
+  else if (p.rows == 64) tile_attn_kernel<2, 2, 64, WINDOW, SPLITP><<<grid, 256, 0, s>>>(a);
+  else tile_attn_kernel<1, 4, 128, WINDOW, SPLITP><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+TilePlan window_plan(const DenseDims& d) {
+  const int64_t units = (int64_t)d.n_layers * d.B * d.H_kv;
+  // a row tile of r rows covers at most (r - 2) / G + 2 query tokens
+  int64_t most = (int64_t)d.window + d.n_sink + (256 - 2) / d.G + 1;
+  if (most > d.L_cap) most = d.L_cap;
+  return tile_plan(units, (int64_t)d.T * d.G, most);
+}
+
+TilePlan prefix_plan(const DenseDims& d) {
+  return tile_plan((int64_t)d.n_layers * d.H_kv, (int64_t)d.B * d.G, d.P_cap);
+}
+
+// One query token per sequence, as the attention kernels take it: k_max tokens.
+Dims decode_dims(const DenseDims& d, int k_max) {
+  Dims o{};
+  o.B = d.B;
+  o.L_cap = o.L_max = d.L_cap;
+  o.k_max = k_max;
+  o.n_layers = d.n_layers;
+  o.H_q = d.H_q;
+  o.H_kv = d.H_kv;
+  o.d = kD;
+  o.G = d.G;
+  o.n_sets = 1;
+  o.kv_stride_b = d.kv_stride_b;
+  o.kv_stride_layer = d.kv_stride_layer;
+  o.scale = d.scale;
+  o.plain = false;
+  return o;
+}
+int window_tokens(const DenseDims& d) {
+  const int64_t n = (int64_t)d.window + d.n_sink;
+  return (int)(n < d.L_cap ? n : d.L_cap);
+}
+
+}  // namespace
+
+size_t window_ws_bytes(const DenseDims& d) {
+  const TilePlan p = window_plan(d);
+  const int64_t units = (int64_t)d.n_layers * d.B * d.H_kv;
+  return p.n_split > 1 ? tile_acc_bytes(units, p) + tile_ml_bytes(units, p) : 0;
+}
+
+hipError_t launch_window(const DenseDims& d, const uint16_t* q, const uint16_t* k,
+                         const uint16_t* v, const int32_t* lens, const int32_t* q_lens,
+                         uint16_t* out, float* lse, void* ws, hipStream_t s) {
+  const TilePlan p = window_plan(d);
+  const int64_t units = (int64_t)d.n_layers * d.B * d.H_kv;
+  TileArgs a{q, k, v, lens, q_lens, out, lse, nullptr, nullptr, d.kv_stride_layer, d.kv_stride_b,
+             d.B, d.T, d.H_q, d.H_kv, d.G, d.L_cap, d.window, d.n_sink, (int)units, p.n_rt,
+             p.n_split, p.split_tok, d.scale * kLog2e};
+  if (p.n_split > 1) {
+    a.part_acc = static_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + tile_acc_bytes(units, p));
+  }
+  hipError_t e = launch_tiles<true, false>(p, a, s);
+  if (e != hipSuccess || p.n_split == 1) return e;
+  const int64_t n_out = (int64_t)d.n_layers * d.B * d.T * d.H_q;
+  window_merge_kernel<<<dim3((unsigned)((n_out + 7) / 8)), 256, 0, s>>>(a, p.rows, n_out);
+  return hipGetLastError();
+}
+
+size_t window_decode_ws_bytes(const DenseDims& d) {
+  return attn_dense_ws_bytes(decode_dims(d, window_tokens(d)), false);
+}
+
+hipError_t launch_window_decode(const DenseDims& d, const uint16_t* q, const uint16_t* k,
+                                const uint16_t* v, const int32_t* lens, float* out, float* lse,
+                                void* ws, hipStream_t s) {
+  const DenseAttn m{d.n_sink, nullptr, 0, false, nullptr};
+  return launch_attn_dense(decode_dims(d, window_tokens(d)), m, q, k, v, lens, out, lse, ws, s);
+}
+
+size_t prefix_decode_ws_bytes(const DenseDims& d) {
+  const TilePlan p = prefix_plan(d);
+  const int64_t units = (int64_t)d.n_layers * d.H_kv;
+  return tile_acc_bytes(units, p) + tile_ml_bytes(units, p) +
+         attn_dense_ws_bytes(decode_dims(d, d.L_cap), true);
+}
+
+hipError_t launch_prefix_decode(const DenseDims& d, const uint16_t* q, const uint16_t* k_prefix,
+                                const uint16_t* v_prefix, const int32_t* prefix_len,
+                                const uint16_t* k, const uint16_t* v, const int32_t* lens,
+                                float* out, float* lse, void* ws, hipStream_t s) {
+  const TilePlan p = prefix_plan(d);
+  const int64_t units = (int64_t)d.n_layers * d.H_kv;
+  char* w = static_cast<char*>(ws);
+  TileArgs a{q, k_prefix, v_prefix, prefix_len, nullptr, nullptr, nullptr,
+             reinterpret_cast<float*>(w), reinterpret_cast<float*>(w + tile_acc_bytes(units, p)),
+             d.prefix_stride_layer, 0, 1, d.B, d.H_q, d.H_kv, d.G, d.P_cap, 0, 0, (int)units,
+             p.n_rt, p.n_split, p.split_tok, d.scale * kLog2e};
+  hipError_t e = launch_tiles<false, true>(p, a, s);
+  if (e != hipSuccess) return e;
+  AttnParts own;
+  const DenseAttn m{d.L_cap, nullptr, 0, true, &own};
+  e = launch_attn_dense(decode_dims(d, d.L_cap), m, q, k, v, lens, nullptr, nullptr,
+                        w + tile_acc_bytes(units, p) + tile_ml_bytes(units, p), s);
+  if (e != hipSuccess) return e;
+  const int64_t n_out = (int64_t)d.n_layers * d.B * d.H_q;
+  prefix_merge_kernel<<<dim3((unsigned)((n_out + 7) / 8)), 256, 0, s>>>(a, p.rows, own, lens,
+                                                                        d.L_cap, out, lse, n_out);
+  return hipGetLastError();
+}
+
+// ---- decode attention that adds up its weights ----------------------------
+namespace {
+
+constexpr int kAccumTokens = 1024;  // of a workgroup, four per thread
+
+struct AccumArgs {
+  const float* logits;  // [lb][H_q][stride], log2 units
+  const float* lse;     // [lb][H_q]
+  const int32_t* counts;
+  float* weights;       // [lb][n_sets][L_cap]
+  int64_t stride;
+  int B, H_q, n_sets, L_cap, tiles;  // workgroups of a weights row
+};
+
+// weights[lb][set][t] += sum over the set's heads of 2^(logit - lse log2(e)).
+__global__ __launch_bounds__(256) void accum_kernel(AccumArgs a) {
+  const int tile = blockIdx.x % a.tiles, rest = blockIdx.x / a.tiles;
+  const int set = rest % a.n_sets, lb = rest / a.n_sets;
+  const int count = clampi(a.counts[lb % a.B], 0, a.L_cap);
+  const int t0 = tile * kAccumTokens + threadIdx.x * 4;
+  if (t0 >= count) return;
+  const int heads = a.H_q / a.n_sets;
+  const size_t h0 = (size_t)lb * a.H_q + (size_t)set * heads;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int h = 0; h < heads; ++h) {
+    const float z = a.lse[h0 + h] * kLog2e;
+    if (z == -INFINITY) continue;  // every logit of the head is -inf: no weights
+    const float4 x = *reinterpret_cast<const float4*>(a.logits + (h0 + h) * a.stride + t0);
+    sum.x += exp2f(x.x - z);
+    sum.y += exp2f(x.y - z);
+    sum.z += exp2f(x.z - z);
+    sum.w += exp2f(x.w - z);
+  }
+  float* w = a.weights + ((size_t)lb * a.n_sets + set) * a.L_cap + t0;
+  w[0] += sum.x;
+  if (t0 + 1 < count) w[1] += sum.y;
+  if (t0 + 2 < count) w[2] += sum.z;
+  if (t0 + 3 < count) w[3] += sum.w;
+}
+
+int64_t accum_stride(const DenseDims& d) { return ((int64_t)d.L_cap + 31) / 32 * 32; }
+size_t accum_logit_bytes(const DenseDims& d) {
+  return align_up(sizeof(float) * (size_t)d.n_layers * d.B * d.H_q * accum_stride(d));
+}
+size_t accum_lse_bytes(const DenseDims& d) {
+  return align_up(sizeof(float) * (size_t)d.n_layers * d.B * d.H_q);
+}
+
+}  // namespace
+
+size_t accum_decode_ws_bytes(const DenseDims& d) {
+  return accum_logit_bytes(d) + accum_lse_bytes(d) +
+         attn_dense_ws_bytes(decode_dims(d, d.L_cap), false);
+}
+
+hipError_t launch_accum_decode(const DenseDims& d, const uint16_t* q, const uint16_t* k,
+                               const uint16_t* v, const int32_t* counts, float* weights,
+                               float* out, float* lse, void* ws, hipStream_t s) {
+  char* w = static_cast<char*>(ws);
+  float* logits = reinterpret_cast<float*>(w);
+  float* z = lse ? lse : reinterpret_cast<float*>(w + accum_logit_bytes(d));
+  const DenseAttn m{d.L_cap, logits, accum_stride(d), false, nullptr};
+  const hipError_t e =
+      launch_attn_dense(decode_dims(d, d.L_cap), m, q, k, v, counts, out, z,
+                        w + accum_logit_bytes(d) + accum_lse_bytes(d), s);
+  if (e != hipSuccess) return e;
+  const int tiles = (d.L_cap + kAccumTokens - 1) / kAccumTokens;
+  const AccumArgs a{logits, z, counts, weights, accum_stride(d), d.B, d.H_q, d.n_sets, d.L_cap,
+                    tiles};
+  accum_kernel<<<dim3((unsigned)((int64_t)tiles * d.n_sets * d.n_layers * d.B)), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace spec
