@@ -100,14 +100,59 @@ __device__ __forceinline__ Range window_range(const TileArgs& a, int p0, int i0,
   return {s + hi - lo, s, lo - s};
 }
 
-// Two bf16 values: is one an infinity or a NaN; both with those replaced by 0.
+// Two bf16 values: is one an infinity or a NaN?
 __device__ __forceinline__ bool odd2(uint32_t x) {
   return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
 }
-__device__ __forceinline__ uint32_t finite2(uint32_t x) {
-  if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
-  if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
-  return x;
+
+// The same token by token, for the rare rows that hold infinities or NaNs: those
+// that a query does not see are selected away.  A lane has the dimensions
+// 32 db + 8 e + 4 kg .. + 3 of its row, as the accumulators do.
+template <class TokenOf>
+__device__ __forceinline__ void attend_by_token(const TileArgs& a, const uint16_t* q,
+                                                const uint16_t* k, const uint16_t* v, int64_t rs,
+                                                int kg, int j0, int j1, int pos,
+                                                TokenOf&& token_of, float& m_run, float& l_run,
+                                                floatx16 (&acc)[4]) {
+  auto four = [](const uint16_t* p, float (&f)[4]) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    f[0] = bf16lo(x.x);
+    f[1] = bf16hi(x.x);
+    f[2] = bf16lo(x.y);
+    f[3] = bf16hi(x.y);
+  };
+  m_run = kNoMax;
+  l_run = 0.f;
+#pragma unroll
+  for (int db = 0; db < 4; ++db) acc[db] = 0.f;
+#pragma unroll 1
+  for (int j = j0; j < j1; ++j) {
+    const int t = token_of(j);
+    const int64_t off = (int64_t)t * rs + 4 * kg;
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float x[4], y[4];
+      four(q + 4 * kg + 8 * e, x);
+      four(k + off + 8 * e, y);
+      for (int i = 0; i < 4; ++i) s = fmaf(x[i], y[i], s);
+    }
+    const bool see = t <= pos && (t < a.n_sink || t > pos - a.window);
+    s = pair_sum(s) * a.scale_log2;
+    s = see ? s : -INFINITY;
+    const float mn = fmaxf(m_run, s);
+    const float alpha = exp2_fast(m_run - mn), p = exp2_fast(s - mn);
+    m_run = mn;
+    l_run = l_run * alpha + (kg == 0 ? p : 0.f);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float y[4];
+      four(v + off + 8 * e, y);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        acc[e >> 2][4 * (e & 3) + i] = acc[e >> 2][4 * (e & 3) + i] * alpha + (see ? p * y[i] : 0.f);
+    }
+  }
 }
 
 // RW x TW wavefronts: RW groups of 32 rows, TW parts of each tile's tokens.
@@ -122,7 +167,7 @@ void tile_attn_kernel(TileArgs a) {
   constexpr int NB = TOK / (32 * TW);      // 32-token blocks of a wavefront
   constexpr int LD = TOK * 16 / NT;        // 16-byte loads of a thread for K, and for V
   __shared__ __align__(16) uint16_t lds[2][2][TOK * kD];
-  __shared__ int odd_tile[2];  // the last tile in the buffer that holds an odd value (see below)
+  __shared__ int odd_rows;  // a masked tile holds an infinity or a NaN (see below)
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int rw = wave % RW, tw = wave / RW;
   const int c32 = lane & 31, kg = lane >> 5;
@@ -203,13 +248,14 @@ void tile_attn_kernel(TileArgs a) {
       *reinterpret_cast<uint4*>(&lds[buf][1][o]) = vr[p];
     }
     // A weight of 0 does not keep an infinity or a NaN of a row that is masked
-    // for this query but not for another out of the sums: such tiles are marked.
+    // for this query but not for another out of the sums (0 x NaN): where a
+    // masked tile holds one, everything is done again without the matrix cores.
     if (WINDOW && needs_mask(it)) {
       bool odd = false;
 #pragma unroll
       for (int p = 0; p < LD; ++p)
         odd = odd || odd2(vr[p].x) || odd2(vr[p].y) || odd2(vr[p].z) || odd2(vr[p].w);
-      if (odd) odd_tile[buf] = it;
+      if (odd) odd_rows = 1;
     }
   };
 
@@ -224,8 +270,10 @@ void tile_attn_kernel(TileArgs a) {
   const int ksw = kg ^ swizzle(c32);
   const int a16 = lane & 15, half16 = (lane >> 4) & 1;
 
-  if (tid < 2) odd_tile[tid] = -1;
-  __syncthreads();
+  if (WINDOW) {
+    if (tid == 0) odd_rows = 0;
+    __syncthreads();
+  }
   if (n_tiles > 0) {
     issue(0);
     put(0);
@@ -253,7 +301,6 @@ void tile_attn_kernel(TileArgs a) {
     }
 
     const bool masked = needs_mask(it);
-    const bool odd = WINDOW && masked && odd_tile[it & 1] == it;  // uniform
     if (masked) {
 #pragma unroll
       for (int blk = 0; blk < NB; ++blk)
@@ -307,59 +354,19 @@ void tile_attn_kernel(TileArgs a) {
 
     // O^T += V^T P^T: slots 8 kg .. 8 kg + 7 of a multiplication are tokens
     // 16 m + 4 kg + 0..3 and 16 m + 8 + 4 kg + 0..3, as this lane holds P.
-    auto add_pv = [&](auto&& values) {
 #pragma unroll
-      for (int m = 0; m < 2 * NB; ++m) {
-        const uint16_t* vp =
-            Vt + ((tw * NB) * 32 + 16 * m + 4 * kg + (a16 >> 2)) * kD + 4 * (a16 & 1);
-        const int lo0 = (2 * half16 + ((a16 >> 1) & 1)) ^ kg;
+    for (int m = 0; m < 2 * NB; ++m) {
+      const uint16_t* vp = Vt + ((tw * NB) * 32 + 16 * m + 4 * kg + (a16 >> 2)) * kD + 4 * (a16 & 1);
+      const int lo0 = (2 * half16 + ((a16 >> 1) & 1)) ^ kg;
 #pragma unroll
-        for (int db = 0; db < 4; ++db) {
-          const int hi4 = 4 * (db ^ (a16 >> 2));
-          const bf16x4 x = lds_read_tr(vp + (hi4 + lo0) * 8);
-          const bf16x4 y = lds_read_tr(vp + 8 * kD + (hi4 + (lo0 ^ 2)) * 8);
-          const bf16x8 vf = values(__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, ph[m], acc[db], 0, 0, 0);
-          if constexpr (SPLITP)
-            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl[m], acc[db], 0, 0, 0);
-        }
-      }
-    };
-    if (!(WINDOW && odd)) {
-      add_pv([](bf16x8 x) { return x; });
-    } else {
-      // Infinities and NaNs as 0, and then each row that holds one, for the
-      // queries that see it.
-      add_pv([](bf16x8 x) {
-        const uint4 w = __builtin_bit_cast(uint4, x);
-        return __builtin_bit_cast(
-            bf16x8, make_uint4(finite2(w.x), finite2(w.y), finite2(w.z), finite2(w.w)));
-      });
-      for (int r = 0; r < 32 * NB; ++r) {
-        const int tr = tw * NB * 32 + r;  // row of the tile
-        const uint16_t* vp = Vt + tr * kD;
-        if (!__any(odd2(reinterpret_cast<const uint32_t*>(vp)[lane]))) continue;
-        const int j = j0 + tr, t = token_of(j);
-        const bool see = j < v1 && t <= pos && (t < a.n_sink || t > pos - a.window);
-        float sv = 0.f;  // the logit: register (r / 8, r % 4) of block r / 32, half (r / 4) % 2
-#pragma unroll
-        for (int blk = 0; blk < NB; ++blk)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (r >> 5 == blk && ((r >> 3) & 3) * 4 + (r & 3) == i) sv = s[blk][i];
-        sv = __shfl(sv, c32 + 32 * ((r >> 2) & 1));
-        const float w = exp2_fast(fmaf(sv, a.scale_log2, -m_run));
-#pragma unroll
-        for (int db = 0; db < 4; ++db)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int piece = (4 * db + e) ^ swizzle(tr);  // dims 32 db + 8 e ..
-            const uint2 x = *reinterpret_cast<const uint2*>(vp + piece * 8 + 4 * kg);
-            const float f[4] = {bf16lo(x.x), bf16hi(x.x), bf16lo(x.y), bf16hi(x.y)};
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              acc[db][4 * e + i] += see && !(fabsf(f[i]) <= FLT_MAX) ? w * f[i] : 0.f;
-          }
+      for (int db = 0; db < 4; ++db) {
+        const int hi4 = 4 * (db ^ (a16 >> 2));
+        const bf16x4 x = lds_read_tr(vp + (hi4 + lo0) * 8);
+        const bf16x4 y = lds_read_tr(vp + 8 * kD + (hi4 + (lo0 ^ 2)) * 8);
+        const bf16x8 vf = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, ph[m], acc[db], 0, 0, 0);
+        if constexpr (SPLITP)
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl[m], acc[db], 0, 0, 0);
       }
     }
 
@@ -368,6 +375,9 @@ void tile_attn_kernel(TileArgs a) {
     if (it + 2 < n_tiles) issue(it + 2);
     __syncthreads();
   }
+  if (WINDOW && odd_rows)  // uniform; written before the last barrier
+    attend_by_token(a, a.q + orow * kD, a.k + base, a.v + base, rs, kg, tw == 0 ? v0 : v1, v1, pos,
+                    token_of, m_run, l_run, acc);
   l_run = pair_sum(l_run);
 
   // The parts of a row group, joined by its first wavefront: accumulators stand

@@ -197,16 +197,18 @@ def test_window_odd_values_reach_only_those_that_see_them(dev, T, G, odd):
     for t, dim in bad.items():
         V[0, 0, t, 0, dim] = odd
         clean[0, 0, t, 0, dim] = 0.0
-    lens = i32([cap], dev)
-    got, _ = spec.window_attn(q, K, V, lens, window, n_sink=sinks)
-    want, _ = spec.window_attn(q, K, clean, lens, window, n_sink=sinks)
-    want = want.clone()
+    got, _ = spec.window_attn(q, K, V, i32([cap], dev), window, n_sink=sinks)
+    qq, kk, vv = f64(q[0, 0]), f64(K[0, 0]), f64(clean[0, 0])
+    want, _, spread = dense_oracle.window_attention(qq, kk, vv, cap - T, window, sinks, SCALE)
+    tol = (2 * weight_error(qq, kk, cap) + 2.0 ** -8) * spread + 2.0 ** -8 * np.abs(want) + 1e-30
+    got = f64(got[0, 0])
     for i in range(T):
         seen = set(dense_oracle.visible(cap - T + i, window, sinks))
         for t, dim in bad.items():
             if t in seen:
-                want[0, 0, i, :, dim] = odd
-    assert torch.equal(torch.nan_to_num(got, nan=123.0), torch.nan_to_num(want, nan=123.0))
+                assert (np.isnan(got[i, :, dim]) if odd != odd else got[i, :, dim] == odd).all()
+                got[i, :, dim] = want[i, :, dim]
+    check(got, want, tol, "the other values")
 
 
 def test_window_odd_keys(dev):
