@@ -377,7 +377,7 @@ spec_status resolve_dense(const spec_dense_dims* dm, spec_dense_op op, spec::Den
   if (lb * dm->H_kv > 1 << 21) return SPEC_ERR_UNSUPPORTED;
   if (!evict && lb * dm->H_q > 1 << 26) return SPEC_ERR_UNSUPPORTED;
   if (op == SPEC_DENSE_WINDOW && (lb * dm->H_q * dm->T > 1 << 26)) return SPEC_ERR_UNSUPPORTED;
-  if (op == SPEC_DENSE_ACCUM_DECODE && lb * dm->n_sets * (dm->L_cap / 1024 + 1) > 1 << 23)
+  if (op == SPEC_DENSE_ACCUM_DECODE && lb * dm->n_sets * (dm->L_cap / 64 + 1) > 1 << 23)
     return SPEC_ERR_UNSUPPORTED;
   if ((int64_t)dm->L_cap + dm->T > INT32_MAX - 4096 || dm->P_cap > INT32_MAX - 4096)
     return SPEC_ERR_UNSUPPORTED;

@@ -15,6 +15,8 @@
 //    (ds_read_b64_tr_b16) in the same order.
 #include <float.h>
 
+#include <type_traits>
+
 #include "device_common.h"
 #include "internal.h"
 
@@ -427,9 +429,8 @@ void tile_attn_kernel(TileArgs a) {
     for (int db = 0; db < 4; ++db)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        typedef float floatx4v __attribute__((ext_vector_type(4)));
         const bf16x4 h = __builtin_convertvector(
-            floatx4v{acc[db][4 * e] * inv, acc[db][4 * e + 1] * inv, acc[db][4 * e + 2] * inv,
+            floatx4{acc[db][4 * e] * inv, acc[db][4 * e + 1] * inv, acc[db][4 * e + 2] * inv,
                      acc[db][4 * e + 3] * inv}, bf16x4);
         *reinterpret_cast<uint2*>(dst + 32 * db + 8 * e) = __builtin_bit_cast(uint2, h);
       }
@@ -449,78 +450,131 @@ void tile_attn_kernel(TileArgs a) {
           acc[db][4 * e], acc[db][4 * e + 1], acc[db][4 * e + 2], acc[db][4 * e + 3]);
 }
 
-// Joins partial results: weights 2^(m - M), parts whose sum is 0 left out (their
-// accumulators may never have been written).
+// The joined partial results of one output row, as one thread sees it: its four
+// dimensions, weights 2^(m - M).
 struct Join {
   float M = kNoMax, L = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  __device__ __forceinline__ void add(const float2 ml, const float* acc, int d4) {
-    if (ml.y == 0.f) return;
-    const float4 x = reinterpret_cast<const float4*>(acc)[d4];
-    const float mn = fmaxf(M, ml.x);
-    const float f0 = exp2f(M - mn), f1 = exp2f(ml.x - mn);
-    M = mn;
-    L = L * f0 + ml.y * f1;
-    o.x = o.x * f0 + x.x * f1;
-    o.y = o.y * f0 + x.y * f1;
-    o.z = o.z * f0 + x.z * f1;
-    o.w = o.w * f0 + x.w * f1;
+  __device__ __forceinline__ void rescale(float m) {
+    const float f = exp2f(M - m);
+    M = m;
+    L *= f;
+    o.x *= f;
+    o.y *= f;
+    o.z *= f;
+    o.w *= f;
+  }
+  __device__ __forceinline__ void add(const float2 ml, const float4 x) {  // ml.x <= M
+    const float f = exp2f(ml.x - M);
+    L += ml.y * f;
+    o.x += x.x * f;
+    o.y += x.y * f;
+    o.z += x.z * f;
+    o.w += x.w * f;
   }
   __device__ __forceinline__ float inv() const { return L == 0.f ? 0.f : 1.f / L; }
   __device__ __forceinline__ float lse() const { return (M + log2f(L)) * kLn2; }
 };
 
-// One output row per 32 lanes (4 dimensions each), 8 per workgroup.
+// Joins parts 0 .. n-1 of a row (at(s): pointers to a part's (max, sum) and
+// accumulators) by S groups of 32 threads, of which group 0 has the result.
+// Eight parts of a group are requested together: one round trip for up to 8 S
+// parts.  Parts whose sum is 0 are left out: their accumulators may never have
+// been written.  All threads of the workgroup call.
+template <int S, class At>
+__device__ __forceinline__ Join join_parts(int n, At&& at) {
+  constexpr int kBatch = 8;
+  __shared__ float2 ml_lds[8];
+  __shared__ float4 acc_lds[8][32];
+  const int slot = threadIdx.x >> 5, d4 = threadIdx.x & 31, part = slot % S;
+  Join j;
+  for (int s0 = part; s0 < n; s0 += kBatch * S) {
+    float2 ml[kBatch];
+    float4 x[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {  // clamped: every load is issued
+      const float* acc;
+      const float2* pair;
+      at(min(s0 + u * S, n - 1), pair, acc);
+      ml[u] = *pair;
+      x[u] = reinterpret_cast<const float4*>(acc)[d4];
+    }
+    float m = j.M;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (s0 + u * S < n && ml[u].y != 0.f) m = fmaxf(m, ml[u].x);
+    j.rescale(m);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (s0 + u * S < n && ml[u].y != 0.f) j.add(ml[u], x[u]);
+  }
+  if constexpr (S > 1) {
+    if (d4 == 0) ml_lds[slot] = make_float2(j.M, j.L);
+    acc_lds[slot][d4] = j.o;
+    __syncthreads();
+    if (part == 0) {
+      float m = j.M;
+      for (int p = 1; p < S; ++p) m = fmaxf(m, ml_lds[slot + p].x);
+      j.rescale(m);
+      for (int p = 1; p < S; ++p) j.add(ml_lds[slot + p], acc_lds[slot + p][d4]);
+    }
+  }
+  return j;
+}
+
+// 8 / S output rows per workgroup, 32 threads (4 dimensions each) and S of them.
+template <int S>
 __global__ __launch_bounds__(256) void window_merge_kernel(TileArgs a, int rows_per_tile,
                                                            int64_t n_out) {
-  const int64_t orow = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int64_t want = (int64_t)blockIdx.x * (8 / S) + (threadIdx.x >> 5) / S;
+  const int64_t orow = want < n_out ? want : n_out - 1;
   const int d4 = threadIdx.x & 31;
-  if (orow >= n_out) return;
   const int h = (int)(orow % a.H_q);
   const int64_t rest = orow / a.H_q;
   const int i = (int)(rest % a.T), lb = (int)(rest / a.T);
-  if (a.q_lens && i >= clampi(a.q_lens[lb % a.B], 0, a.T)) return;
+  const bool live = want < n_out && !(a.q_lens && i >= clampi(a.q_lens[lb % a.B], 0, a.T));
   const int g = h / a.G;
   const int r = i * a.G + (h - g * a.G);
   const size_t part = ((size_t)lb * a.H_kv + g) * a.n_rt + r / rows_per_tile;
-  Join j;
-  for (int s = 0; s < a.n_split; ++s) {
+  const Join j = join_parts<S>(live ? a.n_split : 0, [&](int s, const float2*& ml,
+                                                         const float*& acc) {
     const size_t prow = (part * a.n_split + s) * rows_per_tile + r % rows_per_tile;
-    j.add(reinterpret_cast<const float2*>(a.part_ml)[prow], a.part_acc + prow * kD, d4);
-  }
+    ml = reinterpret_cast<const float2*>(a.part_ml) + prow;
+    acc = a.part_acc + prow * kD;
+  });
+  if (!live || (threadIdx.x >> 5) % S != 0) return;
   const float inv = j.inv();
-  typedef float floatx4v __attribute__((ext_vector_type(4)));
   const bf16x4 o = __builtin_convertvector(
-      floatx4v{j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv}, bf16x4);
+      floatx4{j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv}, bf16x4);
   reinterpret_cast<uint2*>(a.out + orow * kD)[d4] = __builtin_bit_cast(uint2, o);
   if (a.lse && d4 == 0) a.lse[orow] = j.lse();
 }
 
 // The prefix's partial results and those of the sequence's own tokens.
+template <int S>
 __global__ __launch_bounds__(256) void prefix_merge_kernel(TileArgs a, int rows_per_tile,
                                                            AttnParts own, const int32_t* own_lens,
                                                            int own_cap, float* out, float* lse,
                                                            int64_t n_out) {
-  const int64_t orow = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int64_t want = (int64_t)blockIdx.x * (8 / S) + (threadIdx.x >> 5) / S;
+  const int64_t orow = want < n_out ? want : n_out - 1;
   const int d4 = threadIdx.x & 31;
-  if (orow >= n_out) return;
   const int h = (int)(orow % a.H_q);
-  const int64_t lb = orow / a.H_q;                       // layer * batch + sequence
+  const int64_t lb = orow / a.H_q;                         // layer * batch + sequence
   const int b = (int)(lb % a.T), layer = (int)(lb / a.T);  // T: the batch
   const int g = h / a.G;
   const int r = b * a.G + (h - g * a.G);
   const size_t part = ((size_t)layer * a.H_kv + g) * a.n_rt + r / rows_per_tile;
-  Join j;
-  for (int s = 0; s < a.n_split; ++s) {
-    const size_t prow = (part * a.n_split + s) * rows_per_tile + r % rows_per_tile;
-    j.add(reinterpret_cast<const float2*>(a.part_ml)[prow], a.part_acc + prow * kD, d4);
-  }
   const int count = clampi(own_lens[b], 0, own_cap);
   const int ns = min(own.n_split, (count + own.split - 1) / own.split);
-  for (int s = 0; s < ns; ++s) {
-    const size_t prow = ((size_t)lb * own.n_split + s) * a.H_q + h;
-    j.add(reinterpret_cast<const float2*>(own.ml)[prow], own.acc + prow * kD, d4);
-  }
+  const Join j = join_parts<S>(a.n_split + ns, [&](int s, const float2*& ml, const float*& acc) {
+    const bool pre = s < a.n_split;
+    const size_t prow = pre ? (part * a.n_split + s) * rows_per_tile + r % rows_per_tile
+                            : ((size_t)lb * own.n_split + (s - a.n_split)) * a.H_q + h;
+    ml = reinterpret_cast<const float2*>(pre ? a.part_ml : own.ml) + prow;
+    acc = (pre ? a.part_acc : own.acc) + prow * kD;
+  });
+  if (want >= n_out || (threadIdx.x >> 5) % S != 0) return;
   const float inv = j.inv();
   reinterpret_cast<float4*>(out + orow * kD)[d4] =
       make_float4(j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv);
@@ -534,12 +588,23 @@ struct TilePlan {
 
 constexpr int kMinSplit = 256;
 
+// Groups of 32 threads that join a row of n partial results: one per eight, whose
+// loads are a single round trip.
+template <class F>
+void with_parts(int n, F&& launch) {
+  if (n <= 8) launch(std::integral_constant<int, 1>{});
+  else if (n <= 16) launch(std::integral_constant<int, 2>{});
+  else if (n <= 32) launch(std::integral_constant<int, 4>{});
+  else launch(std::integral_constant<int, 8>{});
+}
+dim3 merge_grid(int64_t rows, int s) { return dim3((unsigned)((rows * s + 7) / 8)); }
+
 // units: (layer, sequence, KV head); rows: query rows of a unit; most: the most
 // tokens that a row tile of `rows` sees.
-TilePlan tile_plan(int64_t units, int64_t rows, int64_t most) {
+TilePlan tile_plan(int64_t units, int64_t rows, int64_t most, bool shrink) {
   TilePlan p;
   p.rows = rows > 128 ? 256 : rows > 64 ? 128 : rows > 32 ? 64 : 32;
-  while (p.rows > 64 && units * ((rows + p.rows - 1) / p.rows) < kCUs) p.rows /= 2;
+  while (shrink && p.rows > 64 && units * ((rows + p.rows - 1) / p.rows) < kCUs) p.rows /= 2;
   p.tok = p.rows == 32 ? 128 : 64;
   p.n_rt = (int)((rows + p.rows - 1) / p.rows);
   const int64_t wgs = units * p.n_rt;
@@ -579,11 +644,11 @@ TilePlan window_plan(const DenseDims& d) {
   // a row tile of r rows covers at most (r - 2) / G + 2 query tokens
   int64_t most = (int64_t)d.window + d.n_sink + (256 - 2) / d.G + 1;
   if (most > d.L_cap) most = d.L_cap;
-  return tile_plan(units, (int64_t)d.T * d.G, most);
+  return tile_plan(units, (int64_t)d.T * d.G, most, true);
 }
 
 TilePlan prefix_plan(const DenseDims& d) {
-  return tile_plan((int64_t)d.n_layers * d.H_kv, (int64_t)d.B * d.G, d.P_cap);
+  return tile_plan((int64_t)d.n_layers * d.H_kv, (int64_t)d.B * d.G, d.P_cap, false);
 }
 
 // One query token per sequence, as the attention kernels take it: k_max tokens.
@@ -632,7 +697,9 @@ hipError_t launch_window(const DenseDims& d, const uint16_t* q, const uint16_t* 
   hipError_t e = launch_tiles<true, false>(p, a, s);
   if (e != hipSuccess || p.n_split == 1) return e;
   const int64_t n_out = (int64_t)d.n_layers * d.B * d.T * d.H_q;
-  window_merge_kernel<<<dim3((unsigned)((n_out + 7) / 8)), 256, 0, s>>>(a, p.rows, n_out);
+  with_parts(p.n_split, [&](auto S) {
+    window_merge_kernel<S.value><<<merge_grid(n_out, S.value), 256, 0, s>>>(a, p.rows, n_out);
+  });
   return hipGetLastError();
 }
 
@@ -673,15 +740,19 @@ hipError_t launch_prefix_decode(const DenseDims& d, const uint16_t* q, const uin
                         w + tile_acc_bytes(units, p) + tile_ml_bytes(units, p), s);
   if (e != hipSuccess) return e;
   const int64_t n_out = (int64_t)d.n_layers * d.B * d.H_q;
-  prefix_merge_kernel<<<dim3((unsigned)((n_out + 7) / 8)), 256, 0, s>>>(a, p.rows, own, lens,
-                                                                        d.L_cap, out, lse, n_out);
+  with_parts(p.n_split + own.n_split, [&](auto S) {
+    prefix_merge_kernel<S.value><<<merge_grid(n_out, S.value), 256, 0, s>>>(
+        a, p.rows, own, lens, d.L_cap, out, lse, n_out);
+  });
   return hipGetLastError();
 }
 
 // ---- decode attention that adds up its weights ----------------------------
 namespace {
 
-constexpr int kAccumTokens = 1024;  // of a workgroup, four per thread
+// A workgroup's threads are PARTS parts of a set's heads by 256 / PARTS groups of
+// four tokens.
+constexpr int accum_tokens(int parts) { return 4 * 256 / parts; }
 
 struct AccumArgs {
   const float* logits;  // [lb][H_q][stride], log2 units
@@ -692,30 +763,48 @@ struct AccumArgs {
   int B, H_q, n_sets, L_cap, tiles;  // workgroups of a weights row
 };
 
-// weights[lb][set][t] += sum over the set's heads of 2^(logit - lse log2(e)).
+// weights[lb][set][t] += sum over the set's heads of 2^(logit - lse log2(e)), in a
+// fixed order.  A thread has four tokens of every PARTS-th head, four of them
+// requested together; the parts are added in LDS.
+template <int PARTS>
 __global__ __launch_bounds__(256) void accum_kernel(AccumArgs a) {
+  constexpr int TOK = accum_tokens(PARTS);
+  __shared__ float4 sums[PARTS][TOK / 4];
   const int tile = blockIdx.x % a.tiles, rest = blockIdx.x / a.tiles;
   const int set = rest % a.n_sets, lb = rest / a.n_sets;
   const int count = clampi(a.counts[lb % a.B], 0, a.L_cap);
-  const int t0 = tile * kAccumTokens + threadIdx.x * 4;
-  if (t0 >= count) return;
+  if (tile * TOK >= count) return;  // uniform
+  const int t4 = threadIdx.x % (TOK / 4), part = threadIdx.x / (TOK / 4);
+  const int t0 = tile * TOK + t4 * 4;
   const int heads = a.H_q / a.n_sets;
   const size_t h0 = (size_t)lb * a.H_q + (size_t)set * heads;
   float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int h = 0; h < heads; ++h) {
-    const float z = a.lse[h0 + h] * kLog2e;
-    if (z == -INFINITY) continue;  // every logit of the head is -inf: no weights
-    const float4 x = *reinterpret_cast<const float4*>(a.logits + (h0 + h) * a.stride + t0);
-    sum.x += exp2f(x.x - z);
-    sum.y += exp2f(x.y - z);
-    sum.z += exp2f(x.z - z);
-    sum.w += exp2f(x.w - z);
+  for (int h = part; h < heads && t0 < count; h += 4 * PARTS) {
+    float4 x[4];
+    float z[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const size_t r = h0 + min(h + PARTS * u, heads - 1);
+      z[u] = a.lse[r] * kLog2e;
+      x[u] = *reinterpret_cast<const float4*>(a.logits + r * a.stride + t0);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (h + PARTS * u >= heads || z[u] == -INFINITY) continue;  // all -inf: no weights
+      sum.x += exp2f(x[u].x - z[u]);
+      sum.y += exp2f(x[u].y - z[u]);
+      sum.z += exp2f(x[u].z - z[u]);
+      sum.w += exp2f(x[u].w - z[u]);
+    }
   }
-  float* w = a.weights + ((size_t)lb * a.n_sets + set) * a.L_cap + t0;
-  w[0] += sum.x;
-  if (t0 + 1 < count) w[1] += sum.y;
-  if (t0 + 2 < count) w[2] += sum.z;
-  if (t0 + 3 < count) w[3] += sum.w;
+  sums[part][t4] = sum;
+  __syncthreads();
+  float* row = a.weights + ((size_t)lb * a.n_sets + set) * a.L_cap;
+  for (int t = threadIdx.x; t < TOK && tile * TOK + t < count; t += 256) {
+    float add = 0.f;
+    for (int p = 0; p < PARTS; ++p) add += reinterpret_cast<const float*>(sums[p])[t];
+    row[tile * TOK + t] += add;
+  }
 }
 
 int64_t accum_stride(const DenseDims& d) { return ((int64_t)d.L_cap + 31) / 32 * 32; }
@@ -744,10 +833,15 @@ hipError_t launch_accum_decode(const DenseDims& d, const uint16_t* q, const uint
       launch_attn_dense(decode_dims(d, d.L_cap), m, q, k, v, counts, out, z,
                         w + accum_logit_bytes(d) + accum_lse_bytes(d), s);
   if (e != hipSuccess) return e;
-  const int tiles = (d.L_cap + kAccumTokens - 1) / kAccumTokens;
+  const int heads = d.H_q / d.n_sets;
+  const int parts = heads >= 16 ? 16 : heads >= 4 ? 4 : 1;
+  const int tiles = (d.L_cap + accum_tokens(parts) - 1) / accum_tokens(parts);
   const AccumArgs a{logits, z, counts, weights, accum_stride(d), d.B, d.H_q, d.n_sets, d.L_cap,
                     tiles};
-  accum_kernel<<<dim3((unsigned)((int64_t)tiles * d.n_sets * d.n_layers * d.B)), 256, 0, s>>>(a);
+  const dim3 grid((unsigned)((int64_t)tiles * d.n_sets * d.n_layers * d.B));
+  if (parts == 16) accum_kernel<16><<<grid, 256, 0, s>>>(a);
+  else if (parts == 4) accum_kernel<4><<<grid, 256, 0, s>>>(a);
+  else accum_kernel<1><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
