@@ -151,7 +151,8 @@ _lib = None
 _fast = None  # native marshalling (binding/fast.cpp), loaded with the library if built
 # its entry points, in the order its init() takes their addresses
 _FAST_API = ["spec_score", "spec_topk", "spec_sparse_decode_attn", "spec_step",
-             "spec_retrieval_qk", "spec_mla_sparse_decode_attn"]
+             "spec_retrieval_qk", "spec_mla_sparse_decode_attn", "spec_window_decode_attn",
+             "spec_window_attn", "spec_prefix_decode_attn", "spec_accum_decode_attn", "spec_evict"]
 
 
 def load_library(path: Optional[str] = None):
@@ -887,6 +888,12 @@ def _dense_workspace(dims: DenseDims, op: int, device, ws: Optional[torch.Tensor
     return torch.empty(max(need, 16), dtype=torch.uint8, device=device), need
 
 
+def _native(t) -> bool:
+    """Whether a call on t may take the native marshalling: a device tensor
+    proper, on the current device."""
+    return _plain(t) and t.get_device() == torch._C._cuda_getDevice()
+
+
 def _same_device(where: torch.Tensor, **tensors):
     for name, t in tensors.items():
         if t is not None and t.device != where.device:
@@ -933,6 +940,12 @@ def window_decode_attn(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, seq_le
     L_cap, H_kv, d].  Returns (out fp32 [n_layers, B, H_q, d], lse fp32
     [n_layers, B, H_q] or None); no tokens: 0 and -inf."""
     lib = load_library()
+    if out is not None and ws is not None and (lse is not None or not with_lse) and _native(q):
+        st = _fast.window_decode(q, K, V, seq_lens, window, n_sink, scale, out, lse, ws,
+                                 _raw_stream(q))
+        if st is not None:
+            _check(st, "spec_window_decode_attn")
+            return out, lse
     _dense_q(q, K, V, False)
     _i32(seq_lens, "seq_lens", K.shape[1])
     _same_device(q, K=K, V=V, seq_lens=seq_lens, out=out, lse=lse, ws=ws)
@@ -959,6 +972,12 @@ def window_attn(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, seq_lens: tor
     None); queries behind a sequence's last are left as they are (zero when the
     outputs are allocated here)."""
     lib = load_library()
+    if out is not None and ws is not None and (lse is not None or not with_lse) and _native(q):
+        st = _fast.window(q, K, V, seq_lens, q_lens, window, n_sink, scale, out, lse, ws,
+                          _raw_stream(q))
+        if st is not None:
+            _check(st, "spec_window_attn")
+            return out, lse
     _dense_q(q, K, V, True)
     B = K.shape[1]
     _i32(seq_lens, "seq_lens", B)
@@ -993,6 +1012,12 @@ def prefix_decode_attn(q: torch.Tensor, K_prefix: torch.Tensor, V_prefix: torch.
     [n_layers, B, L_cap, H_kv, d].  q [n_layers, B, H_q, d].  Returns (out fp32,
     lse fp32 or None) as window_decode_attn."""
     lib = load_library()
+    if out is not None and ws is not None and (lse is not None or not with_lse) and _native(q):
+        st = _fast.prefix_decode(q, K_prefix, V_prefix, K, V, seq_lens, prefix_len, scale, out,
+                                 lse, ws, _raw_stream(q))
+        if st is not None:
+            _check(st, "spec_prefix_decode_attn")
+            return out, lse
     _dense_q(q, K, V, False)
     n_layers, B, _, H_kv, d = K.shape
     for t, nm in ((K_prefix, "K_prefix"), (V_prefix, "V_prefix")):
@@ -1041,6 +1066,11 @@ def accum_decode_attn(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, counts:
     [n_layers, B, H_kv, L_cap]), to `weights` in place.  Returns (out, lse) as
     window_decode_attn."""
     lib = load_library()
+    if out is not None and ws is not None and (lse is not None or not with_lse) and _native(q):
+        st = _fast.accum_decode(q, K, V, counts, weights, scale, out, lse, ws, _raw_stream(q))
+        if st is not None:
+            _check(st, "spec_accum_decode_attn")
+            return out, lse
     _dense_q(q, K, V, False)
     _i32(counts, "counts", K.shape[1])
     n_sets = _sets_of_weights(weights, K)
@@ -1070,6 +1100,12 @@ def evict(K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, tokens: torch
     the rows held, the last n_recent tokens and the first n_sink stay before all
     others, then the largest weights, ties to the lower slot."""
     lib = load_library()
+    if ws is not None and _native(K):
+        st = _fast.evict(K, V, weights, tokens, counts, keep, pos, k_new, v_new, n_new, n_recent,
+                         n_sink, ws, _raw_stream(K))
+        if st is not None:
+            _check(st, "spec_evict")
+            return
     _check_cache(K, V)
     n_layers, B, L_cap, H_kv, d = K.shape
     n_sets = _sets_of_weights(weights, K)

@@ -31,6 +31,11 @@ struct Api {
   decltype(&spec_step) step;
   decltype(&spec_retrieval_qk) retrieval_qk;
   decltype(&spec_mla_sparse_decode_attn) mla;
+  decltype(&spec_window_decode_attn) window_decode;
+  decltype(&spec_window_attn) window;
+  decltype(&spec_prefix_decode_attn) prefix_decode;
+  decltype(&spec_accum_decode_attn) accum_decode;
+  decltype(&spec_evict) evict;
 };
 Api api = {};
 
@@ -429,6 +434,185 @@ PyObject* fast_mla(PyObject*, PyObject* const* args, Py_ssize_t n) {
               ptr<float>(lse), ws->data_ptr(), ws->nbytes(), stream);
 }
 
+// The caches' dimensions of a dense call.
+spec_dense_dims dense_dims(const at::Tensor& K) {
+  spec_dense_dims d = {};
+  d.n_layers = (int32_t)K.size(0);
+  d.B = (int32_t)K.size(1);
+  d.L_cap = (int32_t)K.size(2);
+  d.H_q = d.H_kv = (int32_t)K.size(3);
+  d.d = (int32_t)K.size(4);
+  d.T = 1;
+  d.n_sets = 1;
+  d.kv_stride_layer = K.stride(0);
+  d.kv_stride_b = K.stride(1);
+  return d;
+}
+
+// q [n_layers][B]([T])[H_q][d] over caches K and V; out of the same shape.
+bool dense_queries(const at::Tensor* q, const at::Tensor* K, const at::Tensor* V,
+                   const at::Tensor* out, const at::Tensor* lse, bool chunk) {
+  return caches(K, V) && is(q, at::kBFloat16, chunk ? 5 : 4) && q->is_contiguous() &&
+         q->size(0) == K->size(0) && q->size(1) == K->size(1) && q->size(-1) == K->size(4) &&
+         out->scalar_type() == (chunk ? at::kBFloat16 : at::kFloat) && out->is_contiguous() &&
+         out->sizes() == q->sizes() &&
+         (!lse || (lse->scalar_type() == at::kFloat && lse->is_contiguous() &&
+                   lse->sizes() == q->sizes().slice(0, q->dim() - 1)));
+}
+
+// window_decode(q, K, V, seq_lens, window, n_sink, scale, out, lse|None, ws, stream)
+PyObject* fast_window_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  EXPECT(n == 11);
+  TENSOR(q, 0);
+  TENSOR(K, 1);
+  TENSOR(V, 2);
+  TENSOR(lens, 3);
+  TENSOR(out, 7);
+  TENSOR_OR_NONE(lse, 8);
+  TENSOR(ws, 9);
+  bool ok;
+  void* stream = as_stream(args[10], &ok);
+  EXPECT(ok && dense_queries(q, K, V, out, lse, false));
+  spec_dense_dims d = dense_dims(*K);
+  EXPECT(as_int(args[4], &d.window) && as_int(args[5], &d.n_sink) && as_float(args[6], &d.scale));
+  EXPECT(has_shape(lens, at::kInt, {K->size(1)}) && same_device(*q, {K, V, lens, out, lse, ws}));
+  d.H_q = (int32_t)q->size(2);
+  return call(api.window_decode, &d, ptr<uint16_t>(q), ptr<uint16_t>(K), ptr<uint16_t>(V),
+              ptr<int32_t>(lens), ptr<float>(out), ptr<float>(lse), ws->data_ptr(), ws->nbytes(),
+              stream);
+}
+
+// window(q, K, V, seq_lens, q_lens|None, window, n_sink, scale, out, lse|None, ws, stream)
+PyObject* fast_window(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  EXPECT(n == 12);
+  TENSOR(q, 0);
+  TENSOR(K, 1);
+  TENSOR(V, 2);
+  TENSOR(lens, 3);
+  TENSOR_OR_NONE(q_lens, 4);
+  TENSOR(out, 8);
+  TENSOR_OR_NONE(lse, 9);
+  TENSOR(ws, 10);
+  bool ok;
+  void* stream = as_stream(args[11], &ok);
+  EXPECT(ok && dense_queries(q, K, V, out, lse, true));
+  spec_dense_dims d = dense_dims(*K);
+  EXPECT(as_int(args[5], &d.window) && as_int(args[6], &d.n_sink) && as_float(args[7], &d.scale));
+  EXPECT(has_shape(lens, at::kInt, {K->size(1)}) &&
+         (!q_lens || has_shape(q_lens, at::kInt, {K->size(1)})) &&
+         same_device(*q, {K, V, lens, q_lens, out, lse, ws}));
+  d.T = (int32_t)q->size(2);
+  d.H_q = (int32_t)q->size(3);
+  return call(api.window, &d, ptr<uint16_t>(q), ptr<uint16_t>(K), ptr<uint16_t>(V),
+              ptr<int32_t>(lens), ptr<int32_t>(q_lens), ptr<uint16_t>(out), ptr<float>(lse),
+              ws->data_ptr(), ws->nbytes(), stream);
+}
+
+// prefix_decode(q, K_prefix, V_prefix, K, V, seq_lens, prefix_len|None, scale, out, lse|None,
+//               ws, stream)
+PyObject* fast_prefix_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  EXPECT(n == 12);
+  TENSOR(q, 0);
+  TENSOR(Kp, 1);
+  TENSOR(Vp, 2);
+  TENSOR(K, 3);
+  TENSOR(V, 4);
+  TENSOR(lens, 5);
+  TENSOR_OR_NONE(plen, 6);
+  TENSOR(out, 8);
+  TENSOR_OR_NONE(lse, 9);
+  TENSOR(ws, 10);
+  bool ok;
+  void* stream = as_stream(args[11], &ok);
+  EXPECT(ok && dense_queries(q, K, V, out, lse, false));
+  EXPECT(is(Kp, at::kBFloat16, 4) && is(Vp, at::kBFloat16, 4) && Kp->sizes() == Vp->sizes() &&
+         Kp->strides() == Vp->strides() && packed(*Kp, 3) && Kp->size(0) == K->size(0) &&
+         Kp->size(2) == K->size(3) && Kp->size(3) == K->size(4));
+  spec_dense_dims d = dense_dims(*K);
+  EXPECT(as_float(args[7], &d.scale));
+  EXPECT(has_shape(lens, at::kInt, {K->size(1)}) && (!plen || has_shape(plen, at::kInt, {1})) &&
+         same_device(*q, {K, V, Kp, Vp, lens, plen, out, lse, ws}));
+  d.H_q = (int32_t)q->size(2);
+  d.P_cap = (int32_t)Kp->size(1);
+  d.prefix_stride_layer = Kp->stride(0);
+  return call(api.prefix_decode, &d, ptr<uint16_t>(q), ptr<uint16_t>(Kp), ptr<uint16_t>(Vp),
+              ptr<int32_t>(plen), ptr<uint16_t>(K), ptr<uint16_t>(V), ptr<int32_t>(lens),
+              ptr<float>(out), ptr<float>(lse), ws->data_ptr(), ws->nbytes(), stream);
+}
+
+// Weights (or tokens) [n_layers][B][1 or H_kv][L_cap] of the caches K.
+bool per_set(const at::Tensor* t, at::ScalarType type, const at::Tensor& K) {
+  return is(t, type, 4) && t->is_contiguous() && t->size(0) == K.size(0) &&
+         t->size(1) == K.size(1) && (t->size(2) == 1 || t->size(2) == K.size(3)) &&
+         t->size(3) == K.size(2);
+}
+
+// accum_decode(q, K, V, counts, weights, scale, out, lse|None, ws, stream)
+PyObject* fast_accum_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  EXPECT(n == 10);
+  TENSOR(q, 0);
+  TENSOR(K, 1);
+  TENSOR(V, 2);
+  TENSOR(counts, 3);
+  TENSOR(weights, 4);
+  TENSOR(out, 6);
+  TENSOR_OR_NONE(lse, 7);
+  TENSOR(ws, 8);
+  bool ok;
+  void* stream = as_stream(args[9], &ok);
+  EXPECT(ok && dense_queries(q, K, V, out, lse, false) && per_set(weights, at::kFloat, *K));
+  spec_dense_dims d = dense_dims(*K);
+  EXPECT(as_float(args[5], &d.scale));
+  EXPECT(has_shape(counts, at::kInt, {K->size(1)}) &&
+         same_device(*q, {K, V, counts, weights, out, lse, ws}));
+  d.H_q = (int32_t)q->size(2);
+  d.n_sets = (int32_t)weights->size(2);
+  return call(api.accum_decode, &d, ptr<uint16_t>(q), ptr<uint16_t>(K), ptr<uint16_t>(V),
+              ptr<int32_t>(counts), ptr<float>(weights), ptr<float>(out), ptr<float>(lse),
+              ws->data_ptr(), ws->nbytes(), stream);
+}
+
+// evict(K, V, weights, tokens, counts, keep, pos, k_new|None, v_new|None, n_new|None, n_recent,
+//       n_sink, ws, stream)
+PyObject* fast_evict(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  EXPECT(n == 14);
+  TENSOR(K, 0);
+  TENSOR(V, 1);
+  TENSOR(weights, 2);
+  TENSOR(tokens, 3);
+  TENSOR(counts, 4);
+  TENSOR(keep, 5);
+  TENSOR(pos, 6);
+  TENSOR_OR_NONE(k_new, 7);
+  TENSOR_OR_NONE(v_new, 8);
+  TENSOR_OR_NONE(n_new, 9);
+  TENSOR(ws, 12);
+  bool ok;
+  void* stream = as_stream(args[13], &ok);
+  EXPECT(ok && caches(K, V) && per_set(weights, at::kFloat, *K) &&
+         per_set(tokens, at::kInt, *K) && tokens->sizes() == weights->sizes());
+  spec_dense_dims d = dense_dims(*K);
+  EXPECT(as_int(args[10], &d.n_recent) && as_int(args[11], &d.n_sink));
+  const int64_t B = K->size(1);
+  EXPECT(has_shape(counts, at::kInt, {B}) && has_shape(keep, at::kInt, {B}) &&
+         has_shape(pos, at::kInt, {B}) && (!n_new || has_shape(n_new, at::kInt, {B})));
+  EXPECT(!k_new == !v_new);
+  d.T = 0;
+  if (k_new) {
+    EXPECT(is(k_new, at::kBFloat16, 5));
+    const int64_t T = k_new->size(2);
+    EXPECT(has_shape(k_new, at::kBFloat16, {K->size(0), B, T, K->size(3), K->size(4)}) &&
+           has_shape(v_new, at::kBFloat16, {K->size(0), B, T, K->size(3), K->size(4)}));
+    d.T = (int32_t)T;
+  }
+  EXPECT(same_device(*K, {V, weights, tokens, counts, keep, pos, k_new, v_new, n_new, ws}));
+  d.n_sets = (int32_t)weights->size(2);
+  const spec_bounded c = {ptr<uint16_t>(K), ptr<uint16_t>(V), ptr<float>(weights),
+                          ptr<int32_t>(tokens), ptr<int32_t>(counts)};
+  return call(api.evict, &d, &c, ptr<int32_t>(keep), ptr<int32_t>(pos), ptr<uint16_t>(k_new),
+              ptr<uint16_t>(v_new), ptr<int32_t>(n_new), ws->data_ptr(), ws->nbytes(), stream);
+}
+
 // init(addresses of the entry points, in Api's order)
 PyObject* fast_init(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != (Py_ssize_t)(sizeof(Api) / sizeof(void*))) {
@@ -472,6 +656,11 @@ PyMethodDef methods[] = {
     METHOD("step", fast_step),
     METHOD("retrieval_qk", fast_retrieval_qk),
     METHOD("mla", fast_mla),
+    METHOD("window_decode", fast_window_decode),
+    METHOD("window", fast_window),
+    METHOD("prefix_decode", fast_prefix_decode),
+    METHOD("accum_decode", fast_accum_decode),
+    METHOD("evict", fast_evict),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast", nullptr, -1, methods};

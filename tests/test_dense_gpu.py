@@ -589,3 +589,67 @@ def test_other_stream_and_two_at_once(dev):
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_native_marshalling_equals_ctypes(dev, monkeypatch):
+    """Calls that hand over every buffer, with and without the native marshalling."""
+    n, B, H_q, H_kv, cap, T, P = 2, 3, 16, 4, 200, 7, 90
+    K, V = cache(n, B, cap, H_kv, 181, dev)
+    Kp, Vp = (normal((n, P, H_kv, D), 183 + i, dev) for i in range(2))
+    q, qc = normal((n, B, H_q, D), 185, dev), normal((n, B, T, H_q, D), 186, dev)
+    kv = normal((2, n, B, 3, H_kv, D), 187, dev)
+    lens, rows, keep = i32([200, 77, 0], dev), i32([7, 3, 0], dev), i32([200, 70, 9], dev)
+
+    def all_calls():
+        w = torch.ones((n, B, H_kv, cap), device=dev)
+        o = [torch.zeros(q.shape, device=dev) for _ in range(3)]
+        z = [torch.zeros(q.shape[:-1], device=dev) for _ in range(3)]
+        oc, zc = torch.zeros_like(qc), torch.zeros(qc.shape[:-1], device=dev)
+        ws = torch.empty(1 << 24, dtype=torch.uint8, device=dev)
+        spec.window_decode_attn(q, K, V, lens, 50, n_sink=3, scale=0.1, out=o[0], lse=z[0], ws=ws)
+        spec.window_attn(qc, K, V, lens, 50, n_sink=3, q_lens=rows, scale=0.1, out=oc, lse=zc,
+                         ws=ws)
+        spec.prefix_decode_attn(q, Kp, Vp, K, V, lens, prefix_len=i32([80], dev), scale=0.1,
+                                out=o[1], lse=z[1], ws=ws)
+        spec.accum_decode_attn(q, K, V, lens, w, scale=0.1, out=o[2], lse=z[2], ws=ws)
+        Ke, Ve, t, c = K.clone(), V.clone(), w.int(), lens.clone()
+        spec.evict(Ke, Ve, w, t, c, keep, i32([300, 77, 0], dev), k_new=kv[0], v_new=kv[1],
+                   n_new=i32([3, 1, 2], dev), n_recent=5, n_sink=2, ws=ws)
+        return o + z + [oc, zc, w, Ke, Ve, t, c]
+
+    assert spec._fast is not None
+    taken = []
+    for name in ("window_decode", "window", "prefix_decode", "accum_decode", "evict"):
+        f = getattr(spec._fast, name)
+        monkeypatch.setattr(spec._fast, name,
+                            lambda *a, f=f, name=name: taken.append((name, r := f(*a))) or r)
+    native = all_calls()
+    assert taken == [(nm, 0) for nm in ("window_decode", "window", "prefix_decode", "accum_decode",
+                                        "evict")]
+    monkeypatch.setattr(spec, "_fast", None)
+    for a, b in zip(native, all_calls()):
+        assert same_bits(a, b)
+
+
+def test_refusals_name_the_argument(dev):
+    K, V = cache(1, 2, 40, 4, 191, dev)
+    q, lens = normal((1, 2, 8, D), 192, dev), i32([40, 3], dev)
+    w = torch.zeros((1, 2, 4, 40), device=dev)
+    ws = torch.empty(8, dtype=torch.uint8, device=dev)
+    for bad, call in (
+            ("q must", lambda: spec.window_decode_attn(q[:, :1], K, V, lens, 8)),
+            ("seq_lens", lambda: spec.window_decode_attn(q, K, V, lens[:1], 8)),
+            ("out", lambda: spec.window_decode_attn(q, K, V, lens, 8, out=q)),
+            ("same shape", lambda: spec.window_decode_attn(q, K, V[:, :, :30], lens, 8)),
+            ("INVALID", lambda: spec.window_decode_attn(q, K, V, lens, 0)),
+            ("UNSUPPORTED", lambda: spec.window_decode_attn(
+                q[..., :64].contiguous(), K[..., :64].contiguous(), V[..., :64].contiguous(), lens,
+                8)),
+            ("K_prefix", lambda: spec.prefix_decode_attn(q, K[0], V[0], K, V, lens)),
+            ("weights", lambda: spec.accum_decode_attn(q, K, V, lens, w[:, :, :2])),
+            ("workspace", lambda: spec.accum_decode_attn(q, K, V, lens, w, ws=ws)),
+            ("tokens", lambda: spec.evict(K, V, w, w.int()[:, :1], lens, lens, lens)),
+            ("together", lambda: spec.evict(K, V, w, w.int(), lens, lens, lens, k_new=K)),
+            ("INVALID", lambda: spec.evict(K, V, w, w.int(), lens, lens, lens, n_recent=-1))):
+        with pytest.raises((ValueError, TypeError, spec.SpecError), match=bad):
+            call()
