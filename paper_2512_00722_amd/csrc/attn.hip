@@ -99,13 +99,8 @@ enum AttnMode { kDirect = 0, kGlobalPartials = 1 };
 //  kKvElastic: the slot buffers, except the slots an elastic update has just
 //              assigned (src[b][slot] = token >= 0): those rows are read from
 //              the cache and written into their slot as they stream through
-//              (Sec. 5.4's loads fused into the attention's reads);
-//  kKvDense:   the cache, without a selection: the first n_sink tokens and the
-//              last of the sequence's, k_max in all (counts are its lengths);
-//  kKvAccum:   as kKvDense, and the logits are kept (a.logits) for the weights
-//              that are added up from them.
-enum KvMode { kKvIndexed = 0, kKvCompact = 1, kKvElastic = 2, kKvDense = 3, kKvAccum = 4 };
-constexpr bool is_dense(int kv) { return kv == kKvDense || kv == kKvAccum; }
+//              (Sec. 5.4's loads fused into the attention's reads).
+enum KvMode { kKvIndexed = 0, kKvCompact = 1, kKvElastic = 2 };
 
 struct AttnArgs {
   const uint16_t* q;      // [n_layers][B][H_q][d]
@@ -133,9 +128,6 @@ struct AttnArgs {
   float scale_log2;       // scale * log2(e)
   int team_heads;         // team kernel: column groups of a workgroup's wavefronts
   int sorted;             // pipelined launches: groups by selection size (see attn_split_kernel)
-  int n_sink;             // dense: first tokens that stay visible
-  float* logits;          // accum: [n_layers*B][H_q][logit_stride] in log2 units
-  int64_t logit_stride;   // a multiple of kChunk, so that whole chunks are stored
 };
 
 __device__ __forceinline__ void wave_sync_lds() {
@@ -228,12 +220,6 @@ template <int KV>
 __device__ __forceinline__ int elastic_row(int v, int slot, int L_cap) {
   if (KV != kKvElastic) return clampi(v, 0, L_cap - 1);
   return v >= 0 ? min(v, L_cap - 1) : -1 - slot;
-}
-// Dense modes: of a sequence of `len` tokens, visible token j is token j of the
-// sinks, or one of the last k_max - n_sink.
-__device__ __forceinline__ int dense_row(const AttnArgs& a, int j, int len) {
-  const int shift = max(min(len, a.L_cap) - a.k_max, 0);
-  return clampi(j < a.n_sink ? j : j + shift, 0, a.L_cap - 1);
 }
 // The row that padding reads (cache hits): row 0, or in elastic mode the unit's
 // first token (lane 0's staged value and slot), wherever that lies: its slot
@@ -342,16 +328,6 @@ __device__ __forceinline__ void softmax_pv(const floatx4 (&sacc)[kTiles], const 
   wave_sync_lds();  // the V tile is rewritten by the next chunk
 }
 
-// Accum mode: the logits of one chunk (its first token `tok`), 16 bytes a lane.
-__device__ __forceinline__ void store_logits(const AttnArgs& a, const floatx4 (&sacc)[kTiles],
-                                             int lb, int gv, int64_t tok, int r16, int kg) {
-  if (r16 >= a.G) return;
-  float* p = a.logits + ((int64_t)lb * a.H_q + gv * a.G + r16) * a.logit_stride + tok + 4 * kg;
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t)
-    *reinterpret_cast<floatx4*>(p + 16 * t) = sacc[t] * a.scale_log2;
-}
-
 // A wavefront's tokens of one (layer, sequence, KV head) group, whose row
 // values are staged in `rows`: n_tok tokens, and one chunk of padding after
 // the last whole or partial chunk.  Local chunk c / kChunk holds the tokens
@@ -439,7 +415,6 @@ __device__ __forceinline__ void attend(const AttnArgs& a, const int lb, const in
     if (writer) store_k_rows(rows + c, kraw, kbf + slot * rs, rs, n_tok - c, kg, r16);
     load_k(c + kChunk, kraw);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (KV == kKvAccum) store_logits(a, sacc, lb, gv, slot, r16, kg);
 
     softmax_pv(sacc, c, n_tok, a.scale_log2, V, r16, kg, m_run, l_run, acc);
   }
@@ -474,8 +449,7 @@ __device__ __forceinline__ void process_item(const AttnArgs& a, const int item, 
   const int split = rest % a.n_split;
   const int lb = rest / a.n_split;  // layer * B + b
   const int b = lb % a.B;
-  const int len = __builtin_amdgcn_readfirstlane(a.counts[b]);
-  const int count = clampi(len, 0, a.k_max);
+  const int count = __builtin_amdgcn_readfirstlane(clampi(a.counts[b], 0, a.k_max));
   const int j0 = split * a.split_tokens;
   const int r16 = lane & 15;  // head of this lane
   const int kg = lane >> 4;
@@ -514,9 +488,7 @@ __device__ __forceinline__ void process_item(const AttnArgs& a, const int item, 
     for (int m = 0; m < kColdRowLoads; ++m) {
       const int j = lane + 64 * m;
       rv[m] = KV == kKvElastic ? -1 : 0;
-      if constexpr (is_dense(KV)) rv[m] = dense_row(a, j0 + min(j, n_tok - 1), len);
-      else if (j < n_tok && (KV != kKvElastic || fz))
-        rv[m] = KV == kKvCompact ? j0 + j : idx_b[j];
+      if (j < n_tok && (KV != kKvElastic || fz)) rv[m] = KV == kKvCompact ? j0 + j : idx_b[j];
     }
     const int pad = pad_row<KV>(rv[0], j0, a.L_cap);
 #pragma unroll
@@ -536,7 +508,7 @@ __device__ __forceinline__ void process_item(const AttnArgs& a, const int item, 
   if (r16 < G) {
     if (a.mode == kDirect) {  // the whole selection: normalise and write the output
       const size_t orow = (size_t)lb * a.H_q + (size_t)gv * G + r16;
-      const float inv = is_dense(KV) && l_run == 0.f ? 0.f : 1.f / l_run;
+      const float inv = 1.f / l_run;
       float* dst = a.out + orow * kD + 4 * kg;
 #pragma unroll
       for (int db = 0; db < 8; ++db)
@@ -619,10 +591,8 @@ void attn_team_kernel(AttnArgs a) {
     // rows past the index row re-read its last entry (one cache line)
     const int t = token(lane + 64 * m);
     rv[m] = 0;
-    if constexpr (is_dense(KV)) continue;  // rows follow from the length alone
     if (64 * m < most) rv[m] = KV == kKvCompact ? t : idx_b[min(t, a.k_max - 1)];
   }
-  const int len = __builtin_amdgcn_readfirstlane(cnt_raw);
   const int count = __builtin_amdgcn_readfirstlane(clampi(cnt_raw, 0, a.k_max));
   const bool fz = __builtin_amdgcn_readfirstlane(fz_raw) != 0;
   // this wavefront's tokens: whole chunks, the selection's last one perhaps partial
@@ -630,13 +600,10 @@ void attn_team_kernel(AttnArgs a) {
   const int mine = n_chunks > gw ? (n_chunks - gw + NW - 1) / NW : 0;
   const int n_tok = mine == 0 ? 0
                     : kChunk * mine - ((n_chunks - 1) % NW == gw ? kChunk * n_chunks - count : 0);
-  // dense: the first token, as token 0 may be one that is not visible
-  const int pad = is_dense(KV) ? dense_row(a, kChunk * gw, len)
-                               : pad_row<KV>(fz ? rv[0] : -1, kChunk * gw, a.L_cap);
+  const int pad = pad_row<KV>(fz ? rv[0] : -1, kChunk * gw, a.L_cap);
 #pragma unroll
   for (int m = 0; m < kLoads; ++m) {
     const int j = lane + 64 * m;
-    if (is_dense(KV)) rv[m] = dense_row(a, token(j), len);
     if (64 * m < most + kChunk)
       rows[j] = j < n_tok ? elastic_row<KV>(fz ? rv[m] : -1, token(j), a.L_cap) : pad;
   }
@@ -684,7 +651,7 @@ void attn_team_kernel(AttnArgs a) {
     }
     if (a.mode == kDirect) {
       const size_t orow = (size_t)lb * a.H_q + (size_t)gv0 * G + hh;
-      const float inv = count > 0 && !(is_dense(KV) && L == 0.f) ? 1.f / L : 0.f;
+      const float inv = count > 0 ? 1.f / L : 0.f;
       reinterpret_cast<float4*>(a.out + orow * kD)[d4] =
           make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
       if (a.lse && d4 == 0) a.lse[orow] = count > 0 ? (M + log2f(L)) * kLn2 : -INFINITY;
@@ -821,7 +788,7 @@ void attn_split_kernel(AttnArgs a) {
 #pragma unroll
     for (int m = 0; m < kRowLoads; ++m) {
       const int j = u.j0 + lane + 64 * m;
-      rv[m] = KV == kKvCompact || is_dense(KV) ? j : idx_b[min(j, jmax)];
+      rv[m] = KV == kKvCompact ? j : idx_b[min(j, jmax)];
     }
     const uint16_t* qp =
         a.q + ((size_t)u.lb * a.H_q + u.gv * a.G + (r16 < a.G ? r16 : 0)) * kD + 8 * kg;
@@ -834,13 +801,10 @@ void attn_split_kernel(AttnArgs a) {
     const int count = __builtin_amdgcn_readfirstlane(clampi(cnt_raw, 0, a.k_max));
     u.n_tok = min(a.split_tokens, count - u.j0);
     const bool fz = __builtin_amdgcn_readfirstlane(fz_raw) != 0;  // elastic: rows may come from the caches
-    const int len = __builtin_amdgcn_readfirstlane(cnt_raw);
-    const int pad = is_dense(KV) ? dense_row(a, u.j0, len)
-                                 : pad_row<KV>(fz ? rv[0] : -1, u.j0, a.L_cap);
+    const int pad = pad_row<KV>(fz ? rv[0] : -1, u.j0, a.L_cap);
 #pragma unroll
     for (int m = 0; m < kRowLoads; ++m) {
       const int j = lane + 64 * m;
-      if (is_dense(KV)) rv[m] = dense_row(a, rv[m], len);
       rows[j] = j < u.n_tok ? elastic_row<KV>(fz ? rv[m] : -1, u.j0 + j, a.L_cap) : pad;
     }
     if (lane < kChunk) rows[kMaxSplit + lane] = pad;
@@ -955,7 +919,6 @@ void attn_split_kernel(AttnArgs a) {
         store_k_rows(rows + c, kraw, kbf + (int64_t)(cur.j0 + c) * rs, rs, n_tok - c, kg, r16);
       load_k(rsrc, ksrc, kfsrc, kraw);
       __builtin_amdgcn_sched_barrier(0);
-      if constexpr (KV == kKvAccum) store_logits(a, sacc, cur.lb, cur.gv, cur.j0 + c, r16, kg);
 
       softmax_pv(sacc, c, n_tok, a.scale_log2, V, r16, kg, m_run, l_run, acc);
     }
@@ -969,7 +932,7 @@ void attn_split_kernel(AttnArgs a) {
       if (a.mode == kDirect) {
         const size_t orow = (size_t)cur.lb * a.H_q + (size_t)cur.gv * G + r16;
         const bool any = n_tok > 0;
-        const float inv = any && !(is_dense(KV) && l_run == 0.f) ? 1.f / l_run : 0.f;
+        const float inv = any ? 1.f / l_run : 0.f;
         float* dst = a.out + orow * kD + 4 * kg;
 #pragma unroll
         for (int db = 0; db < 8; ++db)
@@ -1016,7 +979,6 @@ struct CombineArgs {
   float* out;  // [n_layers*B][H_q][d]
   float* lse;  // [n_layers*B][H_q] or null
   int B, H_q, k_max, n_split, split_tokens;
-  bool dense;  // a sum of 0 (every visible logit is -inf) gives an output of 0
 };
 
 // One workgroup per (layer*B + b, 8 / S heads); thread = (head, part, 4 dims).
@@ -1105,7 +1067,7 @@ __global__ __launch_bounds__(256) void attn_combine_kernel(CombineArgs a) {
       acc.w += x.w * w;
     }
   }
-  const float inv = a.dense && L == 0.f ? 0.f : 1.f / L;
+  const float inv = 1.f / L;
   *o = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
   if (a.lse && d4 == 0) a.lse[(size_t)lb * a.H_q + h] = (M + log2f(L)) * kLn2;
 }
@@ -1129,13 +1091,7 @@ struct AttnPlan {
 // read the same selected tokens' rows for neighbouring heads at the same time:
 // those pieces share DRAM pages.  A split is a whole number of chunks.
 // Column groups of at most 16 query heads per KV head.
-// At most 16 of them, all of one size: for powers of two 16, for others the
-// largest divisor (the dense entry points take any number of query heads).
-int attn_col_groups(const Dims& d) {
-  int c = d.G < 16 ? d.G : 16;
-  while (d.G % c) --c;
-  return d.G / c;
-}
+int attn_col_groups(const Dims& d) { return d.G > 16 ? d.G / 16 : 1; }
 
 // Launches of at most 512 groups, which leave the chip short of units: a
 // workgroup of several wavefronts per unit (attn_team_kernel).  Either a group
@@ -1259,23 +1215,6 @@ int device_cu_count() {
   return n;
 }
 
-namespace {
-
-// The partial results of a launch: `rows` accumulators, then their (max, sum) pairs.
-size_t part_bytes(const Dims& d, const AttnPlan& p) {
-  const size_t rows = (size_t)d.n_layers * d.B * p.n_split * d.H_q;
-  return align_up(sizeof(float) * rows * d.d) + align_up(sizeof(float) * rows * 2);
-}
-
-}  // namespace
-
-// Dense launches that another kernel finishes leave their results as partials
-// even where a selection is not split.
-size_t attn_dense_ws_bytes(const Dims& d, bool partials) {
-  const AttnPlan p = attn_plan(d);
-  return partials || p.mode == kGlobalPartials ? part_bytes(d, p) : 0;
-}
-
 // The larger of what the plan and the plain one (one wavefront per unit) take.
 size_t attn_ws_bytes(const Dims& d) {
   Dims plain = d;
@@ -1283,7 +1222,10 @@ size_t attn_ws_bytes(const Dims& d) {
   size_t most = 0;
   for (const Dims* e : {&d, (const Dims*)&plain}) {
     const AttnPlan p = attn_plan(*e);
-    const size_t n = p.mode == kGlobalPartials ? part_bytes(d, p) : 0;
+    const size_t rows = (size_t)d.n_layers * d.B * p.n_split * d.H_q;
+    const size_t n = p.mode == kGlobalPartials ? align_up(sizeof(float) * rows * d.d) +
+                                                     align_up(sizeof(float) * rows * 2)
+                                               : 0;
     if (n > most) most = n;
   }
   return most;
@@ -1303,8 +1245,6 @@ template <int W>
 void launch_team_w(int kv, dim3 grid, const AttnArgs& a, hipStream_t s) {
   if (kv == kKvIndexed) attn_team_kernel<kKvIndexed, W><<<grid, W * 64, 0, s>>>(a);
   else if (kv == kKvCompact) attn_team_kernel<kKvCompact, W><<<grid, W * 64, 0, s>>>(a);
-  else if (kv == kKvDense) attn_team_kernel<kKvDense, W><<<grid, W * 64, 0, s>>>(a);
-  else if (kv == kKvAccum) attn_team_kernel<kKvAccum, W><<<grid, W * 64, 0, s>>>(a);
   else attn_team_kernel<kKvElastic, W><<<grid, W * 64, 0, s>>>(a);
 }
 void launch_team(int kv, int W, dim3 grid, const AttnArgs& a, hipStream_t s) {
@@ -1315,10 +1255,9 @@ void launch_team(int kv, int W, dim3 grid, const AttnArgs& a, hipStream_t s) {
 // Merges the partial results of split selections (a direct launch has none).
 hipError_t launch_combine(const Dims& d, const AttnPlan& pl, const float* part_acc,
                           const float* part_ml, const int32_t* counts, float* out, float* lse,
-                          bool dense, hipStream_t s) {
+                          hipStream_t s) {
   if (pl.mode != kGlobalPartials) return hipGetLastError();
-  CombineArgs c{part_acc, part_ml, counts,     out,      lse, d.B,
-                d.H_q,    d.k_max, pl.n_split, pl.split, dense};
+  CombineArgs c{part_acc, part_ml, counts, out, lse, d.B, d.H_q, d.k_max, pl.n_split, pl.split};
   const unsigned lb = (unsigned)(d.n_layers * d.B);
   auto heads = [&](int per) { return dim3(lb, (unsigned)((d.H_q + per - 1) / per)); };
   if (pl.n_split <= 8) attn_combine_kernel<1><<<heads(8), 256, 0, s>>>(c);
@@ -1332,13 +1271,8 @@ hipError_t launch_attn_mode(const Dims& d, int kv, const uint16_t* q, const uint
                             const uint16_t* v, const int32_t* idx, uint16_t* kbuf,
                             uint16_t* vbuf, const int32_t* src, const int32_t* fused,
                             const int32_t* counts, float* out, float* lse, void* ws,
-                            hipStream_t s, const DenseAttn* dense = nullptr) {
-  AttnPlan pl = attn_plan(d);
-  const bool combine = !dense || !dense->partials;
-  if (!combine && pl.mode == kDirect) {
-    pl.mode = kGlobalPartials;
-    if (pl.team) pl.split = kChunk;  // only ever compared with a count: some tokens or none
-  }
+                            hipStream_t s) {
+  const AttnPlan pl = attn_plan(d);
   // the row staging area holds one split plus a chunk of padding
   if (pl.split > kMaxSplit || pl.split % kChunk != 0) return hipErrorInvalidValue;
   const size_t rows = (size_t)d.n_layers * d.B * pl.n_split * d.H_q;
@@ -1364,16 +1298,13 @@ hipError_t launch_attn_mode(const Dims& d, int kv, const uint16_t* q, const uint
   AttnArgs a{q, k, v, idx, kbuf, vbuf, src, fused, counts, part_acc, part_ml, out, lse,
              d.kv_stride_layer, d.kv_stride_b, d.B, d.H_q, d.H_kv, d.G / R, d.k_max, d.L_cap,
              pl.n_split, pl.split, (int)n_items, R, pl.mode, n_order, perm, d.n_sets,
-             d.scale * kLog2e, pl.team_heads, 0, dense ? dense->n_sink : 0,
-             dense ? dense->logits : nullptr, dense ? dense->logit_stride : 0};
-  if (dense && dense->parts) *dense->parts = {part_acc, part_ml, pl.n_split, pl.split};
+             d.scale * kLog2e, pl.team_heads, 0};
   // One workgroup per CU, fewer only when there are fewer units than CUs:
   // with few units they are spread over all CUs (each CU's share of the
   // bandwidth is limited) rather than packed four to a CU.
   if (pl.team) {
     launch_team(kv, pl.team, dim3((unsigned)(n_items / pl.team_heads)), a, s);
-    if (!combine) return hipGetLastError();
-    return launch_combine(d, pl, part_acc, part_ml, counts, out, lse, dense != nullptr, s);
+    return launch_combine(d, pl, part_acc, part_ml, counts, out, lse, s);
   }
   const int n_cu = device_cu_count();
   const dim3 grid((unsigned)(n_items < n_cu ? n_items : n_cu));
@@ -1393,14 +1324,9 @@ hipError_t launch_attn_mode(const Dims& d, int kv, const uint16_t* q, const uint
     launch_split<kKvIndexed>(grid, pipe, a, s);
   else if (kv == kKvCompact)
     launch_split<kKvCompact>(grid, pipe, a, s);
-  else if (kv == kKvDense)
-    launch_split<kKvDense>(grid, pipe, a, s);
-  else if (kv == kKvAccum)
-    launch_split<kKvAccum>(grid, pipe, a, s);
   else
     launch_split<kKvElastic>(grid, pipe, a, s);
-  if (!combine) return hipGetLastError();
-  return launch_combine(d, pl, part_acc, part_ml, counts, out, lse, dense != nullptr, s);
+  return launch_combine(d, pl, part_acc, part_ml, counts, out, lse, s);
 }
 
 }  // namespace
@@ -1410,13 +1336,6 @@ hipError_t launch_attn(const Dims& d, const uint16_t* q, const uint16_t* k,
                        float* out, float* lse, void* ws, hipStream_t s) {
   return launch_attn_mode(d, idx ? kKvIndexed : kKvCompact, q, k, v, idx, nullptr, nullptr,
                           nullptr, nullptr, counts, out, lse, ws, s);
-}
-
-hipError_t launch_attn_dense(const Dims& d, const DenseAttn& m, const uint16_t* q,
-                             const uint16_t* k, const uint16_t* v, const int32_t* lens,
-                             float* out, float* lse, void* ws, hipStream_t s) {
-  return launch_attn_mode(d, m.logits ? kKvAccum : kKvDense, q, k, v, nullptr, nullptr, nullptr,
-                          nullptr, nullptr, lens, out, lse, ws, s, &m);
 }
 
 hipError_t launch_attn_elastic(const Dims& d, const uint16_t* q, const uint16_t* k_cache,

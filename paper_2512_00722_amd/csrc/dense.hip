@@ -1,0 +1,247 @@
+// Decode attention over caches that are read in full: a sliding window with sinks,
+// and with the weights added up per token.
+//
+// One workgroup of four wavefronts takes a (layer, sequence, KV head, column group of
+// at most 16 query heads), or one of n_split parts of it (dense_core.h).  The
+// kernel is bound by memory: two workgroups per CU keep 128 KB in flight each.
+#include <stdlib.h>
+#include "dense_core.h"
+
+namespace spec {
+namespace {
+
+constexpr int kW = 4;
+
+template <int HB, int KEEP>
+__global__ __launch_bounds__(kW * 64) __attribute__((amdgpu_waves_per_eu(2)))
+void decode_kernel(DecodeArgs a) {
+  extern __shared__ __align__(16) float lds_logits[];
+  __shared__ __align__(16) uint16_t tiles[kW][kTileElems];
+  __shared__ float2 ml[kW][16];
+  decode_block<kW, HB, KEEP>(a, blockIdx.x, tiles, ml, lds_logits);
+}
+
+// 8 / S output rows per workgroup, 32 threads (4 dimensions each) and S of them.
+template <int S>
+__global__ __launch_bounds__(256) void decode_merge_kernel(DecodeArgs a, float* out, float* lse,
+                                                           int64_t n_out) {
+  const int64_t want = (int64_t)blockIdx.x * (8 / S) + (threadIdx.x >> 5) / S;
+  const int64_t orow = want < n_out ? want : n_out - 1;
+  const int d4 = threadIdx.x & 31;
+  const int h = (int)(orow % a.H_q);
+  const int64_t lb = orow / a.H_q;
+  const Join j = join_parts<S>(a.n_split, [&](int s, const float2*& ml, const float*& acc) {
+    const size_t prow = ((size_t)lb * a.n_split + s) * a.H_q + h;
+    ml = reinterpret_cast<const float2*>(a.part_ml) + prow;
+    acc = a.part_acc + prow * kHeadDim;
+  });
+  if (want >= n_out || (threadIdx.x >> 5) % S != 0) return;
+  const float inv = j.inv();
+  reinterpret_cast<float4*>(out + orow * kHeadDim)[d4] =
+      make_float4(j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv);
+  if (lse && d4 == 0) lse[orow] = j.lse();
+}
+
+// A workgroup's threads are PARTS parts of a set's rows by 256 / PARTS groups of
+// four tokens.
+constexpr int accum_tokens(int parts) { return 4 * 256 / parts; }
+
+struct AccumArgs {
+  const float* rows;    // [lb][n_rows][stride]: logits (log2 units), or weights (lse null)
+  const float* lse;     // [lb][n_rows]
+  const int32_t* counts;
+  float* weights;       // [lb][n_sets][L_cap]
+  int64_t stride;
+  int B, n_rows, n_sets, L_cap, tiles;  // tiles: workgroups of a weights row
+};
+
+// weights[lb][set][t] += sum over the set's rows of the weight, 2^(logit - lse log2(e)),
+// in a fixed order.  A thread has four tokens of every PARTS-th row, four of them
+// requested together; the parts are added in LDS.
+template <int PARTS>
+__global__ __launch_bounds__(256) void accum_kernel(AccumArgs a) {
+  constexpr int TOK = accum_tokens(PARTS);
+  __shared__ float4 sums[PARTS][TOK / 4];
+  const int tile = blockIdx.x % a.tiles, rest = blockIdx.x / a.tiles;
+  const int set = rest % a.n_sets, lb = rest / a.n_sets;
+  const int count = clampi(a.counts[lb % a.B], 0, a.L_cap);
+  if (tile * TOK >= count) return;  // uniform
+  const int t4 = threadIdx.x % (TOK / 4), part = threadIdx.x / (TOK / 4);
+  const int t0 = tile * TOK + t4 * 4;
+  const int rows = a.n_rows / a.n_sets;
+  const size_t r0 = (size_t)lb * a.n_rows + (size_t)set * rows;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int h = part; h < rows && t0 < count; h += 4 * PARTS) {
+    float4 x[4];
+    float z[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const size_t r = r0 + min(h + PARTS * u, rows - 1);
+      z[u] = a.lse ? a.lse[r] * kLog2e : 0.f;
+      x[u] = *reinterpret_cast<const float4*>(a.rows + r * a.stride + t0);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (h + PARTS * u >= rows || z[u] == -INFINITY) continue;  // all -inf: no weights
+      sum.x += a.lse ? exp2f(x[u].x - z[u]) : x[u].x;
+      sum.y += a.lse ? exp2f(x[u].y - z[u]) : x[u].y;
+      sum.z += a.lse ? exp2f(x[u].z - z[u]) : x[u].z;
+      sum.w += a.lse ? exp2f(x[u].w - z[u]) : x[u].w;
+    }
+  }
+  sums[part][t4] = sum;
+  __syncthreads();
+  float* row = a.weights + ((size_t)lb * a.n_sets + set) * a.L_cap;
+  for (int t = threadIdx.x; t < TOK && tile * TOK + t < count; t += 256) {
+    float add = 0.f;
+    for (int p = 0; p < PARTS; ++p) add += reinterpret_cast<const float*>(sums[p])[t];
+    row[tile * TOK + t] += add;
+  }
+}
+
+void launch_accum(AccumArgs a, int64_t lb, hipStream_t s) {
+  const int rows = a.n_rows / a.n_sets;
+  const int parts = rows >= 16 ? 16 : rows >= 4 ? 4 : 1;
+  a.tiles = (a.L_cap + accum_tokens(parts) - 1) / accum_tokens(parts);
+  const dim3 grid((unsigned)(a.tiles * a.n_sets * lb));
+  if (parts == 16) accum_kernel<16><<<grid, 256, 0, s>>>(a);
+  else if (parts == 4) accum_kernel<4><<<grid, 256, 0, s>>>(a);
+  else accum_kernel<1><<<grid, 256, 0, s>>>(a);
+}
+
+// Workgroups per unit: enough to give every CU two, of at least one chunk per
+// wavefront.
+int decode_split(const DenseDims& d, int k_max) {
+  const int64_t units = (int64_t)d.n_layers * d.B * d.H_kv * (d.G / group_heads(d.G));
+  const int64_t most = (k_max + kDecodeChunk * kW - 1) / (kDecodeChunk * kW);
+  int64_t n = units >= kCUs ? 1 : 2 * kCUs / units;
+  if (n > most) n = most;
+  return n < 1 ? 1 : (int)n;
+}
+size_t part_acc_bytes(const DenseDims& d, int n_split) {
+  return n_split > 1 ? align_up(sizeof(float) * kHeadDim * (size_t)d.n_layers * d.B * n_split *
+                                d.H_q)
+                     : 0;
+}
+size_t part_ml_bytes(const DenseDims& d, int n_split) {
+  return n_split > 1 ? align_up(sizeof(float) * 2 * (size_t)d.n_layers * d.B * n_split * d.H_q)
+                     : 0;
+}
+
+DecodeArgs decode_args(const DenseDims& d, int k_max, int n_sink, int n_split, const uint16_t* q,
+                       const uint16_t* k, const uint16_t* v, const int32_t* lens, float* out,
+                       float* lse, char* ws) {
+  const int heads = group_heads(d.G);
+  DecodeArgs a{q, k, v, lens, out, lse, nullptr, nullptr, nullptr, nullptr, d.kv_stride_layer,
+               d.kv_stride_b, 0, d.B, d.H_q, d.H_kv, heads, d.G / heads, d.L_cap, k_max, n_sink,
+               n_split, 0, d.scale * kLog2e};
+  if (n_split > 1) {
+    a.out = nullptr;
+    a.part_acc = reinterpret_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float*>(ws + part_acc_bytes(d, n_split));
+  }
+  return a;
+}
+
+template <int KEEP>
+hipError_t launch_decode(const DenseDims& d, const DecodeArgs& a, float* out, float* lse,
+                         size_t lds, hipStream_t s) {
+  const int64_t blocks = (int64_t)d.n_layers * d.B * d.H_kv * a.R * a.n_split;
+  if (blocks > INT32_MAX / (kW * 64)) return hipErrorInvalidValue;
+  static const int hb = getenv("HB") ? atoi(getenv("HB")) : 1;
+  if (hb == 1 || a.n_split > 1) decode_kernel<1, KEEP><<<dim3((unsigned)blocks), kW * 64, lds, s>>>(a);
+  else if (hb == 2) decode_kernel<2, KEEP><<<dim3((unsigned)blocks / 2), kW * 64, 2*lds, s>>>(a);
+  else decode_kernel<4, KEEP><<<dim3((unsigned)blocks / 4), kW * 64, 4*lds, s>>>(a);
+  if (a.n_split > 1) {
+    const int64_t n_out = (int64_t)d.n_layers * d.B * d.H_q;
+    with_parts(a.n_split, [&](auto S) {
+      decode_merge_kernel<S.value><<<merge_grid(n_out, S.value), 256, 0, s>>>(a, out, lse, n_out);
+    });
+  }
+  return hipGetLastError();
+}
+
+int window_tokens(const DenseDims& d) {
+  const int64_t n = (int64_t)d.window + d.n_sink;
+  return (int)(n < d.L_cap ? n : d.L_cap);
+}
+
+// Weights in LDS (kKeepWeights): where a unit is one workgroup's and its logits
+// leave room for a second workgroup on the CU.
+constexpr size_t kLogitLds = 44 * 1024;
+struct AccumPlan {
+  int n_split;
+  bool in_lds;     // else the logits go through memory
+  bool in_place;   // in_lds: a set is one unit, which adds to the weights itself
+};
+AccumPlan accum_plan(const DenseDims& d) {
+  AccumPlan p;
+  const int heads = group_heads(d.G), R = d.G / heads;
+  p.n_split = decode_split(d, d.L_cap);
+  p.in_lds = p.n_split == 1 && sizeof(float) * heads * logit_pitch(d.L_cap) <= kLogitLds;
+  p.in_place = p.in_lds && d.n_sets == d.H_kv && R == 1;
+  return p;
+}
+int64_t accum_stride(const DenseDims& d) { return ((int64_t)d.L_cap + 31) / 32 * 32; }
+// Logits [lb][H_q], or the units' weights [lb][H_kv R].
+size_t accum_row_bytes(const DenseDims& d, const AccumPlan& p) {
+  if (p.in_place) return 0;
+  const int64_t rows = p.in_lds ? d.H_kv * (d.G / group_heads(d.G)) : d.H_q;
+  return align_up(sizeof(float) * (size_t)d.n_layers * d.B * rows * accum_stride(d));
+}
+size_t accum_lse_bytes(const DenseDims& d) {
+  return align_up(sizeof(float) * (size_t)d.n_layers * d.B * d.H_q);
+}
+
+}  // namespace
+
+size_t window_decode_ws_bytes(const DenseDims& d) {
+  const int n = decode_split(d, window_tokens(d));
+  return part_acc_bytes(d, n) + part_ml_bytes(d, n);
+}
+
+hipError_t launch_window_decode(const DenseDims& d, const uint16_t* q, const uint16_t* k,
+                                const uint16_t* v, const int32_t* lens, float* out, float* lse,
+                                void* ws, hipStream_t s) {
+  const int k_max = window_tokens(d);
+  const DecodeArgs a = decode_args(d, k_max, d.n_sink, decode_split(d, k_max), q, k, v, lens, out,
+                                   lse, static_cast<char*>(ws));
+  return launch_decode<kKeepNone>(d, a, out, lse, 0, s);
+}
+
+size_t accum_decode_ws_bytes(const DenseDims& d) {
+  const AccumPlan p = accum_plan(d);
+  return accum_row_bytes(d, p) + accum_lse_bytes(d) + part_acc_bytes(d, p.n_split) +
+         part_ml_bytes(d, p.n_split);
+}
+
+hipError_t launch_accum_decode(const DenseDims& d, const uint16_t* q, const uint16_t* k,
+                               const uint16_t* v, const int32_t* counts, float* weights,
+                               float* out, float* lse, void* ws, hipStream_t s) {
+  const AccumPlan p = accum_plan(d);
+  char* w = static_cast<char*>(ws);
+  float* rows = reinterpret_cast<float*>(w);
+  w += accum_row_bytes(d, p);
+  float* z = lse ? lse : reinterpret_cast<float*>(w);
+  w += accum_lse_bytes(d);
+  DecodeArgs a = decode_args(d, d.L_cap, d.L_cap, p.n_split, q, k, v, counts, out, z, w);
+  a.logit_stride = accum_stride(d);
+  const int64_t lb = (int64_t)d.n_layers * d.B;
+  if (p.in_lds) {
+    a.add_weights = p.in_place;
+    a.weights = p.in_place ? weights : rows;
+    const size_t lds = sizeof(float) * a.heads * logit_pitch(d.L_cap);
+    const hipError_t e = launch_decode<kKeepWeights>(d, a, out, z, lds, s);
+    if (e != hipSuccess || p.in_place) return e;
+    launch_accum({rows, nullptr, counts, weights, a.logit_stride, d.B, d.H_kv * a.R, d.n_sets,
+                  d.L_cap, 0}, lb, s);
+    return hipGetLastError();
+  }
+  a.logits = rows;
+  const hipError_t e = launch_decode<kKeepLogits>(d, a, out, z, 0, s);
+  if (e != hipSuccess) return e;
+  launch_accum({rows, z, counts, weights, a.logit_stride, d.B, d.H_q, d.n_sets, d.L_cap, 0}, lb, s);
+  return hipGetLastError();
+}
+
+}  // namespace spec

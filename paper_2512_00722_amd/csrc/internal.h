@@ -245,28 +245,6 @@ struct DenseDims {
 };
 constexpr int kHeadDim = 128;
 
-// Where a launch whose results another kernel finishes left them:
-// acc [n_layers*B][n_split][H_q][d], (max, sum) [n_layers*B][n_split][H_q].  A
-// sequence of c tokens has min(n_split, ceil(c / split)) of them.
-struct AttnParts {
-  const float* acc;
-  const float* ml;
-  int n_split, split;
-};
-// One query token per sequence over its cache: d.k_max tokens at most are
-// visible, the first n_sink and the last of the rest.
-struct DenseAttn {
-  int n_sink;
-  float* logits;         // nullable: keep the logits, [n_layers*B][H_q][logit_stride], log2 units
-  int64_t logit_stride;  // of d.k_max rounded up to whole chunks of 32
-  bool partials;         // leave partial results, described in *parts
-  AttnParts* parts;
-};
-size_t attn_dense_ws_bytes(const Dims& d, bool partials);
-hipError_t launch_attn_dense(const Dims& d, const DenseAttn& m, const uint16_t* q,
-                             const uint16_t* k, const uint16_t* v, const int32_t* lens,
-                             float* out, float* lse, void* ws, hipStream_t s);
-
 size_t window_ws_bytes(const DenseDims& d);
 hipError_t launch_window(const DenseDims& d, const uint16_t* q, const uint16_t* k,
                          const uint16_t* v, const int32_t* lens, const int32_t* q_lens,

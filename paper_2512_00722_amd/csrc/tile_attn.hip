@@ -13,25 +13,13 @@
 //  * O^T += V^T P^T takes P from those registers as they are: the token order
 //    inside a multiplication is free, and V is read transposed from LDS
 //    (ds_read_b64_tr_b16) in the same order.
-#include <float.h>
-
-#include <type_traits>
-
-#include "device_common.h"
-#include "internal.h"
+#include "dense_core.h"
 
 namespace spec {
 namespace {
 
 constexpr int kD = kHeadDim;
 typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef float floatx2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-// The running maximum before the first logit: finite, so that logits of -inf
-// weigh nothing from the first tile on.
-constexpr float kNoMax = -FLT_MAX;
 // The maximum is moved, and what has been added up rescaled, only once a logit
 // is 2^8 above it: until then weights are up to 2^8, which neither the fp32 sums
 // nor the bf16 weights (whose precision is relative) notice.
@@ -51,9 +39,9 @@ struct TileArgs {
   int B, T, H_q, H_kv, G, L_cap, window, n_sink;
   int n_units, n_rt, n_split, split_tok;
   float scale_log2;
+  DecodeArgs own;         // prefix: the sequences' own tokens, by
+  int own_blocks;         // the first workgroups of the launch
 };
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // The value of the lane 32 on (each row lives in two lanes).
 __device__ __forceinline__ float pair_max(float v) {
@@ -63,29 +51,6 @@ __device__ __forceinline__ float pair_max(float v) {
 __device__ __forceinline__ float pair_sum(float v) {
   auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(a[0]) + __uint_as_float(a[1]);
-}
-
-__device__ __forceinline__ bf16x4 lds_read_tr(const uint16_t* p) {
-  return __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-      (__attribute__((address_space(3))) bf16x4*)(p));
-}
-
-__device__ __forceinline__ bf16x8 to_bf16x8(const float* p) {  // round to nearest even
-  bf16x8 r;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const bf16x2 h = __builtin_convertvector(floatx2{p[2 * j], p[2 * j + 1]}, bf16x2);
-    r[2 * j] = h[0];
-    r[2 * j + 1] = h[1];
-  }
-  return r;
-}
-
-// The 16-byte pieces of a 256-byte row stand at piece ^ swizzle(token): the 16
-// rows that a quarter of a K read touches then lie in different banks, and so do
-// the four rows of a transposing V read.
-__device__ __forceinline__ int swizzle(int token) {
-  return ((token & 3) << 2) | ((token >> 2) & 3);
 }
 
 // Visible tokens of the query items i0..i1 of one sequence (len cached tokens, n
@@ -173,12 +138,25 @@ void tile_attn_kernel(TileArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int rw = wave % RW, tw = wave / RW;
   const int c32 = lane & 31, kg = lane >> 5;
+  int block = blockIdx.x;
+  if (!WINDOW) {  // own tokens: memory-bound work beside that of the matrix cores
+    if (block < a.own_blocks) {
+      constexpr int W = RW * TW;
+      static_assert(W * kTileElems <= 4 * TOK * kD, "the tiles' LDS holds the wavefronts' V tiles");
+      __shared__ float2 ml[W][16];
+      decode_block<W, 1, kKeepNone>(a.own, block,
+                                 reinterpret_cast<uint16_t(*)[kTileElems]>(&lds[0][0][0]), ml,
+                                 nullptr);
+      return;
+    }
+    block -= a.own_blocks;
+  }
 
   // Units run fastest over the workgroups: those of one KV head keep to one XCD
   // where the units are a multiple of 8, and share its L2.  The last rows, which
   // see the most tokens, go first.
-  const int u = blockIdx.x % a.n_units;
-  const int rest = blockIdx.x / a.n_units;
+  const int u = block % a.n_units;
+  const int rest = block / a.n_units;
   const int split = rest % a.n_split;
   const int rt = a.n_rt - 1 - rest / a.n_split;
   const int lb = u / a.H_kv, g = u % a.H_kv;
@@ -345,12 +323,7 @@ void tile_attn_kernel(TileArgs a) {
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         ph[2 * blk + m] = to_bf16x8(p + 8 * m);
-        if constexpr (SPLITP) {
-          float lo[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) lo[e] = p[8 * m + e] - (float)ph[2 * blk + m][e];
-          pl[2 * blk + m] = to_bf16x8(lo);
-        }
+        if constexpr (SPLITP) pl[2 * blk + m] = rest_bf16x8(p + 8 * m, ph[2 * blk + m]);
       }
     }
 
@@ -450,78 +423,6 @@ void tile_attn_kernel(TileArgs a) {
           acc[db][4 * e], acc[db][4 * e + 1], acc[db][4 * e + 2], acc[db][4 * e + 3]);
 }
 
-// The joined partial results of one output row, as one thread sees it: its four
-// dimensions, weights 2^(m - M).
-struct Join {
-  float M = kNoMax, L = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  __device__ __forceinline__ void rescale(float m) {
-    const float f = exp2f(M - m);
-    M = m;
-    L *= f;
-    o.x *= f;
-    o.y *= f;
-    o.z *= f;
-    o.w *= f;
-  }
-  __device__ __forceinline__ void add(const float2 ml, const float4 x) {  // ml.x <= M
-    const float f = exp2f(ml.x - M);
-    L += ml.y * f;
-    o.x += x.x * f;
-    o.y += x.y * f;
-    o.z += x.z * f;
-    o.w += x.w * f;
-  }
-  __device__ __forceinline__ float inv() const { return L == 0.f ? 0.f : 1.f / L; }
-  __device__ __forceinline__ float lse() const { return (M + log2f(L)) * kLn2; }
-};
-
-// Joins parts 0 .. n-1 of a row (at(s): pointers to a part's (max, sum) and
-// accumulators) by S groups of 32 threads, of which group 0 has the result.
-// Eight parts of a group are requested together: one round trip for up to 8 S
-// parts.  Parts whose sum is 0 are left out: their accumulators may never have
-// been written.  All threads of the workgroup call.
-template <int S, class At>
-__device__ __forceinline__ Join join_parts(int n, At&& at) {
-  constexpr int kBatch = 8;
-  __shared__ float2 ml_lds[8];
-  __shared__ float4 acc_lds[8][32];
-  const int slot = threadIdx.x >> 5, d4 = threadIdx.x & 31, part = slot % S;
-  Join j;
-  for (int s0 = part; s0 < n; s0 += kBatch * S) {
-    float2 ml[kBatch];
-    float4 x[kBatch];
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) {  // clamped: every load is issued
-      const float* acc;
-      const float2* pair;
-      at(min(s0 + u * S, n - 1), pair, acc);
-      ml[u] = *pair;
-      x[u] = reinterpret_cast<const float4*>(acc)[d4];
-    }
-    float m = j.M;
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      if (s0 + u * S < n && ml[u].y != 0.f) m = fmaxf(m, ml[u].x);
-    j.rescale(m);
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u)
-      if (s0 + u * S < n && ml[u].y != 0.f) j.add(ml[u], x[u]);
-  }
-  if constexpr (S > 1) {
-    if (d4 == 0) ml_lds[slot] = make_float2(j.M, j.L);
-    acc_lds[slot][d4] = j.o;
-    __syncthreads();
-    if (part == 0) {
-      float m = j.M;
-      for (int p = 1; p < S; ++p) m = fmaxf(m, ml_lds[slot + p].x);
-      j.rescale(m);
-      for (int p = 1; p < S; ++p) j.add(ml_lds[slot + p], acc_lds[slot + p][d4]);
-    }
-  }
-  return j;
-}
-
 // 8 / S output rows per workgroup, 32 threads (4 dimensions each) and S of them.
 template <int S>
 __global__ __launch_bounds__(256) void window_merge_kernel(TileArgs a, int rows_per_tile,
@@ -553,8 +454,7 @@ __global__ __launch_bounds__(256) void window_merge_kernel(TileArgs a, int rows_
 // The prefix's partial results and those of the sequence's own tokens.
 template <int S>
 __global__ __launch_bounds__(256) void prefix_merge_kernel(TileArgs a, int rows_per_tile,
-                                                           AttnParts own, const int32_t* own_lens,
-                                                           int own_cap, float* out, float* lse,
+                                                           float* out, float* lse,
                                                            int64_t n_out) {
   const int64_t want = (int64_t)blockIdx.x * (8 / S) + (threadIdx.x >> 5) / S;
   const int64_t orow = want < n_out ? want : n_out - 1;
@@ -565,14 +465,12 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(TileArgs a, int rows_
   const int g = h / a.G;
   const int r = b * a.G + (h - g * a.G);
   const size_t part = ((size_t)layer * a.H_kv + g) * a.n_rt + r / rows_per_tile;
-  const int count = clampi(own_lens[b], 0, own_cap);
-  const int ns = min(own.n_split, (count + own.split - 1) / own.split);
-  const Join j = join_parts<S>(a.n_split + ns, [&](int s, const float2*& ml, const float*& acc) {
+  const Join j = join_parts<S>(a.n_split + a.own.n_split, [&](int s, const float2*& ml, const float*& acc) {
     const bool pre = s < a.n_split;
     const size_t prow = pre ? (part * a.n_split + s) * rows_per_tile + r % rows_per_tile
-                            : ((size_t)lb * own.n_split + (s - a.n_split)) * a.H_q + h;
-    ml = reinterpret_cast<const float2*>(pre ? a.part_ml : own.ml) + prow;
-    acc = (pre ? a.part_acc : own.acc) + prow * kD;
+                            : ((size_t)lb * a.own.n_split + (s - a.n_split)) * a.H_q + h;
+    ml = reinterpret_cast<const float2*>(pre ? a.part_ml : a.own.part_ml) + prow;
+    acc = (pre ? a.part_acc : a.own.part_acc) + prow * kD;
   });
   if (want >= n_out || (threadIdx.x >> 5) % S != 0) return;
   const float inv = j.inv();
@@ -587,17 +485,6 @@ struct TilePlan {
 };
 
 constexpr int kMinSplit = 256;
-
-// Groups of 32 threads that join a row of n partial results: one per eight, whose
-// loads are a single round trip.
-template <class F>
-void with_parts(int n, F&& launch) {
-  if (n <= 8) launch(std::integral_constant<int, 1>{});
-  else if (n <= 16) launch(std::integral_constant<int, 2>{});
-  else if (n <= 32) launch(std::integral_constant<int, 4>{});
-  else launch(std::integral_constant<int, 8>{});
-}
-dim3 merge_grid(int64_t rows, int s) { return dim3((unsigned)((rows * s + 7) / 8)); }
 
 // units: (layer, sequence, KV head); rows: query rows of a unit; most: the most
 // tokens that a row tile of `rows` sees.
@@ -629,7 +516,7 @@ size_t tile_ml_bytes(int64_t units, const TilePlan& p) {
 
 template <bool WINDOW, bool SPLITP>
 hipError_t launch_tiles(const TilePlan& p, const TileArgs& a, hipStream_t s) {
-  const int64_t n = (int64_t)a.n_units * a.n_rt * a.n_split;
+  const int64_t n = (int64_t)a.n_units * a.n_rt * a.n_split + a.own_blocks;
   if (n > INT32_MAX) return hipErrorInvalidValue;
   const dim3 grid((unsigned)n);
   if (p.rows == 256) tile_attn_kernel<8, 1, 64, WINDOW, SPLITP><<<grid, 512, 0, s>>>(a);
@@ -651,29 +538,6 @@ TilePlan prefix_plan(const DenseDims& d) {
   return tile_plan((int64_t)d.n_layers * d.H_kv, (int64_t)d.B * d.G, d.P_cap, false);
 }
 
-// One query token per sequence, as the attention kernels take it: k_max tokens.
-Dims decode_dims(const DenseDims& d, int k_max) {
-  Dims o{};
-  o.B = d.B;
-  o.L_cap = o.L_max = d.L_cap;
-  o.k_max = k_max;
-  o.n_layers = d.n_layers;
-  o.H_q = d.H_q;
-  o.H_kv = d.H_kv;
-  o.d = kD;
-  o.G = d.G;
-  o.n_sets = 1;
-  o.kv_stride_b = d.kv_stride_b;
-  o.kv_stride_layer = d.kv_stride_layer;
-  o.scale = d.scale;
-  o.plain = false;
-  return o;
-}
-int window_tokens(const DenseDims& d) {
-  const int64_t n = (int64_t)d.window + d.n_sink;
-  return (int)(n < d.L_cap ? n : d.L_cap);
-}
-
 }  // namespace
 
 size_t window_ws_bytes(const DenseDims& d) {
@@ -689,7 +553,7 @@ hipError_t launch_window(const DenseDims& d, const uint16_t* q, const uint16_t* 
   const int64_t units = (int64_t)d.n_layers * d.B * d.H_kv;
   TileArgs a{q, k, v, lens, q_lens, out, lse, nullptr, nullptr, d.kv_stride_layer, d.kv_stride_b,
              d.B, d.T, d.H_q, d.H_kv, d.G, d.L_cap, d.window, d.n_sink, (int)units, p.n_rt,
-             p.n_split, p.split_tok, d.scale * kLog2e};
+             p.n_split, p.split_tok, d.scale * kLog2e, DecodeArgs{}, 0};
   if (p.n_split > 1) {
     a.part_acc = static_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + tile_acc_bytes(units, p));
@@ -703,22 +567,33 @@ hipError_t launch_window(const DenseDims& d, const uint16_t* q, const uint16_t* 
   return hipGetLastError();
 }
 
-size_t window_decode_ws_bytes(const DenseDims& d) {
-  return attn_dense_ws_bytes(decode_dims(d, window_tokens(d)), false);
+namespace {
+
+// The own tokens' workgroups: as many wavefronts as the tiles' (so many chunks at
+// least per split), and as few partial results as keep them short.
+int own_split(const DenseDims& d, const TilePlan& p) {
+  const int64_t units = (int64_t)d.n_layers * d.B * d.H_kv * (d.G / group_heads(d.G));
+  const int64_t waves = p.rows == 256 ? 8 : 4;
+  const int64_t most = (d.L_cap + 4 * kDecodeChunk * waves - 1) / (4 * kDecodeChunk * waves);
+  int64_t n = (kCUs + units - 1) / units;
+  if (n > most) n = most;
+  return n < 1 ? 1 : (int)n;
+}
+size_t own_acc_bytes(const DenseDims& d, int n_split) {
+  return align_up(sizeof(float) * kD * (size_t)d.n_layers * d.B * n_split * d.H_q);
+}
+size_t own_ml_bytes(const DenseDims& d, int n_split) {
+  return align_up(sizeof(float) * 2 * (size_t)d.n_layers * d.B * n_split * d.H_q);
 }
 
-hipError_t launch_window_decode(const DenseDims& d, const uint16_t* q, const uint16_t* k,
-                                const uint16_t* v, const int32_t* lens, float* out, float* lse,
-                                void* ws, hipStream_t s) {
-  const DenseAttn m{d.n_sink, nullptr, 0, false, nullptr};
-  return launch_attn_dense(decode_dims(d, window_tokens(d)), m, q, k, v, lens, out, lse, ws, s);
-}
+}  // namespace
 
 size_t prefix_decode_ws_bytes(const DenseDims& d) {
   const TilePlan p = prefix_plan(d);
   const int64_t units = (int64_t)d.n_layers * d.H_kv;
-  return tile_acc_bytes(units, p) + tile_ml_bytes(units, p) +
-         attn_dense_ws_bytes(decode_dims(d, d.L_cap), true);
+  const int ns = own_split(d, p);
+  return tile_acc_bytes(units, p) + tile_ml_bytes(units, p) + own_acc_bytes(d, ns) +
+         own_ml_bytes(d, ns);
 }
 
 hipError_t launch_prefix_decode(const DenseDims& d, const uint16_t* q, const uint16_t* k_prefix,
@@ -727,121 +602,25 @@ hipError_t launch_prefix_decode(const DenseDims& d, const uint16_t* q, const uin
                                 float* out, float* lse, void* ws, hipStream_t s) {
   const TilePlan p = prefix_plan(d);
   const int64_t units = (int64_t)d.n_layers * d.H_kv;
+  const int heads = group_heads(d.G), R = d.G / heads, ns = own_split(d, p);
   char* w = static_cast<char*>(ws);
   TileArgs a{q, k_prefix, v_prefix, prefix_len, nullptr, nullptr, nullptr,
              reinterpret_cast<float*>(w), reinterpret_cast<float*>(w + tile_acc_bytes(units, p)),
              d.prefix_stride_layer, 0, 1, d.B, d.H_q, d.H_kv, d.G, d.P_cap, 0, 0, (int)units,
-             p.n_rt, p.n_split, p.split_tok, d.scale * kLog2e};
-  hipError_t e = launch_tiles<false, true>(p, a, s);
-  if (e != hipSuccess) return e;
-  AttnParts own;
-  const DenseAttn m{d.L_cap, nullptr, 0, true, &own};
-  e = launch_attn_dense(decode_dims(d, d.L_cap), m, q, k, v, lens, nullptr, nullptr,
-                        w + tile_acc_bytes(units, p) + tile_ml_bytes(units, p), s);
+             p.n_rt, p.n_split, p.split_tok, d.scale * kLog2e, DecodeArgs{}, 0};
+  w += tile_acc_bytes(units, p) + tile_ml_bytes(units, p);
+  a.own = DecodeArgs{q, k, v, lens, nullptr, nullptr, reinterpret_cast<float*>(w),
+                     reinterpret_cast<float*>(w + own_acc_bytes(d, ns)), nullptr, nullptr,
+                     d.kv_stride_layer, d.kv_stride_b, 0, d.B, d.H_q, d.H_kv, heads, R, d.L_cap,
+                     d.L_cap, d.L_cap, ns, 0, d.scale * kLog2e};
+  a.own_blocks = (int)((int64_t)d.n_layers * d.B * d.H_kv * R * ns);
+  const hipError_t e = launch_tiles<false, true>(p, a, s);
   if (e != hipSuccess) return e;
   const int64_t n_out = (int64_t)d.n_layers * d.B * d.H_q;
-  with_parts(p.n_split + own.n_split, [&](auto S) {
-    prefix_merge_kernel<S.value><<<merge_grid(n_out, S.value), 256, 0, s>>>(
-        a, p.rows, own, lens, d.L_cap, out, lse, n_out);
+  with_parts(p.n_split + ns, [&](auto S) {
+    prefix_merge_kernel<S.value><<<merge_grid(n_out, S.value), 256, 0, s>>>(a, p.rows, out, lse,
+                                                                           n_out);
   });
-  return hipGetLastError();
-}
-
-// ---- decode attention that adds up its weights ----------------------------
-namespace {
-
-// A workgroup's threads are PARTS parts of a set's heads by 256 / PARTS groups of
-// four tokens.
-constexpr int accum_tokens(int parts) { return 4 * 256 / parts; }
-
-struct AccumArgs {
-  const float* logits;  // [lb][H_q][stride], log2 units
-  const float* lse;     // [lb][H_q]
-  const int32_t* counts;
-  float* weights;       // [lb][n_sets][L_cap]
-  int64_t stride;
-  int B, H_q, n_sets, L_cap, tiles;  // workgroups of a weights row
-};
-
-// weights[lb][set][t] += sum over the set's heads of 2^(logit - lse log2(e)), in a
-// fixed order.  A thread has four tokens of every PARTS-th head, four of them
-// requested together; the parts are added in LDS.
-template <int PARTS>
-__global__ __launch_bounds__(256) void accum_kernel(AccumArgs a) {
-  constexpr int TOK = accum_tokens(PARTS);
-  __shared__ float4 sums[PARTS][TOK / 4];
-  const int tile = blockIdx.x % a.tiles, rest = blockIdx.x / a.tiles;
-  const int set = rest % a.n_sets, lb = rest / a.n_sets;
-  const int count = clampi(a.counts[lb % a.B], 0, a.L_cap);
-  if (tile * TOK >= count) return;  // uniform
-  const int t4 = threadIdx.x % (TOK / 4), part = threadIdx.x / (TOK / 4);
-  const int t0 = tile * TOK + t4 * 4;
-  const int heads = a.H_q / a.n_sets;
-  const size_t h0 = (size_t)lb * a.H_q + (size_t)set * heads;
-  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int h = part; h < heads && t0 < count; h += 4 * PARTS) {
-    float4 x[4];
-    float z[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const size_t r = h0 + min(h + PARTS * u, heads - 1);
-      z[u] = a.lse[r] * kLog2e;
-      x[u] = *reinterpret_cast<const float4*>(a.logits + r * a.stride + t0);
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (h + PARTS * u >= heads || z[u] == -INFINITY) continue;  // all -inf: no weights
-      sum.x += exp2f(x[u].x - z[u]);
-      sum.y += exp2f(x[u].y - z[u]);
-      sum.z += exp2f(x[u].z - z[u]);
-      sum.w += exp2f(x[u].w - z[u]);
-    }
-  }
-  sums[part][t4] = sum;
-  __syncthreads();
-  float* row = a.weights + ((size_t)lb * a.n_sets + set) * a.L_cap;
-  for (int t = threadIdx.x; t < TOK && tile * TOK + t < count; t += 256) {
-    float add = 0.f;
-    for (int p = 0; p < PARTS; ++p) add += reinterpret_cast<const float*>(sums[p])[t];
-    row[tile * TOK + t] += add;
-  }
-}
-
-int64_t accum_stride(const DenseDims& d) { return ((int64_t)d.L_cap + 31) / 32 * 32; }
-size_t accum_logit_bytes(const DenseDims& d) {
-  return align_up(sizeof(float) * (size_t)d.n_layers * d.B * d.H_q * accum_stride(d));
-}
-size_t accum_lse_bytes(const DenseDims& d) {
-  return align_up(sizeof(float) * (size_t)d.n_layers * d.B * d.H_q);
-}
-
-}  // namespace
-
-size_t accum_decode_ws_bytes(const DenseDims& d) {
-  return accum_logit_bytes(d) + accum_lse_bytes(d) +
-         attn_dense_ws_bytes(decode_dims(d, d.L_cap), false);
-}
-
-hipError_t launch_accum_decode(const DenseDims& d, const uint16_t* q, const uint16_t* k,
-                               const uint16_t* v, const int32_t* counts, float* weights,
-                               float* out, float* lse, void* ws, hipStream_t s) {
-  char* w = static_cast<char*>(ws);
-  float* logits = reinterpret_cast<float*>(w);
-  float* z = lse ? lse : reinterpret_cast<float*>(w + accum_logit_bytes(d));
-  const DenseAttn m{d.L_cap, logits, accum_stride(d), false, nullptr};
-  const hipError_t e =
-      launch_attn_dense(decode_dims(d, d.L_cap), m, q, k, v, counts, out, z,
-                        w + accum_logit_bytes(d) + accum_lse_bytes(d), s);
-  if (e != hipSuccess) return e;
-  const int heads = d.H_q / d.n_sets;
-  const int parts = heads >= 16 ? 16 : heads >= 4 ? 4 : 1;
-  const int tiles = (d.L_cap + accum_tokens(parts) - 1) / accum_tokens(parts);
-  const AccumArgs a{logits, z, counts, weights, accum_stride(d), d.B, d.H_q, d.n_sets, d.L_cap,
-                    tiles};
-  const dim3 grid((unsigned)((int64_t)tiles * d.n_sets * d.n_layers * d.B));
-  if (parts == 16) accum_kernel<16><<<grid, 256, 0, s>>>(a);
-  else if (parts == 4) accum_kernel<4><<<grid, 256, 0, s>>>(a);
-  else accum_kernel<1><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

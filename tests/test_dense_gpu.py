@@ -131,13 +131,15 @@ def test_window_decode_strided(dev):
 
 def test_window_decode_agrees_with_the_selection(dev):
     """A window without sinks over fewer tokens than it holds is the compact sparse
-    attention, bit for bit."""
+    attention: each is off by at most its own error."""
     K, V = cache(2, 3, 256, 8, 21, dev)
     q = normal((2, 3, 32, D), 23, dev)
     lens = i32([256, 100, 1], dev)
     a = spec.window_decode_attn(q, K, V, lens, 256)
     b = spec.sparse_decode_attn(q, K, V, lens)
-    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    e = weight_error(f64(q), f64(K), 256)
+    assert (a[0] - b[0]).abs().max() <= 4 * e * float(V.abs().max())
+    assert (a[1] - b[1]).abs().max() <= 2 * e + 32 * U * float(b[1].abs().max())
 
 
 # ------------------------------------------------------------------ window, chunks
