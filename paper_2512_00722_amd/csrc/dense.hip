@@ -1,10 +1,11 @@
 // Decode attention over caches that are read in full: a sliding window with sinks,
 // and with the weights added up per token.
 //
-// One workgroup of four wavefronts takes a (layer, sequence, KV head, column group of
-// at most 16 query heads), or one of n_split parts of it (dense_core.h).  The
-// kernel is bound by memory: two workgroups per CU keep 128 KB in flight each.
-#include <stdlib.h>
+// Workgroups of four wavefronts take one, two or four column groups (layer,
+// sequence, KV head, at most 16 query heads) or one of n_split parts of them
+// (dense_core.h).  The kernel is bound by memory; what a launch reaches of it depends
+// on two things (DecodePlan): one workgroup per CU, and wavefronts side by side on
+// the KV heads of the same tokens, whose rows share DRAM pages.
 #include "dense_core.h"
 
 namespace spec {
@@ -12,13 +13,13 @@ namespace {
 
 constexpr int kW = 4;
 
-template <int HB, int KEEP>
+template <int HB, int KEEP, bool HALF>
 __global__ __launch_bounds__(kW * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void decode_kernel(DecodeArgs a) {
   extern __shared__ __align__(16) float lds_logits[];
-  __shared__ __align__(16) uint16_t tiles[kW][kTileElems];
+  __shared__ __align__(16) uint16_t tiles[kW][tile_elems(HALF)];
   __shared__ float2 ml[kW][16];
-  decode_block<kW, HB, KEEP>(a, blockIdx.x, tiles, ml, lds_logits);
+  decode_block<kW, HB, KEEP, HALF>(a, blockIdx.x, tiles, ml, lds_logits);
 }
 
 // 8 / S output rows per workgroup, 32 threads (4 dimensions each) and S of them.
@@ -109,14 +110,59 @@ void launch_accum(AccumArgs a, int64_t lb, hipStream_t s) {
   else accum_kernel<1><<<grid, 256, 0, s>>>(a);
 }
 
-// Workgroups per unit: enough to give every CU two, of at least one chunk per
-// wavefront.
-int decode_split(const DenseDims& d, int k_max) {
-  const int64_t units = (int64_t)d.n_layers * d.B * d.H_kv * (d.G / group_heads(d.G));
-  const int64_t most = (k_max + kDecodeChunk * kW - 1) / (kDecodeChunk * kW);
-  int64_t n = units >= kCUs ? 1 : 2 * kCUs / units;
-  if (n > most) n = most;
-  return n < 1 ? 1 : (int)n;
+// How a launch is divided: hb column groups per workgroup, each over n_split of them.
+struct DecodePlan {
+  int hb, n_split;
+};
+
+int64_t decode_units(const DenseDims& d) {
+  return (int64_t)d.n_layers * d.B * d.H_kv * (d.G / group_heads(d.G));
+}
+
+// The largest of 4, 2, 1 that divides the column groups and is at most `most`.
+int groups_per_block(const DenseDims& d, int64_t most) {
+  const int64_t n = (int64_t)d.H_kv * (d.G / group_heads(d.G));
+  return n % 4 == 0 && most >= 4 ? 4 : n % 2 == 0 && most >= 2 ? 2 : 1;
+}
+
+// One workgroup per CU is the best number throughout (us, 8 KV heads, bf16; 8 to 1024
+// units of 256 to 16384 tokens were measured with 1, 2, 4 groups per workgroup and 1
+// to 8 workgroups per CU): 64 units x 4096 tokens 26.0, with two per CU 28.4; 1024 x
+// 2048 155.8, two 165.7, four 181.1.  Four groups beside each other are faster where a
+// CU has some 400 tokens or more, as a wavefront then has several chunks: 128 x 1024
+// 16.3 against 18.3 with one, 1024 x 2048 155.8 against 194.7; but 64 x 1024 12.1
+// against 11.5.  Parts cost a merge of about 3.5 us, so that launches which fill the
+// CUs with fewer groups per workgroup and no parts take those up to some 40 us (512
+// x 256: 13.9 against 16.2), and short selections are not divided (8 x 256: 7.3
+// against 8.0).
+DecodePlan decode_plan(const DenseDims& d, int k_max) {
+  const int64_t units = decode_units(d);
+  const double per_cu = (double)units * k_max / kCUs;  // tokens
+  const int64_t chunks = (k_max + kDecodeChunk - 1) / kDecodeChunk;
+  if (per_cu < 400) {
+    const int64_t most = (chunks + kW - 1) / kW;  // a chunk per wavefront at least
+    int64_t n = kCUs / units;
+    if (n > most) n = most;
+    return {1, n < 2 || k_max <= 320 ? 1 : (int)n};
+  }
+  const int hb0 = groups_per_block(d, units / kCUs);
+  if (per_cu < 1500 && units >= kCUs) return {hb0, 1};
+  // Rounds of workgroups per CU: a last one that is not full, and more than one.
+  const int hb = groups_per_block(d, 4);
+  const int64_t most = (chunks + kW / hb - 1) / (kW / hb);
+  const double time = (double)units * k_max / 12890;  // us at 6.6 TB/s
+  double best = 1e30;
+  DecodePlan p{hb, 1};
+  for (int64_t n = 1; n <= most && units / hb * n <= 16 * kCUs + units / hb; ++n) {
+    const int64_t wgs = units / hb * n, rounds = (wgs + kCUs - 1) / kCUs;
+    const double cost = time * rounds * kCUs / wgs * (1 + 0.05 * (rounds < 4 ? rounds - 1 : 3)) +
+                        (n > 1 ? 3.5 : 0);
+    if (cost < best) {
+      best = cost;
+      p.n_split = (int)n;
+    }
+  }
+  return p;
 }
 size_t part_acc_bytes(const DenseDims& d, int n_split) {
   return n_split > 1 ? align_up(sizeof(float) * kHeadDim * (size_t)d.n_layers * d.B * n_split *
@@ -143,15 +189,18 @@ DecodeArgs decode_args(const DenseDims& d, int k_max, int n_sink, int n_split, c
   return a;
 }
 
+// lds: bytes of a column group's logits (kKeepWeights: with four groups the V tiles
+// are of 16 tokens, which leaves the LDS to the logits).
 template <int KEEP>
-hipError_t launch_decode(const DenseDims& d, const DecodeArgs& a, float* out, float* lse,
+hipError_t launch_decode(const DenseDims& d, const DecodeArgs& a, int hb, float* out, float* lse,
                          size_t lds, hipStream_t s) {
-  const int64_t blocks = (int64_t)d.n_layers * d.B * d.H_kv * a.R * a.n_split;
+  const int64_t blocks = decode_units(d) / hb * a.n_split;
   if (blocks > INT32_MAX / (kW * 64)) return hipErrorInvalidValue;
-  static const int hb = getenv("HB") ? atoi(getenv("HB")) : 1;
-  if (hb == 1 || a.n_split > 1) decode_kernel<1, KEEP><<<dim3((unsigned)blocks), kW * 64, lds, s>>>(a);
-  else if (hb == 2) decode_kernel<2, KEEP><<<dim3((unsigned)blocks / 2), kW * 64, 2*lds, s>>>(a);
-  else decode_kernel<4, KEEP><<<dim3((unsigned)blocks / 4), kW * 64, 4*lds, s>>>(a);
+  const dim3 grid((unsigned)blocks), block(kW * 64);
+  if (hb == 1) decode_kernel<1, KEEP, false><<<grid, block, lds, s>>>(a);
+  else if (hb == 2) decode_kernel<2, KEEP, false><<<grid, block, 2 * lds, s>>>(a);
+  else if constexpr (KEEP == kKeepWeights) decode_kernel<4, KEEP, true><<<grid, block, 4 * lds, s>>>(a);
+  else decode_kernel<4, KEEP, false><<<grid, block, 4 * lds, s>>>(a);
   if (a.n_split > 1) {
     const int64_t n_out = (int64_t)d.n_layers * d.B * d.H_q;
     with_parts(a.n_split, [&](auto S) {
@@ -166,27 +215,48 @@ int window_tokens(const DenseDims& d) {
   return (int)(n < d.L_cap ? n : d.L_cap);
 }
 
-// Weights in LDS (kKeepWeights): where a unit is one workgroup's and its logits
-// leave room for a second workgroup on the CU.
-constexpr size_t kLogitLds = 44 * 1024;
+// Where the logits stay until their sums are known: in the LDS of the workgroup that
+// has them all (no parts), or in memory.  us, 8 KV heads: 128 sequences and layers of
+// 2048 tokens, 4 query heads each: four groups per workgroup 166, two 186, one 208,
+// memory 229; of 4000 tokens 356 (two), 420, memory 450; 16 query heads each, 512 tokens:
+// 52, 60, 61, memory 76.  Rates of a CU (GB/s) from those; fewer workgroups than CUs
+// leave it idle, so that small launches go through memory in parts.
 struct AccumPlan {
-  int n_split;
-  bool in_lds;     // else the logits go through memory
-  bool in_place;   // in_lds: a set is one unit, which adds to the weights itself
+  DecodePlan plan;
+  bool in_lds;    // else the logits go through memory
+  bool in_place;  // in_lds: a set is one unit, which adds to the weights itself
 };
+size_t logit_lds(const DenseDims& d) {
+  return sizeof(float) * group_heads(d.G) * logit_pitch(d.L_cap);
+}
 AccumPlan accum_plan(const DenseDims& d) {
-  AccumPlan p;
-  const int heads = group_heads(d.G), R = d.G / heads;
-  p.n_split = decode_split(d, d.L_cap);
-  p.in_lds = p.n_split == 1 && sizeof(float) * heads * logit_pitch(d.L_cap) <= kLogitLds;
-  p.in_place = p.in_lds && d.n_sets == d.H_kv && R == 1;
+  constexpr size_t kLds = 160 * 1024, kRest = 2 * 1024;  // of a CU; beside tiles and logits
+  AccumPlan p{decode_plan(d, d.L_cap), false, false};
+  const int64_t units = decode_units(d);
+  const double bytes = 512.0 * d.L_cap;  // of a unit
+  double best = units * bytes / 4.7e6 + 8;  // us, through memory
+  for (int hb = groups_per_block(d, 4); hb >= 1; hb /= 2) {
+    const size_t lds = hb * logit_lds(d) +
+                       kW * sizeof(uint16_t) * tile_elems(hb == 4) + kRest;
+    if (lds > kLds) continue;
+    const int64_t wgs = units / hb, per_cu = hb == 4 ? 1 : lds <= kLds / 2 ? 2 : 1;
+    const int64_t rounds = (wgs + kCUs * per_cu - 1) / (kCUs * per_cu);
+    const double cu = hb == 4 ? 26e3 : hb == 2 ? 23e3 : 20.5e3;  // bytes per us
+    const double time = rounds * per_cu * hb * bytes / cu + 5;
+    if (time < best) {
+      best = time;
+      p.plan = {hb, 1};
+      p.in_lds = true;
+    }
+  }
+  p.in_place = p.in_lds && d.n_sets == d.H_kv && d.G == group_heads(d.G);
   return p;
 }
 int64_t accum_stride(const DenseDims& d) { return ((int64_t)d.L_cap + 31) / 32 * 32; }
 // Logits [lb][H_q], or the units' weights [lb][H_kv R].
 size_t accum_row_bytes(const DenseDims& d, const AccumPlan& p) {
   if (p.in_place) return 0;
-  const int64_t rows = p.in_lds ? d.H_kv * (d.G / group_heads(d.G)) : d.H_q;
+  const int64_t rows = p.in_lds ? (int64_t)d.H_kv * (d.G / group_heads(d.G)) : d.H_q;
   return align_up(sizeof(float) * (size_t)d.n_layers * d.B * rows * accum_stride(d));
 }
 size_t accum_lse_bytes(const DenseDims& d) {
@@ -196,7 +266,7 @@ size_t accum_lse_bytes(const DenseDims& d) {
 }  // namespace
 
 size_t window_decode_ws_bytes(const DenseDims& d) {
-  const int n = decode_split(d, window_tokens(d));
+  const int n = decode_plan(d, window_tokens(d)).n_split;
   return part_acc_bytes(d, n) + part_ml_bytes(d, n);
 }
 
@@ -204,15 +274,16 @@ hipError_t launch_window_decode(const DenseDims& d, const uint16_t* q, const uin
                                 const uint16_t* v, const int32_t* lens, float* out, float* lse,
                                 void* ws, hipStream_t s) {
   const int k_max = window_tokens(d);
-  const DecodeArgs a = decode_args(d, k_max, d.n_sink, decode_split(d, k_max), q, k, v, lens, out,
-                                   lse, static_cast<char*>(ws));
-  return launch_decode<kKeepNone>(d, a, out, lse, 0, s);
+  const DecodePlan p = decode_plan(d, k_max);
+  const DecodeArgs a = decode_args(d, k_max, d.n_sink, p.n_split, q, k, v, lens, out, lse,
+                                   static_cast<char*>(ws));
+  return launch_decode<kKeepNone>(d, a, p.hb, out, lse, 0, s);
 }
 
 size_t accum_decode_ws_bytes(const DenseDims& d) {
   const AccumPlan p = accum_plan(d);
-  return accum_row_bytes(d, p) + accum_lse_bytes(d) + part_acc_bytes(d, p.n_split) +
-         part_ml_bytes(d, p.n_split);
+  return accum_row_bytes(d, p) + accum_lse_bytes(d) + part_acc_bytes(d, p.plan.n_split) +
+         part_ml_bytes(d, p.plan.n_split);
 }
 
 hipError_t launch_accum_decode(const DenseDims& d, const uint16_t* q, const uint16_t* k,
@@ -224,21 +295,20 @@ hipError_t launch_accum_decode(const DenseDims& d, const uint16_t* q, const uint
   w += accum_row_bytes(d, p);
   float* z = lse ? lse : reinterpret_cast<float*>(w);
   w += accum_lse_bytes(d);
-  DecodeArgs a = decode_args(d, d.L_cap, d.L_cap, p.n_split, q, k, v, counts, out, z, w);
+  DecodeArgs a = decode_args(d, d.L_cap, d.L_cap, p.plan.n_split, q, k, v, counts, out, z, w);
   a.logit_stride = accum_stride(d);
   const int64_t lb = (int64_t)d.n_layers * d.B;
   if (p.in_lds) {
     a.add_weights = p.in_place;
     a.weights = p.in_place ? weights : rows;
-    const size_t lds = sizeof(float) * a.heads * logit_pitch(d.L_cap);
-    const hipError_t e = launch_decode<kKeepWeights>(d, a, out, z, lds, s);
+    const hipError_t e = launch_decode<kKeepWeights>(d, a, p.plan.hb, out, z, logit_lds(d), s);
     if (e != hipSuccess || p.in_place) return e;
     launch_accum({rows, nullptr, counts, weights, a.logit_stride, d.B, d.H_kv * a.R, d.n_sets,
                   d.L_cap, 0}, lb, s);
     return hipGetLastError();
   }
   a.logits = rows;
-  const hipError_t e = launch_decode<kKeepLogits>(d, a, out, z, 0, s);
+  const hipError_t e = launch_decode<kKeepLogits>(d, a, p.plan.hb, out, z, 0, s);
   if (e != hipSuccess) return e;
   launch_accum({rows, z, counts, weights, a.logit_stride, d.B, d.H_q, d.n_sets, d.L_cap, 0}, lb, s);
   return hipGetLastError();

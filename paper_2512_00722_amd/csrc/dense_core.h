@@ -90,25 +90,20 @@ struct DecodeUnit {
   float scale_log2;
 };
 
-// A wavefront's results stand in its V tile: 16 heads of 128 floats.
-constexpr int kTileElems = kDecodeChunk * kHeadDim;  // bf16 elements of a V tile
-static_assert(kTileElems * 2 == 16 * kHeadDim * 4, "results fill the V tile");
-// Four floats of head h, dimensions 4 d4 ..: pieces are swizzled so that the 16
-// heads of a store lie in different banks.
-__device__ __forceinline__ int result_at(int h, int d4) {
-  return h * kHeadDim + ((d4 ^ ((h & 7) << 2)) << 2);
-}
+// bf16 elements of a wavefront's V tile: a whole chunk, or (HALF) its 16-token halves
+// in turn.
+constexpr int kTileElems = kDecodeChunk * kHeadDim;
+constexpr int tile_elems(bool half) { return half ? kTileElems / 2 : kTileElems; }
 
-// Leaves a wavefront's (max, sum) of head h in ml[wave][h] and its accumulators in
-// its part of `tiles` (result_at); keep(head, token, logits of four tokens) is called for
-// every four logits (log2 units) of the wavefront's chunks.  Ends with a barrier.
-template <class Keep>
-__device__ __forceinline__ void decode_unit(const DecodeUnit& u, uint16_t (*tiles)[kTileElems],
-                                            float2 (*ml)[16], Keep&& keep) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// A wavefront's share: maximum and sum of head r16 (l_run complete) and O^T[16 db + 4 kg
+// + i][head r16]; keep(head, token, logits of four tokens) is called for every four
+// logits (log2 units) of its chunks.  V: its V tile.
+template <bool HALF, class Keep>
+__device__ __forceinline__ void decode_unit(const DecodeUnit& u, uint16_t* V, float& m_run,
+                                            float& l_run, floatx4 (&acc)[8], Keep&& keep) {
+  const int lane = threadIdx.x & 63;
   const int r16 = lane & 15;  // head of this lane; token of a K tile row
   const int kg = lane >> 4;
-  uint16_t* V = tiles[wave];
   bf16x8 qf[4];  // Q^T: column r16, dimensions 32 s + 8 kg ..
 #pragma unroll
   for (int s = 0; s < 4; ++s) {
@@ -132,30 +127,43 @@ __device__ __forceinline__ void decode_unit(const DecodeUnit& u, uint16_t (*tile
       for (int s = 0; s < 4; ++s) kr[t][s] = ldg16_stream(p + 32 * s);
     }
   };
-  auto load_v = [&](int c) {  // whole rows: token 4 r + kg, dimensions 8 r16 ..
+  constexpr int VH = HALF ? 4 : 8;  // loads of a V tile
+  auto load_v = [&](int c, int r0) {  // whole rows: token 4 r + kg, dimensions 8 r16 ..
 #pragma unroll
-    for (int r = 0; r < 8; ++r) vr[r] = ldg16_stream(row(u.v, c + 4 * r + kg) + 8 * r16);
+    for (int r = r0; r < r0 + VH; ++r)
+      vr[r] = ldg16_stream(row(u.v, c + 4 * r + kg) + 8 * r16);
+  };
+  auto put_v = [&](int r0) {
+#pragma unroll
+    for (int r = 0; r < VH; ++r) {
+      const int t = 4 * r + kg;
+      *reinterpret_cast<uint4*>(V + t * kHeadDim + ((r16 ^ swizzle(t)) << 3)) = vr[r0 + r];
+    }
+  };
+  // transposed V: tokens 16 h + 4 kg .. + 3, dimensions 16 db + r16
+  auto get_v = [&](int h, int db) {
+    const int t = 16 * h + 4 * kg + (r16 >> 2);
+    const int piece = 2 * db + ((r16 >> 1) & 1);
+    return lds_read_tr(V + t * kHeadDim + ((piece ^ swizzle(t)) << 3) + 4 * (r16 & 1));
   };
 
-  float m_run = kNoMax, l_run = 0.f;
-  floatx4 acc[8];  // O^T[16 db + 4 kg + i][head r16]
+  m_run = kNoMax;
+  l_run = 0.f;
 #pragma unroll
   for (int db = 0; db < 8; ++db) acc[db] = floatx4{0.f, 0.f, 0.f, 0.f};
   if (first < u.count) {
-    load_v(first);
+    load_v(first, 0);
     __builtin_amdgcn_sched_barrier(0);
     load_k(first);
+    __builtin_amdgcn_sched_barrier(0);
+    if (HALF) load_v(first, 4);
     __builtin_amdgcn_sched_barrier(0);
   }
   // Each register buffer is refilled as soon as it is consumed; loads retire in
   // issue order, so that every wait is a partial one.
   for (int c = first; c < u.count; c += step) {
-#pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      const int t = 4 * r + kg;
-      *reinterpret_cast<uint4*>(V + t * kHeadDim + ((r16 ^ swizzle(t)) << 3)) = vr[r];
-    }
-    load_v(c + step);
+    put_v(0);
+    load_v(c + step, 0);
     __builtin_amdgcn_sched_barrier(0);
     floatx4 s[2];
 #pragma unroll
@@ -194,30 +202,63 @@ __device__ __forceinline__ void decode_unit(const DecodeUnit& u, uint16_t (*tile
     }
 #pragma unroll
     for (int db = 0; db < 8; ++db) acc[db] *= alpha;
-    wave_sync_lds();
-    // slots 8 kg .. + 7 of a multiplication: tokens 4 kg .. + 3 and 16 + 4 kg .. + 3
     const bf16x8 ph = to_bf16x8(p), pl = rest_bf16x8(p, ph);
-    const int t0 = 4 * kg + (r16 >> 2);
+    wave_sync_lds();
+    if constexpr (HALF) {
+      typedef short shortx4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-    for (int db = 0; db < 8; ++db) {
-      const int piece = 2 * db + ((r16 >> 1) & 1), at = 4 * (r16 & 1);
-      const bf16x4 x =
-          lds_read_tr(V + t0 * kHeadDim + ((piece ^ swizzle(t0)) << 3) + at);
-      const bf16x4 y = lds_read_tr(V + (16 + t0) * kHeadDim + ((piece ^ swizzle(16 + t0)) << 3) + at);
-      const bf16x8 vf = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-      acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph, acc[db], 0, 0, 0);
-      acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl, acc[db], 0, 0, 0);
+      for (int h = 0; h < 2; ++h) {
+        if (h == 1) {
+          wave_sync_lds();
+          put_v(4);
+          load_v(c + step, 4);
+          __builtin_amdgcn_sched_barrier(0);
+          wave_sync_lds();
+        }
+        const bf16x4 hi = h ? __builtin_shufflevector(ph, ph, 4, 5, 6, 7)
+                            : __builtin_shufflevector(ph, ph, 0, 1, 2, 3);
+        const bf16x4 lo = h ? __builtin_shufflevector(pl, pl, 4, 5, 6, 7)
+                            : __builtin_shufflevector(pl, pl, 0, 1, 2, 3);
+#pragma unroll
+        for (int db = 0; db < 8; ++db) {
+          const shortx4 vf = __builtin_bit_cast(shortx4, get_v(0, db));
+          acc[db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+              vf, __builtin_bit_cast(shortx4, hi), acc[db], 0, 0, 0);
+          acc[db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+              vf, __builtin_bit_cast(shortx4, lo), acc[db], 0, 0, 0);
+        }
+      }
+    } else {
+      // slots 8 kg .. + 7 of a multiplication: tokens 4 kg .. + 3 and 16 + 4 kg .. + 3
+#pragma unroll
+      for (int db = 0; db < 8; ++db) {
+        const bf16x8 vf =
+            __builtin_shufflevector(get_v(0, db), get_v(1, db), 0, 1, 2, 3, 4, 5, 6, 7);
+        acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph, acc[db], 0, 0, 0);
+        acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl, acc[db], 0, 0, 0);
+      }
     }
     wave_sync_lds();  // the tile is rewritten by the next chunk
   }
   l_run = quad_sum(l_run);
+}
+
+// Where several wavefronts share a unit, a wavefront's accumulators stand in its V tile
+// (which it no longer needs): 16 heads of 128 floats.  Four floats of head h, dimensions
+// 4 d4 ..: pieces are swizzled so that the 16 heads of a store lie in different banks.
+static_assert(kTileElems * 2 == 16 * kHeadDim * 4, "results fill the V tile");
+__device__ __forceinline__ int result_at(int h, int d4) {
+  return h * kHeadDim + ((d4 ^ ((h & 7) << 2)) << 2);
+}
+__device__ __forceinline__ void leave_results(uint16_t* V, float2* ml, float m_run, float l_run,
+                                              const floatx4 (&acc)[8]) {
+  const int r16 = threadIdx.x & 15, kg = (threadIdx.x >> 4) & 3;
   float* res = reinterpret_cast<float*>(V);
 #pragma unroll
   for (int db = 0; db < 8; ++db)
     *reinterpret_cast<float4*>(res + result_at(r16, 4 * db + kg)) =
         make_float4(acc[db][0], acc[db][1], acc[db][2], acc[db][3]);
-  if (kg == 0) ml[wave][r16] = make_float2(m_run, l_run);
-  __syncthreads();
+  if (kg == 0) ml[r16] = make_float2(m_run, l_run);
 }
 
 // The joined partial results of one output row, as one thread sees it: its four
@@ -292,10 +333,11 @@ __host__ __device__ inline int logit_pitch(int k_max) { return (k_max + 31) / 32
 // and the heads' weights are added up there; memory sees one value per token
 // instead of one per token and head, which matters as any steady writing takes a
 // kernel that streams from 6.5 to 5 TB/s.
-template <int W, int HB, int KEEP>
+template <int W, int HB, int KEEP, bool HALF = false>
 __device__ __forceinline__ void decode_block(const DecodeArgs& a, int block,
-                                             uint16_t (*tiles)[kTileElems], float2 (*ml)[16],
-                                             float* lds_logits) {
+                                             uint16_t (*tiles)[tile_elems(HALF)],
+                                             float2 (*ml)[16], float* lds_logits) {
+  static_assert(!HALF || W == HB, "half tiles do not hold a wavefront's results");
   const int groups = a.H_kv * a.R / HB;
   const int wave = threadIdx.x >> 6;
   const int split = block % a.n_split, rest = block / a.n_split;
@@ -303,6 +345,7 @@ __device__ __forceinline__ void decode_block(const DecodeArgs& a, int block,
   const int lb = rest / groups, b = lb % a.B;
   const int len = clampi(a.lens[b], 0, a.L_cap);
   const size_t row0 = (size_t)lb * a.H_q + (size_t)gv0 * a.heads;  // first query head
+  const size_t part0 = ((size_t)lb * a.n_split + split) * a.H_q + (size_t)gv0 * a.heads;
   const int64_t base = (int64_t)(lb / a.B) * a.stride_layer + (int64_t)b * a.stride_b +
                        (int64_t)(gv / a.R) * kHeadDim;
   DecodeUnit u;
@@ -318,30 +361,52 @@ __device__ __forceinline__ void decode_block(const DecodeArgs& a, int block,
   u.n_parts = a.n_split * (W / HB);
   u.scale_log2 = a.scale_log2;
   const int pitch = logit_pitch(a.k_max), own = wave % HB * a.heads;
-  decode_unit(u, tiles, ml, [&](int h, int tok, const float* x) {
+  float m_run, l_run;
+  floatx4 acc[8];
+  decode_unit<HALF>(u, tiles[wave], m_run, l_run, acc, [&](int h, int tok, const float* x) {
     if (KEEP == kKeepNone || h >= a.heads) return;
     float* p = KEEP == kKeepWeights ? lds_logits + (own + h) * pitch + tok
                                     : a.logits + (row0 + own + h) * a.logit_stride + tok;
     *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
   });
 
+  // a head all of whose logits are -inf has no weights: 2^(-inf - inf) = 0
   __shared__ float lse2[KEEP == kKeepWeights ? 16 * HB : 1];
-  for (int e = threadIdx.x; e < HB * a.heads * 32; e += W * 64) {
-    const int h = e >> 5, d4 = e & 31;  // query head among the workgroup's
-    const int w0 = HB == 1 ? 0 : h / a.heads;
-    const Join j = join_waves<W, HB>(tiles, ml, w0, h - w0 * a.heads, d4);
-    if (a.out) {
-      const float inv = j.inv();
-      reinterpret_cast<float4*>(a.out + (row0 + h) * kHeadDim)[d4] =
-          make_float4(j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv);
-      if (a.lse && d4 == 0) a.lse[row0 + h] = j.lse();
-    } else {
-      const size_t prow = ((size_t)lb * a.n_split + split) * a.H_q + (size_t)gv0 * a.heads + h;
-      reinterpret_cast<float4*>(a.part_acc + prow * kHeadDim)[d4] = j.o;
-      if (d4 == 0) reinterpret_cast<float2*>(a.part_ml)[prow] = make_float2(j.M, j.L);
+  if constexpr (W == HB) {  // a wavefront's results are the unit's
+    const int r16 = threadIdx.x & 15, kg = (threadIdx.x >> 4) & 3;
+    if (r16 < a.heads) {
+      const int h = own + r16;
+      const float f = !a.out ? 1.f : l_run == 0.f ? 0.f : 1.f / l_run;
+      float* dst = (a.out ? a.out + (row0 + h) * kHeadDim : a.part_acc + (part0 + h) * kHeadDim) +
+                   4 * kg;
+#pragma unroll
+      for (int db = 0; db < 8; ++db)
+        *reinterpret_cast<float4*>(dst + 16 * db) =
+            make_float4(acc[db][0] * f, acc[db][1] * f, acc[db][2] * f, acc[db][3] * f);
+      if (kg == 0) {
+        if (!a.out) reinterpret_cast<float2*>(a.part_ml)[part0 + h] = make_float2(m_run, l_run);
+        else if (a.lse) a.lse[row0 + h] = (m_run + log2f(l_run)) * kLn2;
+        if (KEEP == kKeepWeights) lse2[h] = l_run == 0.f ? INFINITY : m_run + log2f(l_run);
+      }
     }
-    // a head all of whose logits are -inf has no weights: 2^(-inf - inf) = 0
-    if (KEEP == kKeepWeights && d4 == 0) lse2[h] = j.L == 0.f ? INFINITY : j.M + log2f(j.L);
+  } else {
+    leave_results(tiles[wave], ml[wave], m_run, l_run, acc);
+    __syncthreads();
+    for (int e = threadIdx.x; e < HB * a.heads * 32; e += W * 64) {
+      const int h = e >> 5, d4 = e & 31;  // query head among the workgroup's
+      const int w0 = HB == 1 ? 0 : h / a.heads;
+      const Join j = join_waves<W, HB>(tiles, ml, w0, h - w0 * a.heads, d4);
+      if (a.out) {
+        const float inv = j.inv();
+        reinterpret_cast<float4*>(a.out + (row0 + h) * kHeadDim)[d4] =
+            make_float4(j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv);
+        if (a.lse && d4 == 0) a.lse[row0 + h] = j.lse();
+      } else {
+        reinterpret_cast<float4*>(a.part_acc + (part0 + h) * kHeadDim)[d4] = j.o;
+        if (d4 == 0) reinterpret_cast<float2*>(a.part_ml)[part0 + h] = make_float2(j.M, j.L);
+      }
+      if (KEEP == kKeepWeights && d4 == 0) lse2[h] = j.L == 0.f ? INFINITY : j.M + log2f(j.L);
+    }
   }
   if constexpr (KEEP == kKeepWeights) {
     __syncthreads();
