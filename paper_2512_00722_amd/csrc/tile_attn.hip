@@ -486,25 +486,12 @@ struct TilePlan {
 
 constexpr int kMinSplit = 256;
 
-// units: (layer, sequence, KV head); rows: query rows of a unit; most: the most
-// tokens that a row tile of `rows` sees.
-TilePlan tile_plan(int64_t units, int64_t rows, int64_t most, bool shrink) {
-  TilePlan p;
-  p.rows = rows > 128 ? 256 : rows > 64 ? 128 : rows > 32 ? 64 : 32;
-  while (shrink && p.rows > 64 && units * ((rows + p.rows - 1) / p.rows) < kCUs) p.rows /= 2;
-  p.tok = p.rows == 32 ? 128 : 64;
-  p.n_rt = (int)((rows + p.rows - 1) / p.rows);
-  const int64_t wgs = units * p.n_rt;
-  const int64_t target = p.rows == 256 || p.rows == 32 ? kCUs : 2 * kCUs;
-  int64_t ns = (target + wgs - 1) / wgs;
-  const int64_t cap = (most + kMinSplit - 1) / kMinSplit;
-  if (ns > cap) ns = cap;
-  if (ns < 1) ns = 1;
-  const int64_t per = ((most + ns - 1) / ns + p.tok - 1) / p.tok * p.tok;
+// Splits a row tile's `most` tokens into about n parts.
+void split_tokens(TilePlan& p, int64_t most, int64_t n) {
+  const int64_t per = ((most + n - 1) / n + p.tok - 1) / p.tok * p.tok;
   p.split_tok = (int)(per < p.tok ? p.tok : per);
   p.n_split = (int)((most + p.split_tok - 1) / p.split_tok);
   if (p.n_split < 1) p.n_split = 1;
-  return p;
 }
 
 size_t tile_acc_bytes(int64_t units, const TilePlan& p) {
@@ -526,16 +513,80 @@ hipError_t launch_tiles(const TilePlan& p, const TileArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Rows and splits of window chunks by estimated time, in microseconds.  A CU needs
+// `full` for a tile of each kind where it has enough workgroups, and a workgroup
+// alone `alone`; `ends` tiles' time goes into its beginning and end, and `edge`
+// more into the masked tiles of a window's far edge (256 rows: no other workgroup
+// shares the CU and covers them).  A further split costs a launch and the rows'
+// partial results, written and read once each.
+// Measured (us, rows / splits; 32 query and 8 KV heads):
+//   8192 tokens                256/1 554  128/1 577
+//   8192 tokens, window 1024   128/1 176  256/1 200   64/1 219
+//   1024 tokens                 64/1  28  128/1  33  256/1  40   64/2  47
+//   512 of 8192 tokens         256/4  88  128/4  93   64/2 111   64/1 147
+//   128 of 32768 tokens       256/16  88 128/16  93   64/8 110   64/1 556
+//   8 x 16 of 4096 tokens       64/4  34   32/2  42   64/2  48
 TilePlan window_plan(const DenseDims& d) {
-  const int64_t units = (int64_t)d.n_layers * d.B * d.H_kv;
-  // a row tile of r rows covers at most (r - 2) / G + 2 query tokens
-  int64_t most = (int64_t)d.window + d.n_sink + (256 - 2) / d.G + 1;
-  if (most > d.L_cap) most = d.L_cap;
-  return tile_plan(units, (int64_t)d.T * d.G, most, true);
+  struct Kind {
+    int rows, tok;
+    double full, alone, ends, edge;
+  };
+  constexpr Kind kKinds[4] = {{256, 64, 2.05, 1.8, 2.6, 4.},
+                              {128, 64, 1.08, 1.46, 2.3, 1.},
+                              {64, 64, 0.72, 1.09, 2., 0.},
+                              {32, 128, 1.5, 1.5, 2., 0.}};
+  constexpr double kMergeLaunch = 5., kMergeBytes = 4e6;  // us, bytes / us
+  const int64_t units = (int64_t)d.n_layers * d.B * d.H_kv, rows = (int64_t)d.T * d.G;
+  const int64_t cap = d.L_cap;
+  // mean over the query tokens i of min(window, L_cap - T + i + 1)
+  const double before = cap > d.T ? (double)(cap - d.T) : 0., w = d.window < cap ? d.window : (double)cap;
+  const double mean = w <= before ? w
+                      : w >= cap  ? before + 0.5 * d.T
+                                  : w - 0.5 * (w - before) * (w - before) / d.T;
+  TilePlan best{};
+  double least = 0.;
+  for (const Kind& k : kKinds) {
+    TilePlan p{k.rows, k.tok, (int)((rows + k.rows - 1) / k.rows), 1, 0};
+    // a row tile covers at most (rows - 2) / G + 2 query tokens
+    const int64_t span = (k.rows - 2) / d.G + 1;
+    int64_t most = (int64_t)d.window + d.n_sink + span;
+    if (most > cap) most = cap;
+    const double avg = mean + 0.5 * span + d.n_sink < most ? mean + 0.5 * span + d.n_sink : (double)most;
+    for (int64_t n = 1; n == 1 || n <= (most + kMinSplit - 1) / kMinSplit; n *= 2) {
+      split_tokens(p, most, n);
+      const int64_t wgs = units * p.n_rt * p.n_split;
+      if (n > 1 && wgs > 4 * kCUs) break;
+      const double ends = k.ends + (w < cap ? k.edge : 0.);
+      const double longest = p.split_tok / p.tok + ends;
+      const double work = avg / p.n_split / p.tok + ends;
+      double t = (double)((wgs + kCUs - 1) / kCUs) * work * k.full;
+      if (t < longest * k.alone) t = longest * k.alone;
+      if (p.n_split > 1)
+        t += kMergeLaunch + (double)units * (double)rows * p.n_split * (2 * 4 * (kD + 2)) / kMergeBytes;
+      if (best.rows == 0 || t < least) {
+        best = p;
+        least = t;
+      }
+    }
+  }
+  return best;
 }
 
+// Prefix: units are (layer, KV head), rows the batch's query rows of a unit.  Few
+// rows fill the chip by splits of the prefix alone.
 TilePlan prefix_plan(const DenseDims& d) {
-  return tile_plan((int64_t)d.n_layers * d.H_kv, (int64_t)d.B * d.G, d.P_cap, false);
+  const int64_t units = (int64_t)d.n_layers * d.H_kv, rows = (int64_t)d.B * d.G;
+  TilePlan p{};
+  p.rows = rows > 128 ? 256 : rows > 64 ? 128 : rows > 32 ? 64 : 32;
+  p.tok = p.rows == 32 ? 128 : 64;
+  p.n_rt = (int)((rows + p.rows - 1) / p.rows);
+  const int64_t wgs = units * p.n_rt;
+  const int64_t target = p.rows == 256 || p.rows == 32 ? kCUs : 2 * kCUs;
+  int64_t ns = (target + wgs - 1) / wgs;
+  const int64_t cap = ((int64_t)d.P_cap + kMinSplit - 1) / kMinSplit;
+  if (ns > cap) ns = cap;
+  split_tokens(p, d.P_cap, ns < 1 ? 1 : ns);
+  return p;
 }
 
 }  // namespace
