@@ -24,9 +24,9 @@ void decode_kernel(DecodeArgs a) {
 
 // 8 / S output rows per workgroup, 32 threads (4 dimensions each) and S of them.
 template <int S>
-__global__ __launch_bounds__(256) void decode_merge_kernel(DecodeArgs a, float* out, float* lse,
-                                                           int64_t n_out) {
-  const int64_t want = (int64_t)blockIdx.x * (8 / S) + (threadIdx.x >> 5) / S;
+__device__ __forceinline__ void decode_merge(const DecodeArgs& a, int block, float* out,
+                                             float* lse, int64_t n_out) {
+  const int64_t want = (int64_t)block * (8 / S) + (threadIdx.x >> 5) / S;
   const int64_t orow = want < n_out ? want : n_out - 1;
   const int d4 = threadIdx.x & 31;
   const int h = (int)(orow % a.H_q);
@@ -42,10 +42,16 @@ __global__ __launch_bounds__(256) void decode_merge_kernel(DecodeArgs a, float* 
       make_float4(j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv);
   if (lse && d4 == 0) lse[orow] = j.lse();
 }
+template <int S>
+__global__ __launch_bounds__(256) void decode_merge_kernel(DecodeArgs a, float* out, float* lse,
+                                                           int64_t n_out) {
+  decode_merge<S>(a, blockIdx.x, out, lse, n_out);
+}
 
 // A workgroup's threads are PARTS parts of a set's rows by 256 / PARTS groups of
 // four tokens.
 constexpr int accum_tokens(int parts) { return 4 * 256 / parts; }
+constexpr int kAccumMerge = 4;  // parts of decode_merge in the same launch
 
 struct AccumArgs {
   const float* rows;    // [lb][n_rows][stride]: logits (log2 units), or weights (lse null)
@@ -54,6 +60,14 @@ struct AccumArgs {
   float* weights;       // [lb][n_sets][L_cap]
   int64_t stride;
   int B, n_rows, n_sets, L_cap, tiles;  // tiles: workgroups of a weights row
+  // Logits of a pass in parts: the first workgroups join its results, and the others
+  // its sums for themselves, which saves a launch (24 units of 1500 tokens: 10.0 us, 12.3
+  // with it).
+  int merge_blocks;     // 0: one part
+  DecodeArgs of;
+  float* out;
+  float* out_lse;
+  int64_t n_out;
 };
 
 // weights[lb][set][t] += sum over the set's rows of the weight, 2^(logit - lse log2(e)),
@@ -62,8 +76,16 @@ struct AccumArgs {
 template <int PARTS>
 __global__ __launch_bounds__(256) void accum_kernel(AccumArgs a) {
   constexpr int TOK = accum_tokens(PARTS);
+  constexpr int ROWS = 4 * PARTS;       // rows at a time
+  constexpr int LANES = 256 / ROWS;     // that join a row's sums
   __shared__ float4 sums[PARTS][TOK / 4];
-  const int tile = blockIdx.x % a.tiles, rest = blockIdx.x / a.tiles;
+  __shared__ float z_lds[ROWS];
+  if ((int)blockIdx.x < a.merge_blocks) {
+    decode_merge<kAccumMerge>(a.of, blockIdx.x, a.out, a.out_lse, a.n_out);
+    return;
+  }
+  const int block = blockIdx.x - a.merge_blocks;
+  const int tile = block % a.tiles, rest = block / a.tiles;
   const int set = rest % a.n_sets, lb = rest / a.n_sets;
   const int count = clampi(a.counts[lb % a.B], 0, a.L_cap);
   if (tile * TOK >= count) return;  // uniform
@@ -72,22 +94,47 @@ __global__ __launch_bounds__(256) void accum_kernel(AccumArgs a) {
   const int rows = a.n_rows / a.n_sets;
   const size_t r0 = (size_t)lb * a.n_rows + (size_t)set * rows;
   float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int h = part; h < rows && t0 < count; h += 4 * PARTS) {
+  for (int h0 = 0; h0 < rows; h0 += ROWS) {
     float4 x[4];
-    float z[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const size_t r = r0 + min(h + PARTS * u, rows - 1);
-      z[u] = a.lse ? a.lse[r] * kLog2e : 0.f;
-      x[u] = *reinterpret_cast<const float4*>(a.rows + r * a.stride + t0);
+      const size_t r = r0 + min(h0 + part + PARTS * u, rows - 1);
+      x[u] = *reinterpret_cast<const float4*>(a.rows + r * a.stride + min(t0, count - 1) / 4 * 4);
+    }
+    if (a.lse) {  // the rows' sums, in log2 units; +inf where there are no weights
+      const int h = set * rows + min(h0 + (int)threadIdx.x / LANES, rows - 1);
+      float m = kNoMax, l = 0.f;
+      if (a.merge_blocks > 0) {
+        const float2* ml = reinterpret_cast<const float2*>(a.of.part_ml) +
+                           (size_t)lb * a.of.n_split * a.n_rows + h;
+        for (int s = threadIdx.x % LANES; s < a.of.n_split; s += LANES) {
+          const float2 x = ml[(size_t)s * a.n_rows];
+          const float mn = fmaxf(m, x.x);
+          l = l * exp2f(m - mn) + x.y * exp2f(x.x - mn);
+          m = mn;
+        }
+#pragma unroll
+        for (int o = 1; o < LANES; o *= 2) {
+          const float m1 = __shfl_xor(m, o), l1 = __shfl_xor(l, o), mn = fmaxf(m, m1);
+          l = l * exp2f(m - mn) + l1 * exp2f(m1 - mn);
+          m = mn;
+        }
+        m += log2f(l);
+      } else {
+        m = a.lse[(size_t)lb * a.n_rows + h] * kLog2e;
+      }
+      __syncthreads();
+      if (threadIdx.x % LANES == 0) z_lds[threadIdx.x / LANES] = m == -INFINITY ? INFINITY : m;
+      __syncthreads();
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      if (h + PARTS * u >= rows || z[u] == -INFINITY) continue;  // all -inf: no weights
-      sum.x += a.lse ? exp2f(x[u].x - z[u]) : x[u].x;
-      sum.y += a.lse ? exp2f(x[u].y - z[u]) : x[u].y;
-      sum.z += a.lse ? exp2f(x[u].z - z[u]) : x[u].z;
-      sum.w += a.lse ? exp2f(x[u].w - z[u]) : x[u].w;
+      if (h0 + part + PARTS * u >= rows) continue;
+      const float z = z_lds[part + PARTS * u];
+      sum.x += a.lse ? exp2f(x[u].x - z) : x[u].x;
+      sum.y += a.lse ? exp2f(x[u].y - z) : x[u].y;
+      sum.z += a.lse ? exp2f(x[u].z - z) : x[u].z;
+      sum.w += a.lse ? exp2f(x[u].w - z) : x[u].w;
     }
   }
   sums[part][t4] = sum;
@@ -100,14 +147,17 @@ __global__ __launch_bounds__(256) void accum_kernel(AccumArgs a) {
   }
 }
 
-void launch_accum(AccumArgs a, int64_t lb, hipStream_t s) {
+hipError_t launch_accum(AccumArgs a, int64_t lb, hipStream_t s) {
   const int rows = a.n_rows / a.n_sets;
   const int parts = rows >= 16 ? 16 : rows >= 4 ? 4 : 1;
   a.tiles = (a.L_cap + accum_tokens(parts) - 1) / accum_tokens(parts);
-  const dim3 grid((unsigned)(a.tiles * a.n_sets * lb));
+  const int64_t blocks = (int64_t)a.tiles * a.n_sets * lb + a.merge_blocks;
+  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks);
   if (parts == 16) accum_kernel<16><<<grid, 256, 0, s>>>(a);
   else if (parts == 4) accum_kernel<4><<<grid, 256, 0, s>>>(a);
   else accum_kernel<1><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 // How a launch is divided: hb column groups per workgroup, each over n_split of them.
@@ -192,8 +242,8 @@ DecodeArgs decode_args(const DenseDims& d, int k_max, int n_sink, int n_split, c
 // lds: bytes of a column group's logits (kKeepWeights: with four groups the V tiles
 // are of 16 tokens, which leaves the LDS to the logits).
 template <int KEEP>
-hipError_t launch_decode(const DenseDims& d, const DecodeArgs& a, int hb, float* out, float* lse,
-                         size_t lds, hipStream_t s) {
+hipError_t launch_decode(const DenseDims& d, const DecodeArgs& a, int hb, size_t lds,
+                         hipStream_t s) {
   const int64_t blocks = decode_units(d) / hb * a.n_split;
   if (blocks > INT32_MAX / (kW * 64)) return hipErrorInvalidValue;
   const dim3 grid((unsigned)blocks), block(kW * 64);
@@ -201,12 +251,6 @@ hipError_t launch_decode(const DenseDims& d, const DecodeArgs& a, int hb, float*
   else if (hb == 2) decode_kernel<2, KEEP, false><<<grid, block, 2 * lds, s>>>(a);
   else if constexpr (KEEP == kKeepWeights) decode_kernel<4, KEEP, true><<<grid, block, 4 * lds, s>>>(a);
   else decode_kernel<4, KEEP, false><<<grid, block, 4 * lds, s>>>(a);
-  if (a.n_split > 1) {
-    const int64_t n_out = (int64_t)d.n_layers * d.B * d.H_q;
-    with_parts(a.n_split, [&](auto S) {
-      decode_merge_kernel<S.value><<<merge_grid(n_out, S.value), 256, 0, s>>>(a, out, lse, n_out);
-    });
-  }
   return hipGetLastError();
 }
 
@@ -277,7 +321,13 @@ hipError_t launch_window_decode(const DenseDims& d, const uint16_t* q, const uin
   const DecodePlan p = decode_plan(d, k_max);
   const DecodeArgs a = decode_args(d, k_max, d.n_sink, p.n_split, q, k, v, lens, out, lse,
                                    static_cast<char*>(ws));
-  return launch_decode<kKeepNone>(d, a, p.hb, out, lse, 0, s);
+  const hipError_t e = launch_decode<kKeepNone>(d, a, p.hb, 0, s);
+  if (e != hipSuccess || p.n_split == 1) return e;
+  const int64_t n_out = (int64_t)d.n_layers * d.B * d.H_q;
+  with_parts(p.n_split, [&](auto S) {
+    decode_merge_kernel<S.value><<<merge_grid(n_out, S.value), 256, 0, s>>>(a, out, lse, n_out);
+  });
+  return hipGetLastError();
 }
 
 size_t accum_decode_ws_bytes(const DenseDims& d) {
@@ -301,17 +351,18 @@ hipError_t launch_accum_decode(const DenseDims& d, const uint16_t* q, const uint
   if (p.in_lds) {
     a.add_weights = p.in_place;
     a.weights = p.in_place ? weights : rows;
-    const hipError_t e = launch_decode<kKeepWeights>(d, a, p.plan.hb, out, z, logit_lds(d), s);
+    const hipError_t e = launch_decode<kKeepWeights>(d, a, p.plan.hb, logit_lds(d), s);
     if (e != hipSuccess || p.in_place) return e;
-    launch_accum({rows, nullptr, counts, weights, a.logit_stride, d.B, d.H_kv * a.R, d.n_sets,
-                  d.L_cap, 0}, lb, s);
-    return hipGetLastError();
+    return launch_accum({rows, nullptr, counts, weights, a.logit_stride, d.B, d.H_kv * a.R,
+                         d.n_sets, d.L_cap, 0, 0, a, nullptr, nullptr, 0}, lb, s);
   }
   a.logits = rows;
-  const hipError_t e = launch_decode<kKeepLogits>(d, a, p.plan.hb, out, z, 0, s);
+  const hipError_t e = launch_decode<kKeepLogits>(d, a, p.plan.hb, 0, s);
   if (e != hipSuccess) return e;
-  launch_accum({rows, z, counts, weights, a.logit_stride, d.B, d.H_q, d.n_sets, d.L_cap, 0}, lb, s);
-  return hipGetLastError();
+  const int64_t n_out = lb * d.H_q;
+  const int merge = p.plan.n_split > 1 ? (int)merge_grid(n_out, kAccumMerge).x : 0;
+  return launch_accum({rows, z, counts, weights, a.logit_stride, d.B, d.H_q, d.n_sets, d.L_cap, 0,
+                       merge, a, out, lse, n_out}, lb, s);
 }
 
 }  // namespace spec
