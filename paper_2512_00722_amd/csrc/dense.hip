@@ -152,7 +152,7 @@ hipError_t launch_accum(AccumArgs a, int64_t lb, hipStream_t s) {
   const int parts = rows >= 16 ? 16 : rows >= 4 ? 4 : 1;
   a.tiles = (a.L_cap + accum_tokens(parts) - 1) / accum_tokens(parts);
   const int64_t blocks = (int64_t)a.tiles * a.n_sets * lb + a.merge_blocks;
-  if (blocks > INT32_MAX) return hipErrorInvalidValue;
+  if (blocks > UINT32_MAX / 256) return hipErrorInvalidValue;  // threads of a launch
   const dim3 grid((unsigned)blocks);
   if (parts == 16) accum_kernel<16><<<grid, 256, 0, s>>>(a);
   else if (parts == 4) accum_kernel<4><<<grid, 256, 0, s>>>(a);

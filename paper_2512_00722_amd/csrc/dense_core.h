@@ -423,13 +423,6 @@ __device__ __forceinline__ void decode_block(const DecodeArgs& a, int block,
   }
 }
 
-// Query heads of a column group: all of a KV head's where there are at most 16, else
-// their largest divisor up to 16.
-inline int group_heads(int G) {
-  int c = G < 16 ? G : 16;
-  while (G % c) --c;
-  return c;
-}
 // Joins parts 0 .. n-1 of a row (at(s): pointers to a part's (max, sum) and
 // accumulators) by S groups of 32 threads, of which group 0 has the result.
 // Eight parts of a group are requested together: one round trip for up to 8 S

@@ -244,6 +244,13 @@ struct DenseDims {
   float scale;
 };
 constexpr int kHeadDim = 128;
+// Query heads of a column group: all of a KV head's where there are at most 16, else
+// their largest divisor up to 16.
+inline int group_heads(int G) {
+  int c = G < 16 ? G : 16;
+  while (G % c) --c;
+  return c;
+}
 
 size_t window_ws_bytes(const DenseDims& d);
 hipError_t launch_window(const DenseDims& d, const uint16_t* q, const uint16_t* k,

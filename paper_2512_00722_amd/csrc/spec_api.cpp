@@ -371,12 +371,15 @@ spec_status resolve_dense(const spec_dense_dims* dm, spec_dense_op op, spec::Den
   if ((evict || op == SPEC_DENSE_ACCUM_DECODE) && dm->n_sets != 1 && dm->n_sets != dm->H_kv)
     return SPEC_ERR_UNSUPPORTED;
   if (dm->B > 65535 || dm->n_layers > 65535 || dm->H_kv > 65535) return SPEC_ERR_UNSUPPORTED;
-  // Launch grids: at most 2^26 query rows, 2^21 KV heads or token sets, and
-  // 2^23 workgroups over the weights.
+  // Launch grids: at most 2^26 query rows, 2^21 KV heads or token sets, 2^22 column
+  // groups of a decode launch, and 2^23 workgroups over the weights.
   const int64_t lb = (int64_t)dm->n_layers * dm->B;
   if (lb * dm->H_kv > 1 << 21) return SPEC_ERR_UNSUPPORTED;
   if (!evict && lb * dm->H_q > 1 << 26) return SPEC_ERR_UNSUPPORTED;
   if (op == SPEC_DENSE_WINDOW && (lb * dm->H_q * dm->T > 1 << 26)) return SPEC_ERR_UNSUPPORTED;
+  if (!evict && op != SPEC_DENSE_WINDOW &&
+      lb * dm->H_q / spec::group_heads(dm->H_q / dm->H_kv) > 1 << 22)
+    return SPEC_ERR_UNSUPPORTED;
   if (op == SPEC_DENSE_ACCUM_DECODE && lb * dm->n_sets * (dm->L_cap / 64 + 1) > 1 << 23)
     return SPEC_ERR_UNSUPPORTED;
   if ((int64_t)dm->L_cap + dm->T > INT32_MAX - 4096 || dm->P_cap > INT32_MAX - 4096)

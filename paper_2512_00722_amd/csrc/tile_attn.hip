@@ -504,7 +504,7 @@ size_t tile_ml_bytes(int64_t units, const TilePlan& p) {
 template <bool WINDOW, bool SPLITP>
 hipError_t launch_tiles(const TilePlan& p, const TileArgs& a, hipStream_t s) {
   const int64_t n = (int64_t)a.n_units * a.n_rt * a.n_split + a.own_blocks;
-  if (n > INT32_MAX) return hipErrorInvalidValue;
+  if (n > UINT32_MAX / 512) return hipErrorInvalidValue;  // threads of a launch
   const dim3 grid((unsigned)n);
   if (p.rows == 256) tile_attn_kernel<8, 1, 64, WINDOW, SPLITP><<<grid, 512, 0, s>>>(a);
   else if (p.rows == 128) tile_attn_kernel<4, 1, 64, WINDOW, SPLITP><<<grid, 256, 0, s>>>(a);

@@ -198,3 +198,16 @@ def test_oracle_evict_by_hand():
     # more new rows than the budget: the last of them
     assert dense_oracle.evict_plan(w, t, 5, 4, 2, 15, 0, 0) == (2, [(0, ("new", 2)),
                                                                    (1, ("new", 3))])
+
+
+def test_sizes_beyond_a_launch_are_refused(lib):
+    big = dict(B=65535, L_cap=64, n_layers=1, T=1, n_sets=1)
+    for op, kw, want in (
+            (0, dict(H_q=32, H_kv=32), 0), (0, dict(H_q=64, H_kv=64), 2),      # KV heads
+            (1, dict(H_q=32, H_kv=8, T=33), 2), (1, dict(H_q=32, H_kv=8, T=2), 0),
+            (0, dict(H_q=8 * 127, H_kv=8), 2), (0, dict(H_q=8 * 128, H_kv=8), 0),
+            (0, dict(H_q=127, H_kv=1), 2), (2, dict(H_q=127, H_kv=1), 2),      # a prime: 127 groups
+            (3, dict(H_q=127, H_kv=1), 2), (1, dict(H_q=127, H_kv=1), 0),
+            (3, dict(H_q=8, H_kv=8, L_cap=1 << 14), 2), (3, dict(H_q=8, H_kv=8, L_cap=1 << 12), 0)):
+        status, n = size(lib, dims(**{**big, **kw}), op)
+        assert status == want, (op, kw, status)
