@@ -38,12 +38,11 @@ __device__ __forceinline__ bf16x8 to_bf16x8(const float* p) {  // round to neare
   }
   return r;
 }
-// What to_bf16x8 left of eight values, rounded: a pair holds them to ~2^-18.
-__device__ __forceinline__ bf16x8 rest_bf16x8(const float* p, bf16x8 high) {
-  float lo[8];
+// Takes what to_bf16x8 gave off eight values (exactly) and rounds the rest.
+__device__ __forceinline__ bf16x8 next_bf16x8(float* p, bf16x8 high) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) lo[e] = p[e] - (float)high[e];
-  return to_bf16x8(lo);
+  for (int e = 0; e < 8; ++e) p[e] -= (float)high[e];
+  return to_bf16x8(p);
 }
 
 // LDS tiles of whole 256-byte rows: the 16-byte pieces of a row stand at piece ^
@@ -202,7 +201,10 @@ __device__ __forceinline__ void decode_unit(const DecodeUnit& u, uint16_t* V, fl
     }
 #pragma unroll
     for (int db = 0; db < 8; ++db) acc[db] *= alpha;
-    const bf16x8 ph = to_bf16x8(p), pl = rest_bf16x8(p, ph);
+    // Weights enter as three bf16 numbers, 2^-26 relative: a pair's 2^-18 would be most of
+    // the result's error, and the third is free in a kernel bound by memory (321 us with
+    // either; 32 layers x 8 sequences x 2048 tokens).
+    const bf16x8 ph = to_bf16x8(p), pl = next_bf16x8(p, ph), pt = next_bf16x8(p, pl);
     wave_sync_lds();
     if constexpr (HALF) {
       typedef short shortx4 __attribute__((ext_vector_type(4)));
@@ -219,6 +221,8 @@ __device__ __forceinline__ void decode_unit(const DecodeUnit& u, uint16_t* V, fl
                             : __builtin_shufflevector(ph, ph, 0, 1, 2, 3);
         const bf16x4 lo = h ? __builtin_shufflevector(pl, pl, 4, 5, 6, 7)
                             : __builtin_shufflevector(pl, pl, 0, 1, 2, 3);
+        const bf16x4 th = h ? __builtin_shufflevector(pt, pt, 4, 5, 6, 7)
+                            : __builtin_shufflevector(pt, pt, 0, 1, 2, 3);
 #pragma unroll
         for (int db = 0; db < 8; ++db) {
           const shortx4 vf = __builtin_bit_cast(shortx4, get_v(0, db));
@@ -226,6 +230,8 @@ __device__ __forceinline__ void decode_unit(const DecodeUnit& u, uint16_t* V, fl
               vf, __builtin_bit_cast(shortx4, hi), acc[db], 0, 0, 0);
           acc[db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
               vf, __builtin_bit_cast(shortx4, lo), acc[db], 0, 0, 0);
+          acc[db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+              vf, __builtin_bit_cast(shortx4, th), acc[db], 0, 0, 0);
         }
       }
     } else {
@@ -236,6 +242,7 @@ __device__ __forceinline__ void decode_unit(const DecodeUnit& u, uint16_t* V, fl
             __builtin_shufflevector(get_v(0, db), get_v(1, db), 0, 1, 2, 3, 4, 5, 6, 7);
         acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph, acc[db], 0, 0, 0);
         acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl, acc[db], 0, 0, 0);
+        acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pt, acc[db], 0, 0, 0);
       }
     }
     wave_sync_lds();  // the tile is rewritten by the next chunk

@@ -124,8 +124,10 @@ __device__ __forceinline__ void attend_by_token(const TileArgs& a, const uint16_
 
 // RW x TW wavefronts: RW groups of 32 rows, TW parts of each tile's tokens.
 // WINDOW: masked rows of a sequence; else every row sees all tokens.  SPLITP:
-// weights as a bf16 pair (~2^-18 relative) for fp32 results; else rounded to
-// bf16 once (2^-9), which the rounding of a bf16 result hides.
+// weights as a bf16 pair (~2^-18 relative) for fp32 results, or with few rows, which
+// leave the matrix cores idle, as three bf16 numbers (2 % of the time of 32 rows, 5 %
+// of that of 64); else rounded to bf16 once (2^-9), which the rounding of a bf16
+// result hides.
 template <int RW, int TW, int TOK, bool WINDOW, bool SPLITP>
 __global__ __launch_bounds__(RW* TW * 64) __attribute__((amdgpu_waves_per_eu(TOK == 64 ? 2 : 1)))
 void tile_attn_kernel(TileArgs a) {
@@ -311,7 +313,8 @@ void tile_attn_kernel(TileArgs a) {
       for (int db = 0; db < 4; ++db) acc[db] *= alpha;
     }
 
-    bf16x8 ph[2 * NB], pl[SPLITP ? 2 * NB : 1];
+    constexpr bool kThird = SPLITP && RW == 1;
+    bf16x8 ph[2 * NB], pl[SPLITP ? 2 * NB : 1], pt[kThird ? 2 * NB : 1];
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk) {
       float p[16];
@@ -323,7 +326,8 @@ void tile_attn_kernel(TileArgs a) {
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         ph[2 * blk + m] = to_bf16x8(p + 8 * m);
-        if constexpr (SPLITP) pl[2 * blk + m] = rest_bf16x8(p + 8 * m, ph[2 * blk + m]);
+        if constexpr (SPLITP) pl[2 * blk + m] = next_bf16x8(p + 8 * m, ph[2 * blk + m]);
+        if constexpr (kThird) pt[2 * blk + m] = next_bf16x8(p + 8 * m, pl[2 * blk + m]);
       }
     }
 
@@ -342,6 +346,8 @@ void tile_attn_kernel(TileArgs a) {
         acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, ph[m], acc[db], 0, 0, 0);
         if constexpr (SPLITP)
           acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl[m], acc[db], 0, 0, 0);
+        if constexpr (kThird)
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pt[m], acc[db], 0, 0, 0);
       }
     }
 
