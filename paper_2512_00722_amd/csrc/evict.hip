@@ -28,24 +28,9 @@
 namespace spec {
 namespace {
 
-// Per sequence: rows held before, E, C', first new row taken.
-__global__ __launch_bounds__(256) void evict_counts_kernel(int32_t* counts, const int32_t* keep,
-                                                           const int32_t* n_new, int4* head, int B,
-                                                           int L_cap, int T) {
-  const int b = blockIdx.x * 256 + threadIdx.x;
-  if (b >= B) return;
-  const int c = clampi(counts[b], 0, L_cap);
-  const int n = n_new ? clampi(n_new[b], 0, T) : T;
-  const int k = clampi(keep[b], 0, L_cap);
-  const int after = (int)min((int64_t)k, (int64_t)c + n);
-  const int taken = min(n, after);
-  head[b] = make_int4(c, after - taken, after, n - taken);
-  counts[b] = after;
-}
-
 struct EvictKernelArgs {
   EvictArgs x;
-  const int4* head;      // [B]
+  int4* head;            // [B] head_of each sequence
   int2* filled;          // [sets]: slots filled, of them from the cache
   int32_t* dst;          // [sets][L_cap] slots filled, ascending
   int32_t* src;          // [sets][L_cap] kept slots at C' or above, ascending
@@ -53,6 +38,32 @@ struct EvictKernelArgs {
   int B, n_sets, H_kv, L_cap, T, n_recent, n_sink;
   int blocks;            // workgroups of a set in the move
 };
+
+// Of a sequence: rows held before, E, C', first new row taken.
+__device__ __forceinline__ int4 head_of(const EvictKernelArgs& a, int b) {
+  const int c = clampi(a.x.counts[b], 0, a.L_cap);
+  const int n = a.x.n_new ? clampi(a.x.n_new[b], 0, a.T) : a.T;
+  const int k = clampi(a.x.keep[b], 0, a.L_cap);
+  const int after = (int)min((int64_t)k, (int64_t)c + n);
+  const int taken = min(n, after);
+  return make_int4(c, after - taken, after, n - taken);
+}
+// Every workgroup of a plan reads the counts, so that they are rewritten in another
+// launch: before a plan that moves the rows itself, else by the move.
+__global__ __launch_bounds__(256) void evict_counts_kernel(EvictKernelArgs a) {
+  const int b = blockIdx.x * 256 + threadIdx.x;
+  if (b >= a.B) return;
+  const int4 hd = head_of(a, b);
+  a.head[b] = hd;
+  a.x.counts[b] = hd.z;
+}
+__device__ __forceinline__ int4 plan_head(const EvictKernelArgs& a, int set, bool move) {
+  const int b = (set / a.n_sets) % a.B;
+  if (move) return a.head[b];
+  const int4 hd = head_of(a, b);
+  if (set == b * a.n_sets && threadIdx.x == 0) a.head[b] = hd;
+  return hd;
+}
 
 // Protected rows count as +inf; NaN ranks with -inf, -0 with +0.
 __device__ __forceinline__ uint32_t rank_key(float w, int32_t tok, int64_t recent_from,
@@ -170,7 +181,7 @@ __global__ __launch_bounds__(NT) void evict_plan_kernel(EvictKernelArgs a) {
   const int set = blockIdx.x;
   const int b = (set / a.n_sets) % a.B;
   const int tid = threadIdx.x, wave = tid >> 6;
-  const int4 hd = a.head[b];
+  const int4 hd = plan_head(a, set, MOVE);
   const int c = hd.x, E = hd.y, after = hd.z, taken = after - E;
   const int64_t recent_from =
       (int64_t)a.x.pos[b] + (a.x.n_new ? clampi(a.x.n_new[b], 0, a.T) : a.T) - a.n_recent;
@@ -317,7 +328,7 @@ __global__ __launch_bounds__(kRadixThreads) void evict_plan_long_kernel(EvictKer
   const int set = blockIdx.x;
   const int b = (set / a.n_sets) % a.B;
   const int tid = threadIdx.x;
-  const int4 hd = a.head[b];
+  const int4 hd = plan_head(a, set, false);
   const int c = hd.x, E = hd.y, after = hd.z, taken = after - E;
   const float* w = a.x.weights + (size_t)set * a.L_cap;
   const int32_t* tok = a.x.tokens + (size_t)set * a.L_cap;
@@ -395,6 +406,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictKernelArgs a) {
   const int set = blockIdx.x / a.blocks, part = blockIdx.x % a.blocks;
   const int b = (set / a.n_sets) % a.B;
   const size_t list = (size_t)set * a.L_cap;
+  if (blockIdx.x == b * a.n_sets * a.blocks && threadIdx.x == 0) a.x.counts[b] = a.head[b].z;
   move_rows(a, set, a.head[b].w, a.filled[set], a.dst + list, a.src + list,
             (int64_t)part * 256 + threadIdx.x, (int64_t)a.blocks * 256);
 }
@@ -439,10 +451,9 @@ hipError_t launch_evict(const DenseDims& d, const EvictArgs& x, void* ws, hipStr
   const int blocks = (int)(sets >= 2048 ? 1 : 2048 / sets);
   const EvictKernelArgs a{x, head, filled, dst, src, d.kv_stride_layer, d.kv_stride_b, d.B,
                           d.n_sets, d.H_kv, d.L_cap, d.T, d.n_recent, d.n_sink, blocks};
-  evict_counts_kernel<<<dim3((unsigned)((d.B + 255) / 256)), 256, 0, s>>>(
-      x.counts, x.keep, x.n_new, head, d.B, d.L_cap, d.T);
   const bool in_plan = d.T > 0 && d.T <= kMoveInPlan && d.L_cap <= kPlanSlots;
   if (in_plan) {
+    evict_counts_kernel<<<dim3((unsigned)((d.B + 255) / 256)), 256, 0, s>>>(a);
     launch_plan<true>(sets, a, s);
     return hipGetLastError();
   }
