@@ -259,102 +259,106 @@ void tile_attn_kernel(TileArgs a) {
   if (n_tiles > 0) {
     issue(0);
     put(0);
+    // Used here, and inside a branch that no way into the loop leaves out, as the tiles
+    // would otherwise wait for them, and with them for the loads in flight.
+#pragma unroll
+    for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(qf[s]));
     if (n_tiles > 1) issue(1);
-  }
-  __syncthreads();
-
-  for (int it = 0; it < n_tiles; ++it) {
-    const uint16_t* Kt = lds[it & 1][0];
-    const uint16_t* Vt = lds[it & 1][1];
-    const int j0 = v0 + it * TOK;
-
-    // S^T of this wavefront's blocks: token 32 blk + 8 (i / 4) + 4 kg + i % 4
-    floatx16 s[NB];
-#pragma unroll
-    for (int blk = 0; blk < NB; ++blk) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[blk][i] = 0.f;
-      const uint16_t* kp = Kt + ((tw * NB + blk) * 32 + c32) * kD;
-#pragma unroll
-      for (int st = 0; st < 8; ++st) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kp + (((2 * st) ^ ksw) * 8));
-        s[blk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[blk], 0, 0, 0);
-      }
-    }
-
-    const bool masked = needs_mask(it);
-    if (masked) {
-#pragma unroll
-      for (int blk = 0; blk < NB; ++blk)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = j0 + (tw * NB + blk) * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
-          bool see = j < v1;
-          if (WINDOW) {
-            const int t = token_of(j);
-            see = see && t <= pos && (t < a.n_sink || t > pos - a.window);
-          }
-          s[blk][i] = see ? s[blk][i] : -INFINITY;
-        }
-    }
-
-    float mx = -INFINITY;
-#pragma unroll
-    for (int blk = 0; blk < NB; ++blk)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[blk][i]);
-    mx = pair_max(mx) * a.scale_log2;
-    if (__any(mx > m_run + kSlack)) {
-      const float mn = fmaxf(m_run, mx);
-      const float alpha = exp2_fast(m_run - mn);
-      m_run = mn;
-      l_run *= alpha;
-#pragma unroll
-      for (int db = 0; db < 4; ++db) acc[db] *= alpha;
-    }
-
-    constexpr bool kThird = SPLITP && RW == 1;
-    bf16x8 ph[2 * NB], pl[SPLITP ? 2 * NB : 1], pt[kThird ? 2 * NB : 1];
-#pragma unroll
-    for (int blk = 0; blk < NB; ++blk) {
-      float p[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[i] = exp2_fast(fmaf(s[blk][i], a.scale_log2, -m_run));
-        l_run += p[i];
-      }
-#pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        ph[2 * blk + m] = to_bf16x8(p + 8 * m);
-        if constexpr (SPLITP) pl[2 * blk + m] = next_bf16x8(p + 8 * m, ph[2 * blk + m]);
-        if constexpr (kThird) pt[2 * blk + m] = next_bf16x8(p + 8 * m, pl[2 * blk + m]);
-      }
-    }
-
-    // O^T += V^T P^T: slots 8 kg .. 8 kg + 7 of a multiplication are tokens
-    // 16 m + 4 kg + 0..3 and 16 m + 8 + 4 kg + 0..3, as this lane holds P.
-#pragma unroll
-    for (int m = 0; m < 2 * NB; ++m) {
-      const uint16_t* vp = Vt + ((tw * NB) * 32 + 16 * m + 4 * kg + (a16 >> 2)) * kD + 4 * (a16 & 1);
-      const int lo0 = (2 * half16 + ((a16 >> 1) & 1)) ^ kg;
-#pragma unroll
-      for (int db = 0; db < 4; ++db) {
-        const int hi4 = 4 * (db ^ (a16 >> 2));
-        const bf16x4 x = lds_read_tr(vp + (hi4 + lo0) * 8);
-        const bf16x4 y = lds_read_tr(vp + 8 * kD + (hi4 + (lo0 ^ 2)) * 8);
-        const bf16x8 vf = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, ph[m], acc[db], 0, 0, 0);
-        if constexpr (SPLITP)
-          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl[m], acc[db], 0, 0, 0);
-        if constexpr (kThird)
-          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pt[m], acc[db], 0, 0, 0);
-      }
-    }
-
-    // The other buffer was last read before the previous barrier.
-    if (it + 1 < n_tiles) put(it + 1);
-    if (it + 2 < n_tiles) issue(it + 2);
     __syncthreads();
+
+    for (int it = 0; it < n_tiles; ++it) {
+      const uint16_t* Kt = lds[it & 1][0];
+      const uint16_t* Vt = lds[it & 1][1];
+      const int j0 = v0 + it * TOK;
+
+      // S^T of this wavefront's blocks: token 32 blk + 8 (i / 4) + 4 kg + i % 4
+      floatx16 s[NB];
+  #pragma unroll
+      for (int blk = 0; blk < NB; ++blk) {
+  #pragma unroll
+        for (int i = 0; i < 16; ++i) s[blk][i] = 0.f;
+        const uint16_t* kp = Kt + ((tw * NB + blk) * 32 + c32) * kD;
+  #pragma unroll
+        for (int st = 0; st < 8; ++st) {
+          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kp + (((2 * st) ^ ksw) * 8));
+          s[blk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[blk], 0, 0, 0);
+        }
+      }
+
+      const bool masked = needs_mask(it);
+      if (masked) {
+  #pragma unroll
+        for (int blk = 0; blk < NB; ++blk)
+  #pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int j = j0 + (tw * NB + blk) * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
+            bool see = j < v1;
+            if (WINDOW) {
+              const int t = token_of(j);
+              see = see && t <= pos && (t < a.n_sink || t > pos - a.window);
+            }
+            s[blk][i] = see ? s[blk][i] : -INFINITY;
+          }
+      }
+
+      float mx = -INFINITY;
+  #pragma unroll
+      for (int blk = 0; blk < NB; ++blk)
+  #pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[blk][i]);
+      mx = pair_max(mx) * a.scale_log2;
+      if (__any(mx > m_run + kSlack)) {
+        const float mn = fmaxf(m_run, mx);
+        const float alpha = exp2_fast(m_run - mn);
+        m_run = mn;
+        l_run *= alpha;
+  #pragma unroll
+        for (int db = 0; db < 4; ++db) acc[db] *= alpha;
+      }
+
+      constexpr bool kThird = SPLITP && RW == 1;
+      bf16x8 ph[2 * NB], pl[SPLITP ? 2 * NB : 1], pt[kThird ? 2 * NB : 1];
+  #pragma unroll
+      for (int blk = 0; blk < NB; ++blk) {
+        float p[16];
+  #pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          p[i] = exp2_fast(fmaf(s[blk][i], a.scale_log2, -m_run));
+          l_run += p[i];
+        }
+  #pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          ph[2 * blk + m] = to_bf16x8(p + 8 * m);
+          if constexpr (SPLITP) pl[2 * blk + m] = next_bf16x8(p + 8 * m, ph[2 * blk + m]);
+          if constexpr (kThird) pt[2 * blk + m] = next_bf16x8(p + 8 * m, pl[2 * blk + m]);
+        }
+      }
+
+      // O^T += V^T P^T: slots 8 kg .. 8 kg + 7 of a multiplication are tokens
+      // 16 m + 4 kg + 0..3 and 16 m + 8 + 4 kg + 0..3, as this lane holds P.
+  #pragma unroll
+      for (int m = 0; m < 2 * NB; ++m) {
+        const uint16_t* vp = Vt + ((tw * NB) * 32 + 16 * m + 4 * kg + (a16 >> 2)) * kD + 4 * (a16 & 1);
+        const int lo0 = (2 * half16 + ((a16 >> 1) & 1)) ^ kg;
+  #pragma unroll
+        for (int db = 0; db < 4; ++db) {
+          const int hi4 = 4 * (db ^ (a16 >> 2));
+          const bf16x4 x = lds_read_tr(vp + (hi4 + lo0) * 8);
+          const bf16x4 y = lds_read_tr(vp + 8 * kD + (hi4 + (lo0 ^ 2)) * 8);
+          const bf16x8 vf = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, ph[m], acc[db], 0, 0, 0);
+          if constexpr (SPLITP)
+            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl[m], acc[db], 0, 0, 0);
+          if constexpr (kThird)
+            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pt[m], acc[db], 0, 0, 0);
+        }
+      }
+
+      // The other buffer was last read before the previous barrier.
+      if (it + 1 < n_tiles) put(it + 1);
+      if (it + 2 < n_tiles) issue(it + 2);
+      __syncthreads();
+    }
   }
   if (WINDOW && odd_rows)  // uniform; written before the last barrier
     attend_by_token(a, a.q + orow * kD, a.k + base, a.v + base, rs, kg, tw == 0 ? v0 : v1, v1, pos,
