@@ -273,12 +273,12 @@ void tile_attn_kernel(TileArgs a) {
 
       // S^T of this wavefront's blocks: token 32 blk + 8 (i / 4) + 4 kg + i % 4
       floatx16 s[NB];
-  #pragma unroll
+#pragma unroll
       for (int blk = 0; blk < NB; ++blk) {
-  #pragma unroll
+#pragma unroll
         for (int i = 0; i < 16; ++i) s[blk][i] = 0.f;
         const uint16_t* kp = Kt + ((tw * NB + blk) * 32 + c32) * kD;
-  #pragma unroll
+#pragma unroll
         for (int st = 0; st < 8; ++st) {
           const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kp + (((2 * st) ^ ksw) * 8));
           s[blk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[blk], 0, 0, 0);
@@ -287,9 +287,9 @@ void tile_attn_kernel(TileArgs a) {
 
       const bool masked = needs_mask(it);
       if (masked) {
-  #pragma unroll
+#pragma unroll
         for (int blk = 0; blk < NB; ++blk)
-  #pragma unroll
+#pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int j = j0 + (tw * NB + blk) * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
             bool see = j < v1;
@@ -302,9 +302,9 @@ void tile_attn_kernel(TileArgs a) {
       }
 
       float mx = -INFINITY;
-  #pragma unroll
+#pragma unroll
       for (int blk = 0; blk < NB; ++blk)
-  #pragma unroll
+#pragma unroll
         for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[blk][i]);
       mx = pair_max(mx) * a.scale_log2;
       if (__any(mx > m_run + kSlack)) {
@@ -312,21 +312,21 @@ void tile_attn_kernel(TileArgs a) {
         const float alpha = exp2_fast(m_run - mn);
         m_run = mn;
         l_run *= alpha;
-  #pragma unroll
+#pragma unroll
         for (int db = 0; db < 4; ++db) acc[db] *= alpha;
       }
 
       constexpr bool kThird = SPLITP && RW == 1;
       bf16x8 ph[2 * NB], pl[SPLITP ? 2 * NB : 1], pt[kThird ? 2 * NB : 1];
-  #pragma unroll
+#pragma unroll
       for (int blk = 0; blk < NB; ++blk) {
         float p[16];
-  #pragma unroll
+#pragma unroll
         for (int i = 0; i < 16; ++i) {
           p[i] = exp2_fast(fmaf(s[blk][i], a.scale_log2, -m_run));
           l_run += p[i];
         }
-  #pragma unroll
+#pragma unroll
         for (int m = 0; m < 2; ++m) {
           ph[2 * blk + m] = to_bf16x8(p + 8 * m);
           if constexpr (SPLITP) pl[2 * blk + m] = next_bf16x8(p + 8 * m, ph[2 * blk + m]);
@@ -336,11 +336,11 @@ void tile_attn_kernel(TileArgs a) {
 
       // O^T += V^T P^T: slots 8 kg .. 8 kg + 7 of a multiplication are tokens
       // 16 m + 4 kg + 0..3 and 16 m + 8 + 4 kg + 0..3, as this lane holds P.
-  #pragma unroll
+#pragma unroll
       for (int m = 0; m < 2 * NB; ++m) {
         const uint16_t* vp = Vt + ((tw * NB) * 32 + 16 * m + 4 * kg + (a16 >> 2)) * kD + 4 * (a16 & 1);
         const int lo0 = (2 * half16 + ((a16 >> 1) & 1)) ^ kg;
-  #pragma unroll
+#pragma unroll
         for (int db = 0; db < 4; ++db) {
           const int hi4 = 4 * (db ^ (a16 >> 2));
           const bf16x4 x = lds_read_tr(vp + (hi4 + lo0) * 8);
