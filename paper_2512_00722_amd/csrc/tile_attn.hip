@@ -6,8 +6,8 @@
 // One pass over the tokens with a running maximum and sum per row:
 //     m' = max(m, max_t s_t),  l' = l 2^(m-m') + sum_t 2^(s_t-m'),
 //     O' = O 2^(m-m') + sum_t 2^(s_t-m') v_t,     s_t = scale log2(e) q.k_t
-// Tiles of TOK tokens go through LDS (two buffers; the next tile's loads are in
-// flight in registers while this one is multiplied).  A wavefront owns 32 rows:
+// Tiles of TOK tokens are loaded straight into LDS, the next ones while this one is
+// multiplied.  A wavefront owns 32 rows:
 //  * S^T = K Q^T with v_mfma_f32_32x32x16_bf16 leaves a row's logits in one lane
 //    (and its partner 32 lanes on), so that the softmax needs one lane swap;
 //  * O^T += V^T P^T takes P from those registers as they are: the token order
@@ -67,18 +67,14 @@ __device__ __forceinline__ Range window_range(const TileArgs& a, int p0, int i0,
   return {s + hi - lo, s, lo - s};
 }
 
-// Two bf16 values: is one an infinity or a NaN?
-__device__ __forceinline__ bool odd2(uint32_t x) {
-  return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-}
-
-// The same token by token, for the rare rows that hold infinities or NaNs: those
-// that a query does not see are selected away.  A lane has the dimensions
-// 32 db + 8 e + 4 kg .. + 3 of its row, as the accumulators do.
-template <class TokenOf>
+// The same token by token, for the rare sums that hold infinities or NaNs: of rows that
+// a query does not see, they are selected away.  The wavefront's tokens are j0 .. j0 + run
+// - 1 and those `step` further on, up to j1.  A lane has the dimensions 32 db + 8 e + 4 kg
+// .. + 3 of its row, as the accumulators do.
+template <bool WINDOW, class TokenOf>
 __device__ __forceinline__ void attend_by_token(const TileArgs& a, const uint16_t* q,
                                                 const uint16_t* k, const uint16_t* v, int64_t rs,
-                                                int kg, int j0, int j1, int pos,
+                                                int kg, int j0, int j1, int run, int step, int pos,
                                                 TokenOf&& token_of, float& m_run, float& l_run,
                                                 floatx16 (&acc)[4]) {
   auto four = [](const uint16_t* p, float (&f)[4]) {
@@ -93,7 +89,8 @@ __device__ __forceinline__ void attend_by_token(const TileArgs& a, const uint16_
 #pragma unroll
   for (int db = 0; db < 4; ++db) acc[db] = 0.f;
 #pragma unroll 1
-  for (int j = j0; j < j1; ++j) {
+  for (int j = j0, left = run; j < j1; left = left == 1 ? run : left - 1,
+           j += left == run ? step - run + 1 : 1) {
     const int t = token_of(j);
     const int64_t off = (int64_t)t * rs + 4 * kg;
     float s = 0.f;
@@ -104,7 +101,7 @@ __device__ __forceinline__ void attend_by_token(const TileArgs& a, const uint16_
       four(k + off + 8 * e, y);
       for (int i = 0; i < 4; ++i) s = fmaf(x[i], y[i], s);
     }
-    const bool see = t <= pos && (t < a.n_sink || t > pos - a.window);
+    const bool see = !WINDOW || (t <= pos && (t < a.n_sink || t > pos - a.window));
     s = pair_sum(s) * a.scale_log2;
     s = see ? s : -INFINITY;
     const float mn = fmaxf(m_run, s);
@@ -122,6 +119,23 @@ __device__ __forceinline__ void attend_by_token(const TileArgs& a, const uint16_
   }
 }
 
+// s_waitcnt immediate (gfx9 encoding: vmcnt[3:0], expcnt[6:4], lgkmcnt[11:8], vmcnt[5:4]
+// in bits [15:14]) that waits for the vector-memory count only.
+constexpr int waitcnt_vm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) | (15 << 8); }
+
+// Global-to-LDS copy of 16 bytes per lane: lane l's bytes land at lds + 16 l (M0 holds
+// the wave-uniform base).  From inline assembly, as the compiler, which cannot tell the
+// stage being read from the one being filled, would wait for all pending loads
+// before every LDS read.  It has no output registers; the kernel does the waiting.
+// Nothing else in this file uses M0 (tests/test_isa_dense_cpu.py).
+__device__ __forceinline__ void load_to_lds(const void* g, const void* lds) {
+  const uint32_t base = (uint32_t)(uintptr_t)lds;
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(__builtin_amdgcn_readfirstlane(base)), "v"(g)
+               : "memory", "m0");
+}
+
 // RW x TW wavefronts: RW groups of 32 rows, TW parts of each tile's tokens.
 // WINDOW: masked rows of a sequence; else every row sees all tokens.  SPLITP:
 // weights as a bf16 pair (~2^-18 relative) for fp32 results, or with few rows, which
@@ -134,9 +148,8 @@ void tile_attn_kernel(TileArgs a) {
   constexpr int NT = RW * TW * 64;
   constexpr int ROWS = 32 * RW;
   constexpr int NB = TOK / (32 * TW);      // 32-token blocks of a wavefront
-  constexpr int LD = TOK * 16 / NT;        // 16-byte loads of a thread for K, and for V
+  constexpr int LD = TOK / 4 / (RW * TW);  // loads of a wavefront for K, and for V: 4 rows each
   __shared__ __align__(16) uint16_t lds[2][2][TOK * kD];
-  __shared__ int odd_rows;  // a masked tile holds an infinity or a NaN (see below)
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int rw = wave % RW, tw = wave / RW;
   const int c32 = lane & 31, kg = lane >> 5;
@@ -194,52 +207,47 @@ void tile_attn_kernel(TileArgs a) {
     const uint16_t* qp = a.q + orow * kD + 8 * kg;
 #pragma unroll
     for (int s = 0; s < 8; ++s) qf[s] = __builtin_bit_cast(bf16x8, ldg16(qp + 16 * s));
+    // Waited for here: in the loop the wait would cover the tiles' loads as well.
+#pragma unroll
+    for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(qf[s]));
   }
 
   const int64_t rs = (int64_t)a.H_kv * kD;
   const int64_t base = (int64_t)(lb / a.B) * a.stride_layer + (int64_t)b * a.stride_b + g * kD;
-  const uint16_t* kb = a.k + base + (tid & 15) * 8;
-  const uint16_t* vb = a.v + base + (tid & 15) * 8;
-
-  uint4 kr[LD], vr[LD];
   auto token_of = [&](int j) { return j + (j < rg.n_sink ? 0 : rg.shift); };
-  auto issue = [&](int it) {  // tokens past the range read its last one
-#pragma unroll
-    for (int p = 0; p < LD; ++p) {
-      const int j = min(v0 + it * TOK + (tid >> 4) + p * (NT / 16), v1 - 1);
-      const int64_t off = (int64_t)token_of(j) * rs;
-      kr[p] = ldg16(kb + off);
-      vr[p] = ldg16(vb + off);
-    }
+  // A load brings four rows, 16 bytes per lane, to where they are read from (swizzle);
+  // rows behind the range are its last one.  Tiles behind the last are loaded, and not
+  // read, so that no branch stands between the multiplications.
+  auto issue = [&](int it, int e) {
+    const int r0 = (wave * LD + e / 2) * 4, r = r0 + (lane >> 4);
+    const int j = min(v0 + it * TOK + r, v1 - 1);
+    const int64_t off = base + (int64_t)token_of(j) * rs + (((lane & 15) ^ swizzle(r)) * 8);
+    load_to_lds((e % 2 ? a.v : a.k) + off, &lds[it & 1][e % 2][r0 * kD]);
   };
-  // Tiles that every row sees whole need no mask (uniform).
-  auto needs_mask = [&](int it) {
-    const int j0 = v0 + it * TOK, jl = j0 + TOK - 1;
-    if (!WINDOW) return jl >= v1;
-    const int first = j0 < rg.n_sink ? rg.n_sink + rg.shift : token_of(j0);  // behind the sinks
-    return jl >= v1 || token_of(jl) > p0 + i0 ||
-           (jl >= rg.n_sink && first <= p0 + i1 - a.window);
-  };
-  auto put = [&](int it) {
-    const int buf = it & 1;
-#pragma unroll
-    for (int p = 0; p < LD; ++p) {
-      const int r = (tid >> 4) + p * (NT / 16);
-      const int o = r * kD + (((tid & 15) ^ swizzle(r)) * 8);
-      *reinterpret_cast<uint4*>(&lds[buf][0][o]) = kr[p];
-      *reinterpret_cast<uint4*>(&lds[buf][1][o]) = vr[p];
+
+  // Tiles that every row sees whole need no mask: those before `clear`, but for the ones
+  // on the window's edge, edge0 .. edge1 - 1.
+  int clear, edge0 = 0, edge1 = 0;
+  {
+    int last = v1 - 1;  // the last token that the first query sees
+    if (WINDOW) {
+      const int p = p0 + i0;
+      last = min(last, p - rg.shift >= rg.n_sink ? p - rg.shift : min(p, rg.n_sink - 1));
+      const int out = p0 + i1 - a.window - rg.shift;  // the last one the last does not see
+      if (rg.n_sink <= out) {
+        edge0 = max(rg.n_sink - v0, 0) / TOK;
+        edge1 = out >= v0 ? (out - v0) / TOK + 1 : 0;
+      }
     }
-    // A weight of 0 does not keep an infinity or a NaN of a row that is masked
-    // for this query but not for another out of the sums (0 x NaN): where a
-    // masked tile holds one, everything is done again without the matrix cores.
-    if (WINDOW && needs_mask(it)) {
-      bool odd = false;
-#pragma unroll
-      for (int p = 0; p < LD; ++p)
-        odd = odd || odd2(vr[p].x) || odd2(vr[p].y) || odd2(vr[p].z) || odd2(vr[p].w);
-      if (odd) odd_rows = 1;
-    }
-  };
+    clear = max(last + 1 - v0, 0) / TOK;
+  }
+  // This row sees tokens 0 .. sinks - 1 and lo .. lo + n - 1 of the range.
+  int sinks = 0, lo = 0, n = v1;
+  if (WINDOW) {
+    sinks = min(min(rg.n_sink, pos + 1), v1);
+    lo = max(rg.n_sink, pos - a.window + 1 - rg.shift);
+    n = max(min(pos + 1 - rg.shift, v1) - lo, 0);
+  }
 
   float m_run = kNoMax, l_run = 0.f;
   floatx16 acc[4];  // O^T[32 db + 8 (i / 4) + 4 kg + i % 4][row]
@@ -252,117 +260,118 @@ void tile_attn_kernel(TileArgs a) {
   const int ksw = kg ^ swizzle(c32);
   const int a16 = lane & 15, half16 = (lane >> 4) & 1;
 
-  if (WINDOW) {
-    if (tid == 0) odd_rows = 0;
+  // Each wavefront waits for its own loads before the barrier in front of their use.
+  if (n_tiles > 0) {
+#pragma unroll
+    for (int e = 0; e < 2 * LD; ++e) issue(0, e);
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
     __syncthreads();
   }
-  if (n_tiles > 0) {
-    issue(0);
-    put(0);
-    // Used here, and inside a branch that no way into the loop leaves out, as the tiles
-    // would otherwise wait for them, and with them for the loads in flight.
+
+  for (int it = 0; it < n_tiles; ++it) {
+    const uint16_t* Kt = lds[it & 1][0];
+    const uint16_t* Vt = lds[it & 1][1];
+
+    // S^T of this wavefront's blocks: token 32 blk + 8 (i / 4) + 4 kg + i % 4.  Between
+    // the products the next tile's loads, into the stage that was last read before the
+    // previous barrier.
+    floatx16 s[NB];
 #pragma unroll
-    for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(qf[s]));
-    if (n_tiles > 1) issue(1);
-    __syncthreads();
-
-    for (int it = 0; it < n_tiles; ++it) {
-      const uint16_t* Kt = lds[it & 1][0];
-      const uint16_t* Vt = lds[it & 1][1];
-      const int j0 = v0 + it * TOK;
-
-      // S^T of this wavefront's blocks: token 32 blk + 8 (i / 4) + 4 kg + i % 4
-      floatx16 s[NB];
+    for (int blk = 0; blk < NB; ++blk) s[blk] = 0.f;
+#pragma unroll
+    for (int st = 0; st < 8; ++st) {
 #pragma unroll
       for (int blk = 0; blk < NB; ++blk) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[blk][i] = 0.f;
         const uint16_t* kp = Kt + ((tw * NB + blk) * 32 + c32) * kD;
-#pragma unroll
-        for (int st = 0; st < 8; ++st) {
-          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kp + (((2 * st) ^ ksw) * 8));
-          s[blk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[blk], 0, 0, 0);
-        }
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kp + (((2 * st) ^ ksw) * 8));
+        s[blk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[blk], 0, 0, 0);
       }
-
-      const bool masked = needs_mask(it);
-      if (masked) {
 #pragma unroll
-        for (int blk = 0; blk < NB; ++blk)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int j = j0 + (tw * NB + blk) * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
-            bool see = j < v1;
-            if (WINDOW) {
-              const int t = token_of(j);
-              see = see && t <= pos && (t < a.n_sink || t > pos - a.window);
-            }
-            s[blk][i] = see ? s[blk][i] : -INFINITY;
-          }
-      }
+      for (int e = st * LD / 4; e < (st + 1) * LD / 4; ++e) issue(it + 1, e);
+    }
 
-      float mx = -INFINITY;
+    if (it >= clear || (WINDOW && it >= edge0 && it < edge1)) {
 #pragma unroll
       for (int blk = 0; blk < NB; ++blk)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[blk][i]);
-      mx = pair_max(mx) * a.scale_log2;
-      if (__any(mx > m_run + kSlack)) {
-        const float mn = fmaxf(m_run, mx);
-        const float alpha = exp2_fast(m_run - mn);
-        m_run = mn;
-        l_run *= alpha;
-#pragma unroll
-        for (int db = 0; db < 4; ++db) acc[db] *= alpha;
-      }
-
-      constexpr bool kThird = SPLITP && RW == 1;
-      bf16x8 ph[2 * NB], pl[SPLITP ? 2 * NB : 1], pt[kThird ? 2 * NB : 1];
-#pragma unroll
-      for (int blk = 0; blk < NB; ++blk) {
-        float p[16];
-#pragma unroll
         for (int i = 0; i < 16; ++i) {
-          p[i] = exp2_fast(fmaf(s[blk][i], a.scale_log2, -m_run));
-          l_run += p[i];
+          const int j = v0 + it * TOK + (tw * NB + blk) * 32 + 8 * (i >> 2) + 4 * kg + (i & 3);
+          bool see = (uint32_t)(j - lo) < (uint32_t)n;
+          if (WINDOW) see = see | (j < sinks);
+          s[blk][i] = see ? s[blk][i] : -INFINITY;
+          if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // few conditions at a time
         }
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          ph[2 * blk + m] = to_bf16x8(p + 8 * m);
-          if constexpr (SPLITP) pl[2 * blk + m] = next_bf16x8(p + 8 * m, ph[2 * blk + m]);
-          if constexpr (kThird) pt[2 * blk + m] = next_bf16x8(p + 8 * m, pl[2 * blk + m]);
-        }
-      }
-
-      // O^T += V^T P^T: slots 8 kg .. 8 kg + 7 of a multiplication are tokens
-      // 16 m + 4 kg + 0..3 and 16 m + 8 + 4 kg + 0..3, as this lane holds P.
-#pragma unroll
-      for (int m = 0; m < 2 * NB; ++m) {
-        const uint16_t* vp = Vt + ((tw * NB) * 32 + 16 * m + 4 * kg + (a16 >> 2)) * kD + 4 * (a16 & 1);
-        const int lo0 = (2 * half16 + ((a16 >> 1) & 1)) ^ kg;
-#pragma unroll
-        for (int db = 0; db < 4; ++db) {
-          const int hi4 = 4 * (db ^ (a16 >> 2));
-          const bf16x4 x = lds_read_tr(vp + (hi4 + lo0) * 8);
-          const bf16x4 y = lds_read_tr(vp + 8 * kD + (hi4 + (lo0 ^ 2)) * 8);
-          const bf16x8 vf = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, ph[m], acc[db], 0, 0, 0);
-          if constexpr (SPLITP)
-            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl[m], acc[db], 0, 0, 0);
-          if constexpr (kThird)
-            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pt[m], acc[db], 0, 0, 0);
-        }
-      }
-
-      // The other buffer was last read before the previous barrier.
-      if (it + 1 < n_tiles) put(it + 1);
-      if (it + 2 < n_tiles) issue(it + 2);
-      __syncthreads();
     }
+
+    float mx = -INFINITY;
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[blk][i]);
+    mx = pair_max(mx) * a.scale_log2;
+    if (__any(mx > m_run + kSlack)) {
+      const float mn = fmaxf(m_run, mx);
+      const float alpha = exp2_fast(m_run - mn);
+      m_run = mn;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < 4; ++db) acc[db] *= alpha;
+    }
+
+    constexpr bool kThird = SPLITP && RW == 1;
+    bf16x8 ph[2 * NB], pl[SPLITP ? 2 * NB : 1], pt[kThird ? 2 * NB : 1];
+#pragma unroll
+    for (int blk = 0; blk < NB; ++blk) {
+      float p[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[i] = exp2_fast(fmaf(s[blk][i], a.scale_log2, -m_run));
+        l_run += p[i];
+      }
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        ph[2 * blk + m] = to_bf16x8(p + 8 * m);
+        if constexpr (SPLITP) pl[2 * blk + m] = next_bf16x8(p + 8 * m, ph[2 * blk + m]);
+        if constexpr (kThird) pt[2 * blk + m] = next_bf16x8(p + 8 * m, pl[2 * blk + m]);
+      }
+    }
+
+    // O^T += V^T P^T: slots 8 kg .. 8 kg + 7 of a multiplication are tokens
+    // 16 m + 4 kg + 0..3 and 16 m + 8 + 4 kg + 0..3, as this lane holds P.
+#pragma unroll
+    for (int m = 0; m < 2 * NB; ++m) {
+      const uint16_t* vp = Vt + (tw * NB * 32 + 16 * m + 4 * kg + (a16 >> 2)) * kD + 4 * (a16 & 1);
+      const int lo0 = (2 * half16 + ((a16 >> 1) & 1)) ^ kg;
+#pragma unroll
+      for (int db = 0; db < 4; ++db) {
+        const int hi4 = 4 * (db ^ (a16 >> 2));
+        const bf16x4 x = lds_read_tr(vp + (hi4 + lo0) * 8);
+        const bf16x4 y = lds_read_tr(vp + 8 * kD + (hi4 + (lo0 ^ 2)) * 8);
+        const bf16x8 vf = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, ph[m], acc[db], 0, 0, 0);
+        if constexpr (SPLITP)
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pl[m], acc[db], 0, 0, 0);
+        if constexpr (kThird)
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pt[m], acc[db], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __syncthreads();
   }
-  if (WINDOW && odd_rows)  // uniform; written before the last barrier
-    attend_by_token(a, a.q + orow * kD, a.k + base, a.v + base, rs, kg, tw == 0 ? v0 : v1, v1, pos,
-                    token_of, m_run, l_run, acc);
+  // Where an infinity or a NaN got into the sums, they are taken again without the matrix
+  // cores: a weight of 0 does not keep one of a row that this query does not see out of
+  // them (0 x NaN), nor is an infinity of one that it sees the product with a weight's
+  // parts.
+  {
+    float odd = 0.f;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) odd = fmaf(acc[db][i], 0.f, odd);
+    if (__any(odd != odd))
+      attend_by_token<WINDOW>(a, a.q + orow * kD, a.k + base, a.v + base, rs, kg, v0 + tw * NB * 32, v1,
+                      NB * 32, TOK, pos, token_of, m_run, l_run, acc);
+  }
   l_run = pair_sum(l_run);
 
   // The parts of a row group, joined by its first wavefront: accumulators stand
