@@ -6,8 +6,15 @@
 // One pass over the tokens with a running maximum and sum per row:
 //     m' = max(m, max_t s_t),  l' = l 2^(m-m') + sum_t 2^(s_t-m'),
 //     O' = O 2^(m-m') + sum_t 2^(s_t-m') v_t,     s_t = scale log2(e) q.k_t
-// Tiles of TOK tokens are loaded straight into LDS, the next ones while this one is
-// multiplied.  A wavefront owns 32 rows:
+// Tiles of TOK tokens go through LDS, two stages of them: the next tile's loads go
+// there directly, issued between this one's products.  (By way of registers, their
+// issue and the LDS writes took 1200 of a tile's 3200 cycles with 64 rows, as a
+// wavefront waits where the path is full: 2 x 4096 tokens 294 us against 271, 512
+// tokens 17 against 15.)  The largest chunks reach 1.0 PFLOP/s of the 1.2 of a library
+// product of bf16 (its limit is power: with zeros it reaches 1.7, and the chunks lose
+// 10 % of their time).  More stages, products of the next tile beside this one's
+// exponentials, and wavefronts half a tile apart changed that by 2 % at most.
+// A wavefront owns 32 rows:
 //  * S^T = K Q^T with v_mfma_f32_32x32x16_bf16 leaves a row's logits in one lane
 //    (and its partner 32 lanes on), so that the softmax needs one lane swap;
 //  * O^T += V^T P^T takes P from those registers as they are: the token order
@@ -539,21 +546,23 @@ hipError_t launch_tiles(const TilePlan& p, const TileArgs& a, hipStream_t s) {
 // shares the CU and covers them).  A further split costs a launch and the rows'
 // partial results, written and read once each.
 // Measured (us, rows / splits; 32 query and 8 KV heads):
-//   8192 tokens                256/1 554  128/1 577
-//   8192 tokens, window 1024   128/1 176  256/1 200   64/1 219
-//   1024 tokens                 64/1  28  128/1  33  256/1  40   64/2  47
-//   512 of 8192 tokens         256/4  88  128/4  93   64/2 111   64/1 147
-//   128 of 32768 tokens       256/16  88 128/16  93   64/8 110   64/1 556
-//   8 x 16 of 4096 tokens       64/4  34   32/2  42   64/2  48
+//   8192 tokens                256/1 531  128/1 556   64/1 664
+//   8192 tokens, window 1024   128/1 164  256/1 179   64/1 194
+//   2048 tokens                128/1  56   64/1  58  256/1  61  128/2  86
+//   1024 tokens                 64/1  23  128/1  27  256/1  34   64/2  44
+//   512 of 8192 tokens         256/4  83  128/4  89   64/2  99   64/1 112
+//   128 of 32768 tokens       256/16  84 128/16  89   64/8  99   64/1 414
+//   32 of 16384 tokens         64/16  28 128/32  28   32/8  34   64/8  39
+//   8 x 16 of 4096 tokens       64/4  33   32/2  35   64/2  40
 TilePlan window_plan(const DenseDims& d) {
   struct Kind {
     int rows, tok;
     double full, alone, ends, edge;
   };
-  constexpr Kind kKinds[4] = {{256, 64, 2.05, 1.8, 2.6, 4.},
-                              {128, 64, 1.08, 1.46, 2.3, 1.},
-                              {64, 64, 0.72, 1.09, 2., 0.},
-                              {32, 128, 1.5, 1.5, 2., 0.}};
+  constexpr Kind kKinds[4] = {{256, 64, 1.94, 1.44, 3.2, 2.},
+                              {128, 64, 1.02, 1.25, 3., 0.},
+                              {64, 64, 0.62, 0.81, 3., 0.},
+                              {32, 128, 1.2, 1.2, 2., 0.}};
   constexpr double kMergeLaunch = 5., kMergeBytes = 4e6;  // us, bytes / us
   const int64_t units = (int64_t)d.n_layers * d.B * d.H_kv, rows = (int64_t)d.T * d.G;
   const int64_t cap = d.L_cap;
