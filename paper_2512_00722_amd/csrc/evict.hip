@@ -31,6 +31,7 @@ namespace {
 struct EvictKernelArgs {
   EvictArgs x;
   int4* head;            // [B] head_of each sequence
+  int32_t* pos;          // [B] x.pos, which may be the counts' memory
   int2* filled;          // [sets]: slots filled, of them from the cache
   int32_t* dst;          // [sets][L_cap] slots filled, ascending
   int32_t* src;          // [sets][L_cap] kept slots at C' or above, ascending
@@ -55,13 +56,17 @@ __global__ __launch_bounds__(256) void evict_counts_kernel(EvictKernelArgs a) {
   if (b >= a.B) return;
   const int4 hd = head_of(a, b);
   a.head[b] = hd;
+  a.pos[b] = a.x.pos[b];
   a.x.counts[b] = hd.z;
 }
 __device__ __forceinline__ int4 plan_head(const EvictKernelArgs& a, int set, bool move) {
   const int b = (set / a.n_sets) % a.B;
   if (move) return a.head[b];
   const int4 hd = head_of(a, b);
-  if (set == b * a.n_sets && threadIdx.x == 0) a.head[b] = hd;
+  if (set == b * a.n_sets && threadIdx.x == 0) {
+    a.head[b] = hd;
+    a.pos[b] = a.x.pos[b];
+  }
   return hd;
 }
 
@@ -126,7 +131,7 @@ __device__ __forceinline__ void move_rows(const EvictKernelArgs& a, int set, int
     *reinterpret_cast<uint4*>(vc + d * rs + 8 * piece) = vv;
     if (piece == 0) {
       w[d] = held ? w[x] : 0.f;
-      tok[d] = held ? tok[x] : a.x.pos[b] + x;
+      tok[d] = held ? tok[x] : a.pos[b] + x;
     }
   }
 }
@@ -184,7 +189,7 @@ __global__ __launch_bounds__(NT) void evict_plan_kernel(EvictKernelArgs a) {
   const int4 hd = plan_head(a, set, MOVE);
   const int c = hd.x, E = hd.y, after = hd.z, taken = after - E;
   const int64_t recent_from =
-      (int64_t)a.x.pos[b] + (a.x.n_new ? clampi(a.x.n_new[b], 0, a.T) : a.T) - a.n_recent;
+      (int64_t)(MOVE ? a.pos : a.x.pos)[b] + (a.x.n_new ? clampi(a.x.n_new[b], 0, a.T) : a.T) - a.n_recent;
   int32_t* dst = a.dst + (size_t)set * a.L_cap;
   int32_t* src = a.src + (size_t)set * a.L_cap;
 
@@ -412,6 +417,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictKernelArgs a) {
 }
 
 size_t head_bytes(const DenseDims& d) { return align_up(sizeof(int4) * (size_t)d.B); }
+size_t pos_bytes(const DenseDims& d) { return align_up(sizeof(int32_t) * (size_t)d.B); }
 size_t filled_bytes(int64_t sets) { return align_up(sizeof(int2) * (size_t)sets); }
 size_t list_bytes(const DenseDims& d, int64_t sets) {
   return align_up(sizeof(int32_t) * (size_t)sets * d.L_cap);
@@ -436,7 +442,7 @@ constexpr int kPlanSlots = 32768;  // what the widest of them holds
 
 size_t evict_ws_bytes(const DenseDims& d) {
   const int64_t sets = (int64_t)d.n_layers * d.B * d.n_sets;
-  return head_bytes(d) + filled_bytes(sets) + 2 * list_bytes(d, sets);
+  return head_bytes(d) + pos_bytes(d) + filled_bytes(sets) + 2 * list_bytes(d, sets);
 }
 
 hipError_t launch_evict(const DenseDims& d, const EvictArgs& x, void* ws, hipStream_t s) {
@@ -444,12 +450,14 @@ hipError_t launch_evict(const DenseDims& d, const EvictArgs& x, void* ws, hipStr
   char* w = static_cast<char*>(ws);
   int4* head = reinterpret_cast<int4*>(w);
   w += head_bytes(d);
+  int32_t* pos = reinterpret_cast<int32_t*>(w);
+  w += pos_bytes(d);
   int2* filled = reinterpret_cast<int2*>(w);
   w += filled_bytes(sets);
   int32_t* dst = reinterpret_cast<int32_t*>(w);
   int32_t* src = reinterpret_cast<int32_t*>(w + list_bytes(d, sets));
   const int blocks = (int)(sets >= 2048 ? 1 : 2048 / sets);
-  const EvictKernelArgs a{x, head, filled, dst, src, d.kv_stride_layer, d.kv_stride_b, d.B,
+  const EvictKernelArgs a{x, head, pos, filled, dst, src, d.kv_stride_layer, d.kv_stride_b, d.B,
                           d.n_sets, d.H_kv, d.L_cap, d.T, d.n_recent, d.n_sink, blocks};
   const bool in_plan = d.T > 0 && d.T <= kMoveInPlan && d.L_cap <= kPlanSlots;
   if (in_plan) {

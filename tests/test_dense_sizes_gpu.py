@@ -206,6 +206,21 @@ def test_evict(dev, case):
         assert same_bits(got, ref), nm
 
 
+@pytest.mark.parametrize("T", [2, 40])
+def test_evict_positions_in_the_counts(dev, T):
+    """Until a cache is full, the tokens seen are the rows held: one tensor for both."""
+    n, B, H_kv, cap = 2, 3, 2, 100
+    counts = [90, 100, 0]
+    x = bounded(n, B, H_kv, H_kv, cap, 231, dev)
+    k_new, v_new = (normal((n, B, T, H_kv, D), 233 + i, dev) for i in range(2))
+    *want, after = evict_reference(x, H_kv, counts, [cap] * B, counts, [T] * B, k_new, v_new, 8, 2)
+    c = i32(counts, dev)
+    spec.evict(*x, c, i32([cap] * B, dev), c, k_new=k_new, v_new=v_new, n_recent=8, n_sink=2)
+    assert c.tolist() == after
+    for got, ref, nm in zip(x, want, ("K", "V", "weights", "tokens")):
+        assert same_bits(got, ref), nm
+
+
 # ------------------------------------------------------------------ offsets past 32 bits
 
 def test_large_offsets(dev):
