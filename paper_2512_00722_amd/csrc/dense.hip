@@ -249,7 +249,8 @@ hipError_t launch_decode(const DenseDims& d, const DecodeArgs& a, int hb, size_t
   const dim3 grid((unsigned)blocks), block(kW * 64);
   if (hb == 1) decode_kernel<1, KEEP, false><<<grid, block, lds, s>>>(a);
   else if (hb == 2) decode_kernel<2, KEEP, false><<<grid, block, 2 * lds, s>>>(a);
-  else if constexpr (KEEP == kKeepWeights) decode_kernel<4, KEEP, true><<<grid, block, 4 * lds, s>>>(a);
+  else if constexpr (KEEP == kKeepWeights)
+    decode_kernel<4, KEEP, true><<<grid, block, 4 * lds, s>>>(a);
   else decode_kernel<4, KEEP, false><<<grid, block, 4 * lds, s>>>(a);
   return hipGetLastError();
 }

@@ -189,7 +189,8 @@ __global__ __launch_bounds__(NT) void evict_plan_kernel(EvictKernelArgs a) {
   const int4 hd = plan_head(a, set, MOVE);
   const int c = hd.x, E = hd.y, after = hd.z, taken = after - E;
   const int64_t recent_from =
-      (int64_t)(MOVE ? a.pos : a.x.pos)[b] + (a.x.n_new ? clampi(a.x.n_new[b], 0, a.T) : a.T) - a.n_recent;
+      (int64_t)(MOVE ? a.pos : a.x.pos)[b] +
+      (a.x.n_new ? clampi(a.x.n_new[b], 0, a.T) : a.T) - a.n_recent;
   int32_t* dst = a.dst + (size_t)set * a.L_cap;
   int32_t* src = a.src + (size_t)set * a.L_cap;
 
@@ -222,8 +223,9 @@ __global__ __launch_bounds__(NT) void evict_plan_kernel(EvictKernelArgs a) {
     // slots that hold nothing rank below every key (the least is that of -inf)
 #pragma unroll
     for (int i = 0; i < PER; ++i)
-      key[i] = PER * tid + i < c ? rank_key(wv[i / 4][i % 4], tv[i / 4][i % 4], recent_from, a.n_sink)
-                                 : 0u;
+      key[i] = PER * tid + i < c
+                   ? rank_key(wv[i / 4][i % 4], tv[i / 4][i % 4], recent_from, a.n_sink)
+                   : 0u;
   }
 
   uint32_t cut = 0;   // kept: the keys above it, and

@@ -6,7 +6,7 @@
 // One pass over the tokens with a running maximum and sum per row:
 //     m' = max(m, max_t s_t),  l' = l 2^(m-m') + sum_t 2^(s_t-m'),
 //     O' = O 2^(m-m') + sum_t 2^(s_t-m') v_t,     s_t = scale log2(e) q.k_t
-// Tiles of TOK tokens go through LDS, two stages of them: the next tile's loads go
+// Tiles of TOK tokens go through two or three stages in LDS: later tiles' loads go
 // there directly, issued between this one's products.  (By way of registers, their
 // issue and the LDS writes took 1200 of a tile's 3200 cycles with 64 rows, as a
 // wavefront waits where the path is full: 2 x 4096 tokens 294 us against 271, 512
@@ -121,7 +121,8 @@ __device__ __forceinline__ void attend_by_token(const TileArgs& a, const uint16_
       four(v + off + 8 * e, y);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        acc[e >> 2][4 * (e & 3) + i] = acc[e >> 2][4 * (e & 3) + i] * alpha + (see ? p * y[i] : 0.f);
+        acc[e >> 2][4 * (e & 3) + i] =
+            acc[e >> 2][4 * (e & 3) + i] * alpha + (see ? p * y[i] : 0.f);
     }
   }
 }
@@ -152,23 +153,25 @@ __device__ __forceinline__ void load_to_lds(const void* g, const void* lds) {
 template <int RW, int TW, int TOK, bool WINDOW, bool SPLITP>
 __global__ __launch_bounds__(RW* TW * 64) __attribute__((amdgpu_waves_per_eu(TOK == 64 ? 2 : 1)))
 void tile_attn_kernel(TileArgs a) {
-  constexpr int NT = RW * TW * 64;
   constexpr int ROWS = 32 * RW;
   constexpr int NB = TOK / (32 * TW);      // 32-token blocks of a wavefront
   constexpr int LD = TOK / 4 / (RW * TW);  // loads of a wavefront for K, and for V: 4 rows each
-  __shared__ __align__(16) uint16_t lds[2][2][TOK * kD];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // Tiles in LDS: one workgroup of eight wavefronts is alone on its CU, with room for a
+  // third (2 x 4096 tokens not in the caches: 302 us, with two 307).
+  constexpr int STAGES = RW * TW == 8 ? 3 : 2;
+  __shared__ __align__(16) uint16_t lds[STAGES][2][TOK * kD];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int rw = wave % RW, tw = wave / RW;
   const int c32 = lane & 31, kg = lane >> 5;
   int block = blockIdx.x;
   if (!WINDOW) {  // own tokens: memory-bound work beside that of the matrix cores
     if (block < a.own_blocks) {
       constexpr int W = RW * TW;
-      static_assert(W * kTileElems <= 4 * TOK * kD, "the tiles' LDS holds the wavefronts' V tiles");
+      static_assert(W * kTileElems <= STAGES * 2 * TOK * kD, "room for the wavefronts' V tiles");
       __shared__ float2 ml[W][16];
       decode_block<W, 1, kKeepNone>(a.own, block,
-                                 reinterpret_cast<uint16_t(*)[kTileElems]>(&lds[0][0][0]), ml,
-                                 nullptr);
+                                    reinterpret_cast<uint16_t(*)[kTileElems]>(&lds[0][0][0]), ml,
+                                    nullptr);
       return;
     }
     block -= a.own_blocks;
@@ -225,11 +228,11 @@ void tile_attn_kernel(TileArgs a) {
   // A load brings four rows, 16 bytes per lane, to where they are read from (swizzle);
   // rows behind the range are its last one.  Tiles behind the last are loaded, and not
   // read, so that no branch stands between the multiplications.
-  auto issue = [&](int it, int e) {
+  auto issue = [&](int it, int stage, int e) {
     const int r0 = (wave * LD + e / 2) * 4, r = r0 + (lane >> 4);
     const int j = min(v0 + it * TOK + r, v1 - 1);
     const int64_t off = base + (int64_t)token_of(j) * rs + (((lane & 15) ^ swizzle(r)) * 8);
-    load_to_lds((e % 2 ? a.v : a.k) + off, &lds[it & 1][e % 2][r0 * kD]);
+    load_to_lds((e % 2 ? a.v : a.k) + off, &lds[stage][e % 2][r0 * kD]);
   };
 
   // Tiles that every row sees whole need no mask: those before `clear`, but for the ones
@@ -267,20 +270,25 @@ void tile_attn_kernel(TileArgs a) {
   const int ksw = kg ^ swizzle(c32);
   const int a16 = lane & 15, half16 = (lane >> 4) & 1;
 
-  // Each wavefront waits for its own loads before the barrier in front of their use.
+  // Each wavefront waits for its own loads of a tile, those of later ones being in flight,
+  // before the barrier in front of its use.
+  constexpr int kWait = waitcnt_vm((STAGES - 2) * 2 * LD);
   if (n_tiles > 0) {
 #pragma unroll
-    for (int e = 0; e < 2 * LD; ++e) issue(0, e);
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    for (int t = 0; t < STAGES - 1; ++t)
+#pragma unroll
+      for (int e = 0; e < 2 * LD; ++e) issue(t, t, e);
+    __builtin_amdgcn_s_waitcnt(kWait);
     __syncthreads();
   }
 
+  int now = 0, then = STAGES - 1;  // stages of this tile, and of the one that is requested
   for (int it = 0; it < n_tiles; ++it) {
-    const uint16_t* Kt = lds[it & 1][0];
-    const uint16_t* Vt = lds[it & 1][1];
+    const uint16_t* Kt = lds[now][0];
+    const uint16_t* Vt = lds[now][1];
 
     // S^T of this wavefront's blocks: token 32 blk + 8 (i / 4) + 4 kg + i % 4.  Between
-    // the products the next tile's loads, into the stage that was last read before the
+    // the products a later tile's loads, into the stage that was last read before the
     // previous barrier.
     floatx16 s[NB];
 #pragma unroll
@@ -294,7 +302,7 @@ void tile_attn_kernel(TileArgs a) {
         s[blk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[blk], 0, 0, 0);
       }
 #pragma unroll
-      for (int e = st * LD / 4; e < (st + 1) * LD / 4; ++e) issue(it + 1, e);
+      for (int e = st * LD / 4; e < (st + 1) * LD / 4; ++e) issue(it + STAGES - 1, then, e);
     }
 
     if (it >= clear || (WINDOW && it >= edge0 && it < edge1)) {
@@ -362,9 +370,13 @@ void tile_attn_kernel(TileArgs a) {
           acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pt[m], acc[db], 0, 0, 0);
       }
     }
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    __builtin_amdgcn_s_waitcnt(kWait);
     __syncthreads();
+    now = now == STAGES - 1 ? 0 : now + 1;
+    then = then == STAGES - 1 ? 0 : then + 1;
   }
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));  // loads past the last tile, before LDS is
+  __syncthreads();                            // used anew or given back
   // Where an infinity or a NaN got into the sums, they are taken again without the matrix
   // cores: a weight of 0 does not keep one of a row that this query does not see out of
   // them (0 x NaN), nor is an infinity of one that it sees the product with a weight's
@@ -376,8 +388,9 @@ void tile_attn_kernel(TileArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) odd = fmaf(acc[db][i], 0.f, odd);
     if (__any(odd != odd))
-      attend_by_token<WINDOW>(a, a.q + orow * kD, a.k + base, a.v + base, rs, kg, v0 + tw * NB * 32, v1,
-                      NB * 32, TOK, pos, token_of, m_run, l_run, acc);
+      attend_by_token<WINDOW>(a, a.q + orow * kD, a.k + base, a.v + base, rs, kg,
+                              v0 + tw * NB * 32, v1, NB * 32, TOK, pos, token_of, m_run, l_run,
+                              acc);
   }
   l_run = pair_sum(l_run);
 
@@ -491,7 +504,8 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(TileArgs a, int rows_
   const int g = h / a.G;
   const int r = b * a.G + (h - g * a.G);
   const size_t part = ((size_t)layer * a.H_kv + g) * a.n_rt + r / rows_per_tile;
-  const Join j = join_parts<S>(a.n_split + a.own.n_split, [&](int s, const float2*& ml, const float*& acc) {
+  const Join j = join_parts<S>(a.n_split + a.own.n_split, [&](int s, const float2*& ml,
+                                                              const float*& acc) {
     const bool pre = s < a.n_split;
     const size_t prow = pre ? (part * a.n_split + s) * rows_per_tile + r % rows_per_tile
                             : ((size_t)lb * a.own.n_split + (s - a.n_split)) * a.H_q + h;
@@ -567,7 +581,8 @@ TilePlan window_plan(const DenseDims& d) {
   const int64_t units = (int64_t)d.n_layers * d.B * d.H_kv, rows = (int64_t)d.T * d.G;
   const int64_t cap = d.L_cap;
   // mean over the query tokens i of min(window, L_cap - T + i + 1)
-  const double before = cap > d.T ? (double)(cap - d.T) : 0., w = d.window < cap ? d.window : (double)cap;
+  const double before = cap > d.T ? (double)(cap - d.T) : 0.;
+  const double w = d.window < cap ? (double)d.window : (double)cap;
   const double mean = w <= before ? w
                       : w >= cap  ? before + 0.5 * d.T
                                   : w - 0.5 * (w - before) * (w - before) / d.T;
@@ -579,7 +594,8 @@ TilePlan window_plan(const DenseDims& d) {
     const int64_t span = (k.rows - 2) / d.G + 1;
     int64_t most = (int64_t)d.window + d.n_sink + span;
     if (most > cap) most = cap;
-    const double avg = mean + 0.5 * span + d.n_sink < most ? mean + 0.5 * span + d.n_sink : (double)most;
+    double avg = mean + 0.5 * span + d.n_sink;
+    if (avg > most) avg = (double)most;
     for (int64_t n = 1; n == 1 || n <= (most + kMinSplit - 1) / kMinSplit; n *= 2) {
       split_tokens(p, most, n);
       const int64_t wgs = units * p.n_rt * p.n_split;
@@ -590,7 +606,8 @@ TilePlan window_plan(const DenseDims& d) {
       double t = (double)((wgs + kCUs - 1) / kCUs) * work * k.full;
       if (t < longest * k.alone) t = longest * k.alone;
       if (p.n_split > 1)
-        t += kMergeLaunch + (double)units * (double)rows * p.n_split * (2 * 4 * (kD + 2)) / kMergeBytes;
+        t += kMergeLaunch +
+             (double)units * (double)rows * p.n_split * (2 * 4 * (kD + 2)) / kMergeBytes;
       if (best.rows == 0 || t < least) {
         best = p;
         least = t;
