@@ -47,7 +47,8 @@ struct TileArgs {
   int n_units, n_rt, n_split, split_tok;
   float scale_log2;
   DecodeArgs own;         // prefix: the sequences' own tokens, by
-  int own_blocks;         // the first workgroups of the launch
+  int own_blocks;         // the first workgroups of the launch,
+  int own_hb;             // one or four column groups each
 };
 
 // The value of the lane 32 on (each row lives in two lanes).
@@ -156,9 +157,11 @@ void tile_attn_kernel(TileArgs a) {
   constexpr int ROWS = 32 * RW;
   constexpr int NB = TOK / (32 * TW);      // 32-token blocks of a wavefront
   constexpr int LD = TOK / 4 / (RW * TW);  // loads of a wavefront for K, and for V: 4 rows each
-  // Tiles in LDS: one workgroup of eight wavefronts is alone on its CU, with room for a
-  // third (2 x 4096 tokens not in the caches: 302 us, with two 307).
-  constexpr int STAGES = RW * TW == 8 ? 3 : 2;
+  // Tiles in LDS: a workgroup of eight wavefronts is alone on its CU, with room for a third
+  // (2 x 4096 tokens not in the caches: 302 us, with two 307), and 64 rows on a prefix,
+  // which wait for memory, are faster so than two workgroups of two stages (2 layers of
+  // 20011 tokens, 16 sequences: 60.0 us, 62.9).
+  constexpr int STAGES = RW * TW == 8 || (!WINDOW && RW == 2) ? 3 : 2;
   __shared__ __align__(16) uint16_t lds[STAGES][2][TOK * kD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int rw = wave % RW, tw = wave / RW;
@@ -169,9 +172,9 @@ void tile_attn_kernel(TileArgs a) {
       constexpr int W = RW * TW;
       static_assert(W * kTileElems <= STAGES * 2 * TOK * kD, "room for the wavefronts' V tiles");
       __shared__ float2 ml[W][16];
-      decode_block<W, 1, kKeepNone>(a.own, block,
-                                    reinterpret_cast<uint16_t(*)[kTileElems]>(&lds[0][0][0]), ml,
-                                    nullptr);
+      auto tiles = reinterpret_cast<uint16_t(*)[kTileElems]>(&lds[0][0][0]);
+      if (a.own_hb == 4) decode_block<W, 4, kKeepNone>(a.own, block, tiles, ml, nullptr);
+      else decode_block<W, 1, kKeepNone>(a.own, block, tiles, ml, nullptr);
       return;
     }
     block -= a.own_blocks;
@@ -626,7 +629,7 @@ TilePlan prefix_plan(const DenseDims& d) {
   p.tok = p.rows == 32 ? 128 : 64;
   p.n_rt = (int)((rows + p.rows - 1) / p.rows);
   const int64_t wgs = units * p.n_rt;
-  const int64_t target = p.rows == 256 || p.rows == 32 ? kCUs : 2 * kCUs;
+  const int64_t target = p.rows == 128 ? 2 * kCUs : kCUs;  // workgroups: two share a CU, or one
   int64_t ns = (target + wgs - 1) / wgs;
   const int64_t cap = ((int64_t)d.P_cap + kMinSplit - 1) / kMinSplit;
   if (ns > cap) ns = cap;
@@ -649,7 +652,7 @@ hipError_t launch_window(const DenseDims& d, const uint16_t* q, const uint16_t* 
   const int64_t units = (int64_t)d.n_layers * d.B * d.H_kv;
   TileArgs a{q, k, v, lens, q_lens, out, lse, nullptr, nullptr, d.kv_stride_layer, d.kv_stride_b,
              d.B, d.T, d.H_q, d.H_kv, d.G, d.L_cap, d.window, d.n_sink, (int)units, p.n_rt,
-             p.n_split, p.split_tok, d.scale * kLog2e, DecodeArgs{}, 0};
+             p.n_split, p.split_tok, d.scale * kLog2e, DecodeArgs{}, 0, 1};
   if (p.n_split > 1) {
     a.part_acc = static_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + tile_acc_bytes(units, p));
@@ -665,15 +668,24 @@ hipError_t launch_window(const DenseDims& d, const uint16_t* q, const uint16_t* 
 
 namespace {
 
-// The own tokens' workgroups: as many wavefronts as the tiles' (so many chunks at
-// least per split), and as few partial results as keep them short.
-int own_split(const DenseDims& d, const TilePlan& p) {
-  const int64_t units = (int64_t)d.n_layers * d.B * d.H_kv * (d.G / group_heads(d.G));
-  const int64_t waves = p.rows == 256 ? 8 : 4;
-  const int64_t most = (d.L_cap + 4 * kDecodeChunk * waves - 1) / (4 * kDecodeChunk * waves);
-  int64_t n = (kCUs + units - 1) / units;
-  if (n > most) n = most;
-  return n < 1 ? 1 : (int)n;
+// The own tokens' workgroups, of as many wavefronts as the tiles': hb column groups each,
+// over n_split of them.  Four groups side by side where that leaves a workgroup per CU
+// (16 sequences of 777 tokens at most on a prefix of 20011 58.5 -> 57.6 us, 64 of 1024 on
+// one of 32768 321 -> 312), and a few chunks to a wavefront.
+struct OwnPlan {
+  int hb, n_split;
+};
+OwnPlan own_plan(const DenseDims& d, const TilePlan& p) {
+  const int64_t groups = (int64_t)d.H_kv * (d.G / group_heads(d.G));
+  OwnPlan best{1, 1};
+  for (int hb = groups % 4 == 0 ? 4 : 1; hb >= 1; hb /= 4) {
+    const int64_t wgs = (int64_t)d.n_layers * d.B * groups / hb;
+    const int64_t tokens = 4 * kDecodeChunk * (p.rows == 256 ? 8 : 4) / hb;
+    const int64_t most = (d.L_cap + tokens - 1) / tokens, n = (kCUs + wgs - 1) / wgs;
+    best = {hb, (int)(n < most ? n : most)};
+    if (n <= most) break;
+  }
+  return best;
 }
 size_t own_acc_bytes(const DenseDims& d, int n_split) {
   return align_up(sizeof(float) * kD * (size_t)d.n_layers * d.B * n_split * d.H_q);
@@ -687,7 +699,7 @@ size_t own_ml_bytes(const DenseDims& d, int n_split) {
 size_t prefix_decode_ws_bytes(const DenseDims& d) {
   const TilePlan p = prefix_plan(d);
   const int64_t units = (int64_t)d.n_layers * d.H_kv;
-  const int ns = own_split(d, p);
+  const int ns = own_plan(d, p).n_split;
   return tile_acc_bytes(units, p) + tile_ml_bytes(units, p) + own_acc_bytes(d, ns) +
          own_ml_bytes(d, ns);
 }
@@ -698,18 +710,20 @@ hipError_t launch_prefix_decode(const DenseDims& d, const uint16_t* q, const uin
                                 float* out, float* lse, void* ws, hipStream_t s) {
   const TilePlan p = prefix_plan(d);
   const int64_t units = (int64_t)d.n_layers * d.H_kv;
-  const int heads = group_heads(d.G), R = d.G / heads, ns = own_split(d, p);
+  const OwnPlan own = own_plan(d, p);
+  const int heads = group_heads(d.G), R = d.G / heads, ns = own.n_split;
   char* w = static_cast<char*>(ws);
   TileArgs a{q, k_prefix, v_prefix, prefix_len, nullptr, nullptr, nullptr,
              reinterpret_cast<float*>(w), reinterpret_cast<float*>(w + tile_acc_bytes(units, p)),
              d.prefix_stride_layer, 0, 1, d.B, d.H_q, d.H_kv, d.G, d.P_cap, 0, 0, (int)units,
-             p.n_rt, p.n_split, p.split_tok, d.scale * kLog2e, DecodeArgs{}, 0};
+             p.n_rt, p.n_split, p.split_tok, d.scale * kLog2e, DecodeArgs{}, 0, 1};
   w += tile_acc_bytes(units, p) + tile_ml_bytes(units, p);
   a.own = DecodeArgs{q, k, v, lens, nullptr, nullptr, reinterpret_cast<float*>(w),
                      reinterpret_cast<float*>(w + own_acc_bytes(d, ns)), nullptr, nullptr,
                      d.kv_stride_layer, d.kv_stride_b, 0, d.B, d.H_q, d.H_kv, heads, R, d.L_cap,
                      d.L_cap, d.L_cap, ns, 0, d.scale * kLog2e};
-  a.own_blocks = (int)((int64_t)d.n_layers * d.B * d.H_kv * R * ns);
+  a.own_blocks = (int)((int64_t)d.n_layers * d.B * d.H_kv * R / own.hb * ns);
+  a.own_hb = own.hb;
   const hipError_t e = launch_tiles<false, true>(p, a, s);
   if (e != hipSuccess) return e;
   const int64_t n_out = (int64_t)d.n_layers * d.B * d.H_q;
