@@ -327,3 +327,108 @@ def test_two_graphs_share_a_workspace(dev):
         torch.cuda.synchronize()
         for a, b in zip(o + z + [oc, zc], want):
             assert torch.equal(a, b), i
+
+
+# ------------------------------------------------------------------ values and lengths
+
+@pytest.mark.parametrize("B,G", [(2, 4), (12, 4), (20, 4), (40, 8)])
+@pytest.mark.parametrize("odd", [math.nan, math.inf, -math.inf])
+def test_prefix_odd_values(dev, B, G, odd):
+    """A row of the shared V with an infinity or a NaN in one dimension: every query has
+    that value there, and the other dimensions are as if it were 0."""
+    P, cap = 700, 20
+    lens = [cap if b % 2 else b % cap for b in range(B)]
+    K, V = cache(1, B, cap, 1, 241, dev, lens)
+    Kp, Vp = (normal((1, P, 1, D), 243 + i, dev) for i in range(2))
+    q = normal((1, B, G, D), 245, dev)
+    bad = {P - 1: 3, 100: 70, 0: 127}
+    clean = Vp.clone()
+    for t, dim in bad.items():
+        Vp[0, t, 0, dim] = odd
+        clean[0, t, 0, dim] = 0.0
+    out, _ = spec.prefix_decode_attn(q, Kp, Vp, K, V, i32(lens, dev))
+    kp, vp = f64(Kp[0]), f64(clean[0])
+    for b in some(B, 5):
+        got = out[0, b].double().cpu().numpy()
+        for dim in bad.values():
+            assert (np.isnan(got[:, dim]) if odd != odd else got[:, dim] == odd).all()
+        ko, vo, qq = f64(K[0, b, :lens[b]]), f64(V[0, b, :lens[b]]), f64(q[0, b])
+        want, _ = dense_oracle.prefix_attention(qq, kp, vp, ko, vo, SCALE)
+        spread, _ = dense_oracle.prefix_attention(qq, kp, np.abs(vp), ko, np.abs(vo), SCALE)
+        e = weight_error(qq, np.concatenate([kp, ko]), P + cap)
+        for dim in bad.values():
+            got[:, dim] = want[:, dim]
+        check(got, want, 2 * e * spread + 1e-30, ("the other values", b))
+
+
+def test_lengths_are_clamped(dev):
+    n, B, H_q, H_kv, cap, T, P = 1, 3, 8, 2, 70, 6, 50
+    K, V = cache(n, B, cap, H_kv, 251, dev)
+    Kp, Vp = (normal((n, P, H_kv, D), 253 + i, dev) for i in range(2))
+    q, qc = normal((n, B, H_q, D), 255, dev), normal((n, B, T, H_q, D), 256, dev)
+    far, near = i32([-5, cap + 9, 2 ** 31 - 1], dev), i32([0, cap, cap], dev)
+    rows_far, rows = i32([-1, T + 3, 2 ** 31 - 1], dev), i32([0, T, T], dev)
+
+    def accum(lens):
+        w = torch.zeros((n, B, 1, cap), device=dev)
+        return (*spec.accum_decode_attn(q, K, V, lens, w), w)
+
+    for call in (lambda lens, r, p: spec.window_decode_attn(q, K, V, lens, 30, n_sink=2),
+                 lambda lens, r, p: spec.window_attn(qc, K, V, lens, 30, n_sink=2, q_lens=r),
+                 lambda lens, r, p: spec.prefix_decode_attn(q, Kp, Vp, K, V, lens, prefix_len=p),
+                 lambda lens, r, p: accum(lens)):
+        for a, b in zip(call(far, rows_far, i32([P + 4], dev)), call(near, rows, i32([P], dev))):
+            assert same_bits(a, b)
+
+    def evict(counts, keep, rows):
+        x = bounded(n, B, 1, H_kv, cap, 257, dev)
+        kv = normal((2, n, B, T, H_kv, D), 259, dev)
+        c = counts.clone()
+        spec.evict(*x, c, keep, i32([0, 90, 90], dev), k_new=kv[0], v_new=kv[1], n_new=rows,
+                   n_recent=9)
+        return (*x, c)
+
+    for a, b in zip(evict(far, i32([cap + 1, -3, cap], dev), rows_far),
+                    evict(near, i32([cap, 0, cap], dev), rows)):
+        assert same_bits(a, b)
+
+
+def test_debug_mode_rejects(dev, monkeypatch):
+    n, B, H_q, H_kv, cap, T, P = 1, 2, 8, 2, 70, 6, 50
+    K, V = cache(n, B, cap, H_kv, 261, dev)
+    Kp, Vp = (normal((n, P, H_kv, D), 263 + i, dev) for i in range(2))
+    q, qc = normal((n, B, H_q, D), 265, dev), normal((n, B, T, H_q, D), 266, dev)
+    ok, bad = i32([70, 0], dev), i32([71, 0], dev)
+    w, t = torch.zeros((n, B, 1, cap), device=dev), torch.zeros((n, B, 1, cap), dtype=torch.int32,
+                                                                device=dev)
+    kv = normal((2, n, B, T, H_kv, D), 267, dev)
+    want = spec.window_decode_attn(q, K, V, ok, 30)[0]
+    torch.cuda.synchronize()
+    monkeypatch.setenv("SPEC_DEBUG", "1")
+    assert torch.equal(spec.window_decode_attn(q, K, V, ok, 30)[0], want)
+    for call in (lambda: spec.window_decode_attn(q, K, V, bad, 30),
+                 lambda: spec.window_attn(qc, K, V, bad, 30),
+                 lambda: spec.window_attn(qc, K, V, ok, 30, q_lens=i32([7, 0], dev)),
+                 lambda: spec.prefix_decode_attn(q, Kp, Vp, K, V, bad),
+                 lambda: spec.prefix_decode_attn(q, Kp, Vp, K, V, ok, prefix_len=i32([51], dev)),
+                 lambda: spec.accum_decode_attn(q, K, V, i32([-1, 0], dev), w),
+                 lambda: spec.evict(K, V, w, t, bad, ok, ok, k_new=kv[0], v_new=kv[1]),
+                 lambda: spec.evict(K, V, w, t, ok, bad, ok, k_new=kv[0], v_new=kv[1]),
+                 lambda: spec.evict(K, V, w, t, ok, ok, ok, k_new=kv[0], v_new=kv[1],
+                                    n_new=i32([7, 0], dev))):
+        with pytest.raises(spec.SpecError) as e:
+            call()
+        assert e.value.status == 1
+    monkeypatch.delenv("SPEC_DEBUG")
+    assert not w.any() and ok.tolist() == [70, 0]
+
+
+@pytest.mark.parametrize("T,cap", [(9, 64), (40, 3000), (300, 300)])
+def test_window_in_place(dev, T, cap):
+    """The outputs may take the queries' place."""
+    K, V = cache(1, 2, cap, 2, 271, dev)
+    q = normal((1, 2, T, 8, D), 273, dev)
+    lens = i32([cap, cap - 3], dev)
+    want, _ = spec.window_attn(q, K, V, lens, 1000, n_sink=1)
+    got, _ = spec.window_attn(q, K, V, lens, 1000, n_sink=1, out=q)
+    assert got is q and torch.equal(got, want)
