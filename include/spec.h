@@ -463,9 +463,8 @@ SPEC_API spec_status spec_mla_workspace_size(const spec_mla_dims* dm, size_t* by
  * conventions above hold (layouts, lengths on the device and clamped, ownership,
  * alignment, errors, SPEC_DEBUG), with these differences: H_q / H_kv = G may be
  * any number up to 128, H_kv any number, and the workspace must be of the size
- * that spec_dense_workspace_size() gives.  NaNs and infinities in rows that a query
- * does not see do not reach it; an infinity in a row of V that it sees gives an
- * infinity or a NaN there.                                                    */
+ * that spec_dense_workspace_size() gives.  NaNs and infinities reach the queries
+ * that see their rows, and no others.                                         */
 typedef struct spec_dense_dims {
   int32_t B;         /* sequences in the batch                                 */
   int32_t L_cap;     /* token capacity of every cache row                      */

@@ -94,6 +94,48 @@ struct DecodeUnit {
 constexpr int kTileElems = kDecodeChunk * kHeadDim;
 constexpr int tile_elems(bool half) { return half ? kTileElems / 2 : kTileElems; }
 
+// A wavefront's share token by token, without the matrix cores, for the rare sums that
+// hold an infinity or a NaN: an infinity times a weight's parts is not that times the
+// weight.  As decode_unit leaves them, l_run not yet added up over a head's lanes.
+__device__ __forceinline__ void unit_by_token(const DecodeUnit& u, float& m_run, float& l_run,
+                                              floatx4 (&acc)[8]) {
+  const int lane = threadIdx.x & 63, r16 = lane & 15, kg = lane >> 4;
+  const uint16_t* q = u.q + (r16 < u.heads ? r16 : 0) * kHeadDim + 4 * kg;
+  auto four = [](const uint16_t* p) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    return floatx4{bf16lo(x.x), bf16hi(x.x), bf16lo(x.y), bf16hi(x.y)};
+  };
+  m_run = kNoMax;
+  l_run = 0.f;
+#pragma unroll
+  for (int db = 0; db < 8; ++db) acc[db] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int c = kDecodeChunk * u.part; c < u.count; c += kDecodeChunk * u.n_parts) {
+#pragma unroll 1
+    for (int j = c; j < min(c + kDecodeChunk, u.count); ++j) {
+      const int64_t off = (int64_t)(j + (j < u.n_sink ? 0 : u.shift)) * u.rs + 4 * kg;
+      float s = 0.f;
+#pragma unroll
+      for (int db = 0; db < 8; ++db) {
+        const floatx4 x = four(q + 16 * db), y = four(u.k + off + 16 * db);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s = fmaf(x[i], y[i], s);
+      }
+      s = quad_sum(s) * u.scale_log2;
+      const float mn = fmaxf(m_run, s);
+      const float alpha = exp2_fast(m_run - mn), p = exp2_fast(s - mn);
+      m_run = mn;
+      l_run = l_run * alpha + (kg == 0 ? p : 0.f);
+#pragma unroll
+      for (int db = 0; db < 8; ++db) {
+        const floatx4 y = four(u.v + off + 16 * db);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[db][i] = fmaf(acc[db][i], alpha, p * y[i]);
+      }
+    }
+  }
+}
+
 // A wavefront's share: maximum and sum of head r16 (l_run complete) and O^T[16 db + 4 kg
 // + i][head r16]; keep(head, token, logits of four tokens) is called for every four
 // logits (log2 units) of its chunks.  V: its V tile.
@@ -247,6 +289,12 @@ __device__ __forceinline__ void decode_unit(const DecodeUnit& u, uint16_t* V, fl
     }
     wave_sync_lds();  // the tile is rewritten by the next chunk
   }
+  float odd = 0.f;
+#pragma unroll
+  for (int db = 0; db < 8; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) odd = fmaf(acc[db][i], 0.f, odd);
+  if (__any(odd != odd)) unit_by_token(u, m_run, l_run, acc);
   l_run = quad_sum(l_run);
 }
 

@@ -432,3 +432,38 @@ def test_window_in_place(dev, T, cap):
     want, _ = spec.window_attn(q, K, V, lens, 1000, n_sink=1)
     got, _ = spec.window_attn(q, K, V, lens, 1000, n_sink=1, out=q)
     assert got is q and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("n,B,H_q,H_kv,cap", [(1, 2, 8, 2, 300), (1, 1, 24, 1, 2000),
+                                              (16, 8, 32, 8, 130), (1, 3, 6, 3, 20000)])
+@pytest.mark.parametrize("odd", [math.nan, math.inf, -math.inf])
+def test_decode_odd_values(dev, n, B, H_q, H_kv, cap, odd):
+    """The same of the decode entry points: a row of V of the last KV head."""
+    counts = [cap - 7 * b for b in range(B)]
+    K, V = cache(n, B, cap, H_kv, 281, dev, counts)
+    q = normal((n, B, H_q, D), 283, dev)
+    l, g, G = n - 1, H_kv - 1, H_q // H_kv
+    clean = f64(V[l, 0])
+    for t, dim in {counts[0] - 1: 3, 100: 70, 0: 127}.items():
+        V[l, 0, t, g, dim] = odd
+        clean[t, g, dim] = 0.0
+    lens = i32(counts, dev)
+    qq, kk = f64(q[l, 0]), f64(K[l, 0])
+    L = counts[0]
+    want, _, add = dense_oracle.accumulate(qq, kk[:L], clean[:L], 1, SCALE)
+    spread, _, _ = dense_oracle.accumulate(qq, kk[:L], np.abs(clean[:L]), 1, SCALE)
+    e = weight_error(qq, finite(kk), cap)
+    w = torch.zeros((n, B, 1, cap), device=dev)
+    p = normal((n, 40, H_kv, D), 285, dev)
+    for what, out in (("window", spec.window_decode_attn(q, K, V, lens, cap)[0]),
+                      ("accum", spec.accum_decode_attn(q, K, V, lens, w)[0]),
+                      ("prefix", spec.prefix_decode_attn(q, p, p, K, V, lens,
+                                                         prefix_len=i32([0], dev))[0])):
+        got = out[l, 0].double().cpu().numpy()
+        heads = slice(g * G, (g + 1) * G)
+        for dim in (3, 70, 127):
+            at = got[heads, dim]
+            assert (np.isnan(at) if odd != odd else at == odd).all(), what
+            got[heads, dim] = want[heads, dim]
+        check(got, want, 2 * e * spread + 1e-30, what)
+    check(w[l, 0, 0, :L].cpu(), add[0], (2 * e + 2.0 ** -19 + H_q * U) * add[0], "weights")
