@@ -15,7 +15,7 @@
 // thread keeps the keys of a run of consecutive slots in registers, and the E-th
 // largest key is found from counts in LDS of its digits of 11, 11 and 10 bits, done
 // early once the keys that share the digits found all stay (32 sets of 8192 slots:
-// the plan takes 16 us).  Where only a few rows go, as in a decode step, they are
+// the plan takes 13 us).  Where only a few rows go, as in a decode step, they are
 // searched for one after another instead (2048 sets of 2048 slots: 12.8 us in all,
 // 24.1 by digits).  Many new rows are moved by a launch of its own at the rate of a
 // copy (32 sets x 512 rows of 4 KB: 29 us, 4.6 TB/s).
@@ -429,13 +429,17 @@ size_t list_bytes(const DenseDims& d, int64_t sets) {
 // a launch of its own costs about 4 us.
 constexpr int kMoveInPlan = 32;
 
+// Slots of a thread: few enough that its loads are in flight together, and as many
+// threads as leave other workgroups their places (us: 2048 sets of 8192 slots, one new row,
+// by 256 threads 54.4, 512 37.1, 1024 52; 64 such sets of which 8 rows go 19.7, 15.5, 15.1;
+// 2048 sets of 2048 slots by 128 threads 15.5, 256 14.6, 512 19.5).
 template <bool MOVE>
 void launch_plan(int64_t sets, const EvictKernelArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)sets);
   if (a.L_cap <= 2048) evict_plan_kernel<256, 8, MOVE><<<grid, 256, 0, s>>>(a);
-  else if (a.L_cap <= 4096) evict_plan_kernel<256, 16, MOVE><<<grid, 256, 0, s>>>(a);
-  else if (a.L_cap <= 8192) evict_plan_kernel<256, 32, MOVE><<<grid, 256, 0, s>>>(a);
-  else if (a.L_cap <= 16384) evict_plan_kernel<512, 32, MOVE><<<grid, 512, 0, s>>>(a);
+  else if (a.L_cap <= 4096) evict_plan_kernel<512, 8, MOVE><<<grid, 512, 0, s>>>(a);
+  else if (a.L_cap <= 8192) evict_plan_kernel<512, 16, MOVE><<<grid, 512, 0, s>>>(a);
+  else if (a.L_cap <= 16384) evict_plan_kernel<1024, 16, MOVE><<<grid, 1024, 0, s>>>(a);
   else evict_plan_kernel<1024, 32, MOVE><<<grid, 1024, 0, s>>>(a);
 }
 constexpr int kPlanSlots = 32768;  // what the widest of them holds
