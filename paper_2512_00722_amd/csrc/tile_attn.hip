@@ -148,9 +148,9 @@ __device__ __forceinline__ void load_to_lds(const void* g, const void* lds) {
 // RW x TW wavefronts: RW groups of 32 rows, TW parts of each tile's tokens.
 // WINDOW: masked rows of a sequence; else every row sees all tokens.  SPLITP:
 // weights as a bf16 pair (~2^-18 relative) for fp32 results, or with few rows, which
-// leave the matrix cores idle, as three bf16 numbers (2 % of the time of 32 rows, 5 %
-// of that of 64); else rounded to bf16 once (2^-9), which the rounding of a bf16
-// result hides.
+// leave the matrix cores idle, as three bf16 numbers (2 % of the time of 32 rows, but 9 %
+// of that of 64 and 13 % of that of 256); else rounded to bf16 once (2^-9), which the
+// rounding of a bf16 result hides.
 template <int RW, int TW, int TOK, bool WINDOW, bool SPLITP>
 __global__ __launch_bounds__(RW* TW * 64) __attribute__((amdgpu_waves_per_eu(TOK == 64 ? 2 : 1)))
 void tile_attn_kernel(TileArgs a) {
