@@ -173,7 +173,7 @@ EVICT = [
     (1, 1, True, 32769, [32769, 30000], [30000, 30002], 2, 2000, 4, "mixed"),
     (1, 2, False, 40000, [40000, 33000], [39999, 33000], 50, 100, 4, "mixed"),
     (1, 1, True, 40000, [40000, 35000], [40000, 1], 7, 0, 0, "equal"),
-    (1, 2, True, 900, [900, 895], [900, 899], 6, 30, 2, "mixed"),         # six go, and one
+    (1, 2, True, 900, [900, 895], [900, 899], 6, 30, 2, "mixed"),         # six go, and two
     (1, 2, True, 900, [900, 900], [900, 894], 6, 30, 2, "equal"),         # six, and twelve
     (1, 1, True, 4096, [4096, 4096], [1000, 4095], 0, 0, 0, "close"),     # equal but for low bits
     (1, 1, True, 700, [700, 700], [300, 100], 2, 350, 3, "inf"),          # more +inf than stay
