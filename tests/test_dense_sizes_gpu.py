@@ -77,6 +77,9 @@ PREFIX = [
     (32, 8, 20011, None, 777, [777, 5, 400] * 5),
     (64, 8, 4097, 4096, 100, [100, 33] * 6),
     (128, 1, 3000, None, 64, [64] * 5),                      # 640 rows on one KV head
+    (64, 16, 2000, 1990, 700, [700, 5, 0, 699] * 5),         # own tokens by four heads side by
+    (64, 16, 1500, None, 700, [700, 31] * 6),                # side, 128 and 64 rows
+    (16, 4, 900, None, 5000, [5000, 4000]),
 ]
 
 
