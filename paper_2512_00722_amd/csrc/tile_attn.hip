@@ -292,20 +292,26 @@ void tile_attn_kernel(TileArgs a) {
 
     // S^T of this wavefront's blocks: token 32 blk + 8 (i / 4) + 4 kg + i % 4.  Between
     // the products a later tile's loads, into the stage that was last read before the
-    // previous barrier.
+    // previous barrier; as no LDS read moves across those, K is read kAhead products
+    // before it is needed (8192 tokens, window 1024: 158 us, read beside them 164).
     floatx16 s[NB];
 #pragma unroll
     for (int blk = 0; blk < NB; ++blk) s[blk] = 0.f;
+    constexpr int kOps = 8 * NB, kAhead = 5;
+    auto k_operand = [&](int c) {
+      const uint16_t* kp = Kt + ((tw * NB + c / 8) * 32 + c32) * kD;
+      return *reinterpret_cast<const bf16x8*>(kp + (((2 * (c % 8)) ^ ksw) * 8));
+    };
+    bf16x8 kf[kOps];
 #pragma unroll
-    for (int st = 0; st < 8; ++st) {
+    for (int c = 0; c < kAhead; ++c) kf[c] = k_operand(c);
 #pragma unroll
-      for (int blk = 0; blk < NB; ++blk) {
-        const uint16_t* kp = Kt + ((tw * NB + blk) * 32 + c32) * kD;
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kp + (((2 * st) ^ ksw) * 8));
-        s[blk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], s[blk], 0, 0, 0);
-      }
+    for (int c = 0; c < kOps; ++c) {
+      if (c + kAhead < kOps) kf[c + kAhead] = k_operand(c + kAhead);
+      s[c / 8] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], qf[c % 8], s[c / 8], 0, 0, 0);
 #pragma unroll
-      for (int e = st * LD / 4; e < (st + 1) * LD / 4; ++e) issue(it + STAGES - 1, then, e);
+      for (int e = c * LD / (4 * NB); e < (c + 1) * LD / (4 * NB); ++e)
+        issue(it + STAGES - 1, then, e);
     }
 
     if (it >= clear || (WINDOW && it >= edge0 && it < edge1)) {
