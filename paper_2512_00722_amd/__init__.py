@@ -257,7 +257,12 @@ def _need(t: torch.Tensor, name: str, dtype, ndim: int):
 
 
 def _inner_contig(t: torch.Tensor, name: str, n_inner: int):
-    """The last n_inner dims must be densely packed (row-major)."""
+    """The last n_inner dims must be densely packed (row-major), and the outer ones
+    have memory of their own: a stride of 0 means 'densely packed' to the library, so
+    that an expanded dim would be read, or written, far behind its tensor."""
+    for dim in range(t.dim() - n_inner):
+        if t.shape[dim] > 1 and t.stride(dim) == 0:
+            raise ValueError(f"{name}: dim {dim} is expanded (stride 0)")
     exp = 1
     for dim in range(t.dim() - 1, t.dim() - 1 - n_inner, -1):
         if t.shape[dim] != 1 and t.stride(dim) != exp:

@@ -57,8 +57,11 @@ bool is(const at::Tensor* t, at::ScalarType type, int64_t ndim) {
   return t && t->scalar_type() == type && t->dim() == ndim;
 }
 
-// The last n dims are densely packed (row-major).
+// The last n dims are densely packed (row-major), and no outer one is expanded: the C
+// ABI takes a stride of 0 as 'densely packed'.
 bool packed(const at::Tensor& t, int64_t n) {
+  for (int64_t d = 0; d < t.dim() - n; ++d)
+    if (t.size(d) > 1 && t.stride(d) == 0) return false;
   int64_t expect = 1;
   for (int64_t d = t.dim() - 1; d >= t.dim() - n; --d) {
     if (t.size(d) != 1 && t.stride(d) != expect) return false;

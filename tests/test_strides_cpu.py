@@ -1,0 +1,40 @@
+"""Strided tensors that a call must refuse, on a host without a GPU (tensors without
+memory: nothing is launched)."""
+import pytest
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
+
+import paper_2512_00722_amd as spec
+from tests import strided_calls
+
+
+@pytest.mark.parametrize("name", strided_calls.NAMES)
+def test_expanded_tensors_are_refused(name):
+    """A stride of 0 means 'densely packed' to the library, which would go past the
+    tensor's memory."""
+    with FakeTensorMode():
+        a = strided_calls.tensors("cuda")
+        strided = strided_calls.calls(a)[name][0]
+        pairs = [p for p in (("K", "V"), ("K_prefix", "V_prefix"), ("K_r",), ("ckv",))
+                 if p[0] in strided]
+        seen = 0
+        for pair in pairs:
+            outer = 2 if pair[0] in ("K", "ckv") else 1
+            for dim in range(outer):
+                b = dict(a)
+                for t in pair:
+                    b[t] = strided_calls.expanded(a[t], dim)
+                    assert b[t].stride(dim) == 0
+                with pytest.raises(ValueError, match="expanded"):
+                    strided_calls.calls(b)[name][1]()
+                seen += 1
+        assert seen
+
+
+def test_expanded_host_caches_are_refused(monkeypatch):
+    K = torch.zeros((1, 2, 40, 2, 128), dtype=torch.bfloat16)
+    monkeypatch.setattr(torch.Tensor, "is_pinned", lambda t: True)
+    spec._host_kv(K, K)
+    E = strided_calls.expanded(K, 1)
+    with pytest.raises(ValueError, match="expanded"):
+        spec._host_kv(E, E)
