@@ -270,6 +270,12 @@ def _inner_contig(t: torch.Tensor, name: str, n_inner: int):
         exp *= t.shape[dim]
 
 
+def _stride(t: torch.Tensor, dim: int) -> int:
+    """Elements between the entries of an outer dim, as the C ABI takes it.  That of a
+    dim of one entry means nothing (torch leaves any value there): 0, the default."""
+    return t.stride(dim) if t.shape[dim] > 1 else 0
+
+
 def _i32(t: torch.Tensor, name: str, n: int):
     _need(t, name, torch.int32, 1)
     if t.shape[0] != n or not t.is_contiguous():
@@ -297,7 +303,7 @@ def _dims_retrieval(K_r: torch.Tensor, L_max: int, k_max: int, scale_r: float, *
     base = dict(n_layers=1, H_q=1, H_kv=1, d=128)
     base.update(llm)
     return Dims.make(B=B, L_cap=L_cap, L_max=L_max, k_max=k_max, H_r=H_r, d_r=d_r,
-                     kr_stride_b=K_r.stride(0), scale_r=scale_r, **base)
+                     kr_stride_b=_stride(K_r, 0), scale_r=scale_r, **base)
 
 
 # ------------------------------------------------------------------ ops
@@ -377,7 +383,7 @@ def _dims_llm(q: torch.Tensor, K: torch.Tensor, k_max: int, scale: float, L_max=
     _, _, H_q, _ = q.shape
     return Dims.make(B=B, L_cap=L_cap, L_max=L_cap if L_max is None else L_max, k_max=k_max,
                      n_layers=n_layers, H_q=H_q, H_kv=H_kv, d=d,
-                     kv_stride_layer=K.stride(0), kv_stride_b=K.stride(1), scale=scale, **extra)
+                     kv_stride_layer=_stride(K, 0), kv_stride_b=_stride(K, 1), scale=scale, **extra)
 
 
 def _check_cache(K: torch.Tensor, V: torch.Tensor):
@@ -413,7 +419,7 @@ def gather(K: torch.Tensor, V: torch.Tensor, idx: torch.Tensor, counts: torch.Te
     k_max = idx.shape[-1]
     _i32(counts, "counts", B)
     dims = Dims.make(B=B, L_cap=L_cap, L_max=L_cap, k_max=k_max, n_layers=n_layers, H_q=H_kv,
-                     H_kv=H_kv, d=d, kv_stride_layer=K.stride(0), kv_stride_b=K.stride(1),
+                     H_kv=H_kv, d=d, kv_stride_layer=_stride(K, 0), kv_stride_b=_stride(K, 1),
                      n_sets=n_sets)
     if out is None:
         ks = torch.zeros((n_layers, B, k_max, H_kv, d), dtype=torch.bfloat16, device=K.device)
@@ -537,7 +543,7 @@ def delta_gather(idx_now: torch.Tensor, counts: torch.Tensor, K: torch.Tensor, V
         raise ValueError("elastic state shape does not match")
     dims = Dims.make(B=B, L_cap=L_cap, L_max=L_cap if L_max is None else L_max, k_max=k_max,
                      n_layers=n_layers, H_q=H_kv, H_kv=H_kv, d=d,
-                     kv_stride_layer=K.stride(0), kv_stride_b=K.stride(1))
+                     kv_stride_layer=_stride(K, 0), kv_stride_b=_stride(K, 1))
     ws, nws = _workspace(dims, OP_DELTA, K.device, ws)
     el = state.c_struct()
     _check(lib.spec_delta_gather(ctypes.byref(dims), _p(idx_now.contiguous()), _p(counts),
@@ -566,8 +572,8 @@ def _step_args(q_r, K_r, seq_lens, ks, q, K, V, k_max, L_max, scale_r, scale, wi
     L_max = L_cap if L_max is None else int(L_max)
     dims = Dims.make(B=B, L_cap=L_cap, L_max=L_max, k_max=int(k_max), H_r=H_r, d_r=d_r,
                      n_layers=n_layers, H_q=q.shape[2], H_kv=H_kv, d=d,
-                     kr_stride_b=K_r.stride(0), kv_stride_layer=K.stride(0),
-                     kv_stride_b=K.stride(1), scale_r=scale_r, scale=scale,
+                     kr_stride_b=_stride(K_r, 0), kv_stride_layer=_stride(K, 0),
+                     kv_stride_b=_stride(K, 1), scale_r=scale_r, scale=scale,
                      n_sets=H_kv if head_level else 1)
     dev = q.device
     sets = (H_kv,) if head_level else ()
@@ -660,7 +666,7 @@ def _host_kv(Kh: torch.Tensor, Vh: torch.Tensor) -> HostKv:
     if Kh.shape != Vh.shape or Kh.stride() != Vh.stride():
         raise ValueError("K_host and V_host must have the same shape and strides")
     _inner_contig(Kh, "K_host", 3)
-    return HostKv(Kh.data_ptr(), Vh.data_ptr(), Kh.stride(0), Kh.stride(1))
+    return HostKv(Kh.data_ptr(), Vh.data_ptr(), _stride(Kh, 0), _stride(Kh, 1))
 
 
 def offload_load(idx_now: torch.Tensor, counts: torch.Tensor, K_host: torch.Tensor,
@@ -733,9 +739,9 @@ def step_offload(q_r, K_r, seq_lens, ks, q, K, V, K_host, V_host, k_max: int,
     L_max = L if L_max is None else int(L_max)
     dims = Dims.make(B=B, L_cap=L, L_max=L_max, k_max=int(k_max), H_r=H_r, d_r=d_r,
                      n_layers=n_layers, H_q=q.shape[2], H_kv=H_kv, d=d,
-                     kr_stride_b=K_r.stride(0),
-                     kv_stride_layer=K.stride(0) if n_dev else 0,
-                     kv_stride_b=K.stride(1) if n_dev else 0)
+                     kr_stride_b=_stride(K_r, 0),
+                     kv_stride_layer=_stride(K, 0) if n_dev else 0,
+                     kv_stride_b=_stride(K, 1) if n_dev else 0)
     ws, nws = _workspace(dims, OP_OFFLOAD, q.device, ws)
     dev = q.device
     o = outputs if outputs is not None else {}
@@ -861,8 +867,8 @@ def mla_sparse_decode_attn(q: torch.Tensor, ckv: torch.Tensor, w_uk: torch.Tenso
         raise ValueError("idx must be contiguous [B, k_max]")
     _i32(counts, "counts", B)
     dims = MlaDims.make(B=B, L_cap=L_cap, k_max=idx.shape[1], n_layers=n_layers, H=H, d_c=d_c,
-                        d_rope=d_rope, d_nope=d_nope, d_v=d_v, ckv_stride_layer=ckv.stride(0),
-                        ckv_stride_b=ckv.stride(1), scale=scale)
+                        d_rope=d_rope, d_nope=d_nope, d_v=d_v, ckv_stride_layer=_stride(ckv, 0),
+                        ckv_stride_b=_stride(ckv, 1), scale=scale)
     if ws is None:
         ws = torch.empty(mla_workspace_size(dims), dtype=torch.uint8, device=q.device)
     if out is None:
@@ -932,7 +938,7 @@ def _int32(n: int) -> int:
 def _dense_dims(K: torch.Tensor, **kw) -> DenseDims:
     n_layers, B, L_cap, H_kv, d = K.shape
     return DenseDims.make(B=B, L_cap=L_cap, n_layers=n_layers, H_kv=H_kv, d=d,
-                          kv_stride_layer=K.stride(0), kv_stride_b=K.stride(1), **kw)
+                          kv_stride_layer=_stride(K, 0), kv_stride_b=_stride(K, 1), **kw)
 
 
 def window_decode_attn(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, seq_lens: torch.Tensor,
@@ -1038,7 +1044,7 @@ def prefix_decode_attn(q: torch.Tensor, K_prefix: torch.Tensor, V_prefix: torch.
     _same_device(q, K=K, V=V, K_prefix=K_prefix, V_prefix=V_prefix, seq_lens=seq_lens,
                  prefix_len=prefix_len, out=out, lse=lse, ws=ws)
     dims = _dense_dims(K, H_q=q.shape[2], P_cap=K_prefix.shape[1], scale=scale,
-                       prefix_stride_layer=K_prefix.stride(0))
+                       prefix_stride_layer=_stride(K_prefix, 0))
     ws, nws = _dense_workspace(dims, DENSE_PREFIX_DECODE, q.device, ws)
     out = _output(out, "out", q.shape, torch.float32, q.device)
     if lse is not None or with_lse:

@@ -70,6 +70,10 @@ bool packed(const at::Tensor& t, int64_t n) {
   return true;
 }
 
+// Elements between the entries of an outer dim; 0 (the C ABI's default) where there is
+// one, whose stride means nothing.
+int64_t stride(const at::Tensor& t, int64_t d) { return t.size(d) > 1 ? t.stride(d) : 0; }
+
 bool has_shape(const at::Tensor* t, at::ScalarType type, std::initializer_list<int64_t> shape) {
   return t && t->scalar_type() == type && t->is_contiguous() &&
          t->sizes() == c10::IntArrayRef(shape.begin(), shape.size());
@@ -191,8 +195,8 @@ PyObject* fast_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
   d.H_q = (int32_t)H_q;
   d.H_kv = (int32_t)H_kv;
   d.d = (int32_t)hd;
-  d.kv_stride_layer = K->stride(0);
-  d.kv_stride_b = K->stride(1);
+  d.kv_stride_layer = stride(*K, 0);
+  d.kv_stride_b = stride(*K, 1);
   return call(api.attn, &d, ptr<uint16_t>(q), ptr<uint16_t>(K), ptr<uint16_t>(V), ptr<int32_t>(idx),
               ptr<int32_t>(counts), ptr<float>(out), ptr<float>(lse), ws->data_ptr(),
               ws->nbytes(), stream);
@@ -229,7 +233,7 @@ PyObject* fast_score(PyObject*, PyObject* const* args, Py_ssize_t n) {
   d.H_r = (int32_t)H_r;
   d.d_r = (int32_t)d_r;
   d.H_q = d.H_kv = d.n_sets = n_sets;
-  d.kr_stride_b = K_r->stride(0);
+  d.kr_stride_b = stride(*K_r, 0);
   return call(api.score, &d, ptr<uint16_t>(q_r), ptr<uint16_t>(K_r), ptr<int32_t>(seq_lens),
               ptr<float>(out), ws->data_ptr(), ws->nbytes(), stream);
 }
@@ -341,9 +345,9 @@ PyObject* fast_step(PyObject*, PyObject* const* args, Py_ssize_t n) {
   d.H_q = (int32_t)H_q;
   d.H_kv = (int32_t)H_kv;
   d.d = (int32_t)hd;
-  d.kr_stride_b = K_r->stride(0);
-  d.kv_stride_layer = K->stride(0);
-  d.kv_stride_b = K->stride(1);
+  d.kr_stride_b = stride(*K_r, 0);
+  d.kv_stride_layer = stride(*K, 0);
+  d.kv_stride_b = stride(*K, 1);
   d.n_sets = sets ? (int32_t)H_kv : 1;
   return call(api.step, &d, ptr<uint16_t>(q_r), ptr<uint16_t>(K_r), ptr<int32_t>(seq_lens),
               ptr<int32_t>(ks), ptr<uint16_t>(q), ptr<uint16_t>(K), ptr<uint16_t>(V),
@@ -385,7 +389,7 @@ PyObject* fast_retrieval_qk(PyObject*, PyObject* const* args, Py_ssize_t n) {
   d.k_max = 1;
   d.H_r = (int32_t)H_r;
   d.d_r = (int32_t)d_r;
-  d.kr_stride_b = K_r->stride(0);
+  d.kr_stride_b = stride(*K_r, 0);
   fe.vocab = (int32_t)emb->size(0);
   fe.hidden = (int32_t)hidden;
   return call(api.retrieval_qk, &d, &fe, ptr<int32_t>(tokens), ptr<int32_t>(pos),
@@ -430,8 +434,8 @@ PyObject* fast_mla(PyObject*, PyObject* const* args, Py_ssize_t n) {
   d.d_rope = (int32_t)dr;
   d.d_nope = (int32_t)dn;
   d.d_v = (int32_t)dv;
-  d.ckv_stride_layer = ckv->stride(0);
-  d.ckv_stride_b = ckv->stride(1);
+  d.ckv_stride_layer = stride(*ckv, 0);
+  d.ckv_stride_b = stride(*ckv, 1);
   return call(api.mla, &d, ptr<uint16_t>(q), ptr<uint16_t>(ckv), ptr<uint16_t>(w_uk),
               ptr<uint16_t>(w_uv), ptr<int32_t>(idx), ptr<int32_t>(counts), ptr<float>(out),
               ptr<float>(lse), ws->data_ptr(), ws->nbytes(), stream);
@@ -447,8 +451,8 @@ spec_dense_dims dense_dims(const at::Tensor& K) {
   d.d = (int32_t)K.size(4);
   d.T = 1;
   d.n_sets = 1;
-  d.kv_stride_layer = K.stride(0);
-  d.kv_stride_b = K.stride(1);
+  d.kv_stride_layer = stride(K, 0);
+  d.kv_stride_b = stride(K, 1);
   return d;
 }
 
@@ -537,7 +541,7 @@ PyObject* fast_prefix_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
          same_device(*q, {K, V, Kp, Vp, lens, plen, out, lse, ws}));
   d.H_q = (int32_t)q->size(2);
   d.P_cap = (int32_t)Kp->size(1);
-  d.prefix_stride_layer = Kp->stride(0);
+  d.prefix_stride_layer = stride(*Kp, 0);
   return call(api.prefix_decode, &d, ptr<uint16_t>(q), ptr<uint16_t>(Kp), ptr<uint16_t>(Vp),
               ptr<int32_t>(plen), ptr<uint16_t>(K), ptr<uint16_t>(V), ptr<int32_t>(lens),
               ptr<float>(out), ptr<float>(lse), ws->data_ptr(), ws->nbytes(), stream);

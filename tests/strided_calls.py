@@ -76,3 +76,10 @@ NAMES = ["window_decode_attn", "window_attn", "prefix_decode_attn", "accum_decod
 def expanded(t, dim):
     """A view of t's shape whose `dim` repeats its first entry."""
     return t.narrow(dim, 0, 1).expand(t.shape)
+
+
+def loose(t, dim):
+    """t, which has one entry in `dim`, with another stride there."""
+    strides = list(t.stride())
+    strides[dim] = 8
+    return t.as_strided(t.shape, strides)

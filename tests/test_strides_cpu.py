@@ -38,3 +38,17 @@ def test_expanded_host_caches_are_refused(monkeypatch):
     E = strided_calls.expanded(K, 1)
     with pytest.raises(ValueError, match="expanded"):
         spec._host_kv(E, E)
+
+
+def test_strides_of_single_entries_mean_nothing():
+    """One layer, or one sequence: whatever torch leaves as its stride (here 8, as a
+    transposed view of other sizes may have) is not passed on."""
+    for shape, dim in (((1, 3, 40, 2, 128), 0), ((2, 1, 40, 2, 128), 1), ((1, 1, 40, 2, 128), 1)):
+        K = strided_calls.loose(torch.zeros(shape, dtype=torch.bfloat16), dim)
+        q = torch.zeros((*shape[:2], 8, 128), dtype=torch.bfloat16)
+        for op in range(5):
+            spec.dense_workspace_size(
+                spec._dense_dims(K, H_q=8, window=8, P_cap=40, n_sets=2), op)
+        spec.workspace_size(spec._dims_llm(q, K, 16, 0.0), spec.OP_ATTN)
+    K_r = strided_calls.loose(torch.zeros((1, 40, 8, 64), dtype=torch.bfloat16), 0)
+    spec.workspace_size(spec._dims_retrieval(K_r, 40, 16, 0.0), spec.OP_SCORE)

@@ -31,3 +31,40 @@ def test_expanded_tensors_are_refused(dev, name):
                 strided_calls.calls(b)[name][1]()
     plain()    # the tensors themselves are fine
     torch.cuda.synchronize()
+
+
+def test_strides_of_single_entries_mean_nothing(dev):
+    """One layer and one sequence whose strides are arbitrary, with every buffer handed
+    over and without: the results of the packed tensors."""
+    announce("strides of single entries")
+    g = torch.Generator(device=dev).manual_seed(3)
+
+    def rn(*shape):
+        return torch.randn(shape, generator=g, device=dev).to(torch.bfloat16)
+
+    K, V, Kp, Vp = rn(1, 1, 90, 2, 128), rn(1, 1, 90, 2, 128), rn(1, 70, 2, 128), rn(1, 70, 2, 128)
+    q, qc = rn(1, 1, 8, 128), rn(1, 1, 6, 8, 128)
+    lens = torch.tensor([83], dtype=torch.int32, device=dev)
+    idx = torch.arange(0, 64, 2, dtype=torch.int32, device=dev)[None]
+    n = torch.tensor([32], dtype=torch.int32, device=dev)
+    ws = torch.zeros(1 << 24, dtype=torch.uint8, device=dev)
+
+    def outputs(t, kind=torch.float32):
+        return dict(out=torch.zeros(t.shape, dtype=kind, device=dev),
+                    lse=torch.zeros(t.shape[:-1], device=dev), ws=ws)
+
+    def run(K, V, Kp, Vp, buffers):
+        o = (lambda t, *k: outputs(t, *k)) if buffers else (lambda t, *k: {})
+        w = torch.zeros((1, 1, 1, 90), device=dev)
+        return [*spec.window_decode_attn(q, K, V, lens, 30, **o(q)),
+                *spec.window_attn(qc, K, V, lens, 30, **o(qc, torch.bfloat16)),
+                *spec.prefix_decode_attn(q, Kp, Vp, K, V, lens, **o(q)),
+                *spec.accum_decode_attn(q, K, V, lens, w, **o(q)), w,
+                *spec.sparse_decode_attn(q, K, V, n, idx=idx, **o(q))]
+
+    want = run(K, V, Kp, Vp, True)
+    kv = [strided_calls.loose(strided_calls.loose(t, 0), 1) for t in (K, V)]
+    pre = [strided_calls.loose(t, 0) for t in (Kp, Vp)]
+    for buffers in (True, False):
+        for a, b in zip(run(*kv, *pre, buffers), want):
+            assert torch.equal(a, b)
