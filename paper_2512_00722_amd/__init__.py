@@ -289,11 +289,18 @@ def workspace_size(dims: Dims, op: int) -> int:
     return int(n.value)
 
 
+def _bytes(ws: torch.Tensor, device) -> int:
+    """The size of a caller's workspace, all of which is its own memory on the device."""
+    if not ws.is_contiguous() or ws.device != device:
+        raise ValueError(f"ws must be contiguous and on {device}")
+    return ws.numel() * ws.element_size()
+
+
 def _workspace(dims: Dims, op: int, device, ws: Optional[torch.Tensor]):
     """(workspace, bytes): the caller's (the library decides whether it is
     enough, see _check), or one of the size it asks for."""
     if ws is not None:
-        return ws, ws.numel() * ws.element_size()
+        return ws, _bytes(ws, device)
     need = workspace_size(dims, op)
     return torch.empty(max(need, 16), dtype=torch.uint8, device=device), need
 
@@ -871,13 +878,14 @@ def mla_sparse_decode_attn(q: torch.Tensor, ckv: torch.Tensor, w_uk: torch.Tenso
                         ckv_stride_b=_stride(ckv, 1), scale=scale)
     if ws is None:
         ws = torch.empty(mla_workspace_size(dims), dtype=torch.uint8, device=q.device)
+    nws = _bytes(ws, q.device)
     if out is None:
         out = torch.empty((n_layers, B, H, d_v), dtype=torch.float32, device=q.device)
     if lse is None and with_lse:
         lse = torch.empty((n_layers, B, H), dtype=torch.float32, device=q.device)
     _check(lib.spec_mla_sparse_decode_attn(ctypes.byref(dims), _p(q), _p(ckv), _p(w_uk),
                                            _p(w_uv), _p(idx), _p(counts), _p(out), _p(lse),
-                                           _p(ws), ws.numel() * ws.element_size(), _stream(q)),
+                                           _p(ws), nws, _stream(q)),
            "spec_mla_sparse_decode_attn")
     return out, lse
 
@@ -894,7 +902,7 @@ def dense_workspace_size(dims: DenseDims, op: int) -> int:
 
 def _dense_workspace(dims: DenseDims, op: int, device, ws: Optional[torch.Tensor]):
     if ws is not None:
-        return ws, ws.numel() * ws.element_size()
+        return ws, _bytes(ws, device)
     need = dense_workspace_size(dims, op)
     return torch.empty(max(need, 16), dtype=torch.uint8, device=device), need
 

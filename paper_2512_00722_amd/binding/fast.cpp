@@ -136,6 +136,10 @@ bool caches(const at::Tensor* K, const at::Tensor* V) {
   if (args[i] != Py_None && !(name = plain(args[i]))) Py_RETURN_NONE
 #define EXPECT(x) \
   if (!(x)) Py_RETURN_NONE
+// all of its bytes its own memory (not a strided or expanded view)
+#define WORKSPACE(name, i) \
+  TENSOR(name, i);         \
+  EXPECT(name->is_contiguous())
 
 // Calls f without the GIL.  The arguments, the tensors' pointers among them, are
 // evaluated by the caller, so no tensor is touched while other threads run; an
@@ -165,7 +169,7 @@ PyObject* fast_attn(PyObject*, PyObject* const* args, Py_ssize_t n) {
   TENSOR_OR_NONE(idx, 4);
   TENSOR(out, 6);
   TENSOR_OR_NONE(lse, 7);
-  TENSOR(ws, 8);
+  WORKSPACE(ws, 8);
   spec_dims d = base_dims();
   bool ok;
   EXPECT(as_float(args[5], &d.scale));
@@ -209,7 +213,7 @@ PyObject* fast_score(PyObject*, PyObject* const* args, Py_ssize_t n) {
   TENSOR(K_r, 1);
   TENSOR(seq_lens, 2);
   TENSOR(out, 5);
-  TENSOR(ws, 6);
+  WORKSPACE(ws, 6);
   spec_dims d = base_dims();
   bool ok;
   int32_t n_sets;
@@ -246,7 +250,7 @@ PyObject* fast_topk(PyObject*, PyObject* const* args, Py_ssize_t n) {
   TENSOR(ks, 2);
   TENSOR(idx, 4);
   TENSOR(counts, 5);
-  TENSOR(ws, 6);
+  WORKSPACE(ws, 6);
   spec_dims d = base_dims();
   bool ok;
   EXPECT(as_int(args[3], &d.k_max));
@@ -282,7 +286,7 @@ PyObject* fast_step(PyObject*, PyObject* const* args, Py_ssize_t n) {
   TENSOR(q, 4);
   TENSOR(K, 5);
   TENSOR(V, 6);
-  TENSOR(ws, 14);
+  WORKSPACE(ws, 14);
   spec_dims d = base_dims();
   bool ok;
   EXPECT(as_int(args[7], &d.k_max) && as_float(args[9], &d.scale_r) &&
@@ -367,7 +371,7 @@ PyObject* fast_retrieval_qk(PyObject*, PyObject* const* args, Py_ssize_t n) {
   TENSOR(w_k, 4);
   TENSOR(K_r, 5);
   TENSOR(q_r, 11);
-  TENSOR(ws, 12);
+  WORKSPACE(ws, 12);
   spec_frontend fe = {};
   bool ok;
   EXPECT(as_float(args[6], &fe.rope_base) && as_float(args[7], &fe.yarn_scale) &&
@@ -408,7 +412,7 @@ PyObject* fast_mla(PyObject*, PyObject* const* args, Py_ssize_t n) {
   TENSOR(counts, 5);
   TENSOR(out, 7);
   TENSOR_OR_NONE(lse, 8);
-  TENSOR(ws, 9);
+  WORKSPACE(ws, 9);
   spec_mla_dims d = {};
   bool ok;
   EXPECT(as_float(args[6], &d.scale));
@@ -476,7 +480,7 @@ PyObject* fast_window_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
   TENSOR(lens, 3);
   TENSOR(out, 7);
   TENSOR_OR_NONE(lse, 8);
-  TENSOR(ws, 9);
+  WORKSPACE(ws, 9);
   bool ok;
   void* stream = as_stream(args[10], &ok);
   EXPECT(ok && dense_queries(q, K, V, out, lse, false));
@@ -499,7 +503,7 @@ PyObject* fast_window(PyObject*, PyObject* const* args, Py_ssize_t n) {
   TENSOR_OR_NONE(q_lens, 4);
   TENSOR(out, 8);
   TENSOR_OR_NONE(lse, 9);
-  TENSOR(ws, 10);
+  WORKSPACE(ws, 10);
   bool ok;
   void* stream = as_stream(args[11], &ok);
   EXPECT(ok && dense_queries(q, K, V, out, lse, true));
@@ -528,7 +532,7 @@ PyObject* fast_prefix_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
   TENSOR_OR_NONE(plen, 6);
   TENSOR(out, 8);
   TENSOR_OR_NONE(lse, 9);
-  TENSOR(ws, 10);
+  WORKSPACE(ws, 10);
   bool ok;
   void* stream = as_stream(args[11], &ok);
   EXPECT(ok && dense_queries(q, K, V, out, lse, false));
@@ -564,7 +568,7 @@ PyObject* fast_accum_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
   TENSOR(weights, 4);
   TENSOR(out, 6);
   TENSOR_OR_NONE(lse, 7);
-  TENSOR(ws, 8);
+  WORKSPACE(ws, 8);
   bool ok;
   void* stream = as_stream(args[9], &ok);
   EXPECT(ok && dense_queries(q, K, V, out, lse, false) && per_set(weights, at::kFloat, *K));
@@ -593,7 +597,7 @@ PyObject* fast_evict(PyObject*, PyObject* const* args, Py_ssize_t n) {
   TENSOR_OR_NONE(k_new, 7);
   TENSOR_OR_NONE(v_new, 8);
   TENSOR_OR_NONE(n_new, 9);
-  TENSOR(ws, 12);
+  WORKSPACE(ws, 12);
   bool ok;
   void* stream = as_stream(args[13], &ok);
   EXPECT(ok && caches(K, V) && per_set(weights, at::kFloat, *K) &&

@@ -52,3 +52,16 @@ def test_strides_of_single_entries_mean_nothing():
         spec.workspace_size(spec._dims_llm(q, K, 16, 0.0), spec.OP_ATTN)
     K_r = strided_calls.loose(torch.zeros((1, 40, 8, 64), dtype=torch.bfloat16), 0)
     spec.workspace_size(spec._dims_retrieval(K_r, 40, 16, 0.0), spec.OP_SCORE)
+
+
+@pytest.mark.parametrize("name", [n for n in strided_calls.NAMES if n != "gather"])
+def test_workspaces_are_whole_device_memory(name):
+    """A strided or expanded view holds fewer bytes than it counts, and a host tensor
+    none that a kernel may touch."""
+    with FakeTensorMode():
+        a = strided_calls.tensors("cuda")
+        for ws in (a["ws"][:1].expand(1 << 24), a["ws"][::2],
+                   torch.zeros(1 << 24, dtype=torch.uint8)):
+            b = dict(a, ws=ws)
+            with pytest.raises(ValueError, match="ws must be"):
+                strided_calls.calls(b)[name][1]()

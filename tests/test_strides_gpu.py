@@ -68,3 +68,12 @@ def test_strides_of_single_entries_mean_nothing(dev):
     for buffers in (True, False):
         for a, b in zip(run(*kv, *pre, buffers), want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("name", [n for n in strided_calls.NAMES if n != "gather"])
+def test_workspaces_are_whole_device_memory(dev, name):
+    announce(f"workspace views, {name}")
+    a = strided_calls.tensors(dev)
+    for ws in (a["ws"][:1].expand(1 << 24), a["ws"][::2], torch.zeros(1 << 24, dtype=torch.uint8)):
+        with pytest.raises(ValueError, match="ws must be"):
+            strided_calls.calls(dict(a, ws=ws))[name][1]()
