@@ -464,7 +464,17 @@ SPEC_API spec_status spec_mla_workspace_size(const spec_mla_dims* dm, size_t* by
  * alignment, errors, SPEC_DEBUG), with these differences: H_q / H_kv = G may be
  * any number up to 128, H_kv any number, and the workspace must be of the size
  * that spec_dense_workspace_size() gives.  NaNs and infinities reach the queries
- * that see their rows, and no others.                                         */
+ * that see their rows, and no others.
+ *
+ * The decode entry points take the query heads of a KV head together, up to 16 at
+ * once: above 16 in groups of G's largest divisor up to 16, each of which reads the
+ * caches anew.  A G that has none (17, 34, 37 ..) costs a pass for every head or two.
+ *
+ * Sizes beyond a launch give SPEC_ERR_UNSUPPORTED: B, n_layers or H_kv above 65535;
+ * n_layers B H_kv above 2^21; n_layers B H_q (spec_window_attn: times T) above 2^26;
+ * for the decode entry points more than 2^22 such groups of query heads; for
+ * spec_accum_decode_attn n_layers B n_sets L_cap above 2^29; L_cap + T or P_cap above
+ * 2^31 - 4097.                                                                */
 typedef struct spec_dense_dims {
   int32_t B;         /* sequences in the batch                                 */
   int32_t L_cap;     /* token capacity of every cache row                      */

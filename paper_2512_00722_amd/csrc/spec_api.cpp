@@ -372,7 +372,8 @@ spec_status resolve_dense(const spec_dense_dims* dm, spec_dense_op op, spec::Den
     return SPEC_ERR_UNSUPPORTED;
   if (dm->B > 65535 || dm->n_layers > 65535 || dm->H_kv > 65535) return SPEC_ERR_UNSUPPORTED;
   // Launch grids: at most 2^26 query rows, 2^21 KV heads or token sets, 2^22 column
-  // groups of a decode launch, and 2^23 workgroups over the weights.
+  // groups of a decode launch, and 2^29 accumulated weights (workgroups of 64 tokens at
+  // least; a weight stands for 512 bytes of K and V or more, so that more do not fit).
   const int64_t lb = (int64_t)dm->n_layers * dm->B;
   if (lb * dm->H_kv > 1 << 21) return SPEC_ERR_UNSUPPORTED;
   if (!evict && lb * dm->H_q > 1 << 26) return SPEC_ERR_UNSUPPORTED;
@@ -380,7 +381,7 @@ spec_status resolve_dense(const spec_dense_dims* dm, spec_dense_op op, spec::Den
   if (!evict && op != SPEC_DENSE_WINDOW &&
       lb * dm->H_q / spec::group_heads(dm->H_q / dm->H_kv) > 1 << 22)
     return SPEC_ERR_UNSUPPORTED;
-  if (op == SPEC_DENSE_ACCUM_DECODE && lb * dm->n_sets * (dm->L_cap / 64 + 1) > 1 << 23)
+  if (op == SPEC_DENSE_ACCUM_DECODE && lb * dm->n_sets * dm->L_cap > 1 << 29)
     return SPEC_ERR_UNSUPPORTED;
   if ((int64_t)dm->L_cap + dm->T > INT32_MAX - 4096 || dm->P_cap > INT32_MAX - 4096)
     return SPEC_ERR_UNSUPPORTED;
