@@ -190,9 +190,9 @@ __global__ __launch_bounds__(NT) void evict_plan_kernel(EvictKernelArgs a) {
   const int tid = threadIdx.x, wave = tid >> 6;
   const int4 hd = plan_head(a, set, MOVE);
   const int c = hd.x, E = hd.y, after = hd.z, taken = after - E;
+  // hd.w + taken: the new rows (x.n_new may be the counts, which are rewritten by now)
   const int64_t recent_from =
-      (int64_t)(MOVE ? a.pos : a.x.pos)[b] +
-      (a.x.n_new ? clampi(a.x.n_new[b], 0, a.T) : a.T) - a.n_recent;
+      (int64_t)(MOVE ? a.pos : a.x.pos)[b] + hd.w + taken - a.n_recent;
   int32_t* dst = a.dst + (size_t)set * a.L_cap;
   int32_t* src = a.src + (size_t)set * a.L_cap;
 
@@ -343,8 +343,7 @@ __global__ __launch_bounds__(kRadixThreads) void evict_plan_long_kernel(EvictKer
   const int32_t* tok = a.x.tokens + (size_t)set * a.L_cap;
   int32_t* dst = a.dst + (size_t)set * a.L_cap;
   int32_t* src = a.src + (size_t)set * a.L_cap;
-  const int64_t recent_from =
-      (int64_t)a.x.pos[b] + (a.x.n_new ? clampi(a.x.n_new[b], 0, a.T) : a.T) - a.n_recent;
+  const int64_t recent_from = (int64_t)a.x.pos[b] + hd.w + taken - a.n_recent;
 
   if (E == c || E == 0) {  // all stay, or none: no selection
     for (int i = tid; i < taken; i += NT) dst[i] = E + i;
