@@ -464,7 +464,8 @@ SPEC_API spec_status spec_mla_workspace_size(const spec_mla_dims* dm, size_t* by
  * alignment, errors, SPEC_DEBUG), with these differences: H_q / H_kv = G may be
  * any number up to 128, H_kv any number, and the workspace must be of the size
  * that spec_dense_workspace_size() gives.  NaNs and infinities reach the queries
- * that see their rows, and no others.
+ * that see their rows, and no others.  A token whose logit is -inf counts as one that
+ * the query does not see.
  *
  * The decode entry points take the query heads of a KV head together, up to 16 at
  * once: above 16 in groups of G's largest divisor up to 16, each of which reads the

@@ -96,7 +96,9 @@ constexpr int tile_elems(bool half) { return half ? kTileElems / 2 : kTileElems;
 
 // A wavefront's share token by token, without the matrix cores, for the rare sums that
 // hold an infinity or a NaN: an infinity times a weight's parts is not that times the
-// weight.  As decode_unit leaves them, l_run not yet added up over a head's lanes.
+// weight, and a token whose logit is -inf counts for nothing, whatever its row of V holds
+// (in a part of nothing but such tokens as well, which joins leave out).  As decode_unit
+// leaves them, l_run not yet added up over a head's lanes.
 __device__ __forceinline__ void unit_by_token(const DecodeUnit& u, float& m_run, float& l_run,
                                               floatx4 (&acc)[8]) {
   const int lane = threadIdx.x & 63, r16 = lane & 15, kg = lane >> 4;
@@ -130,7 +132,8 @@ __device__ __forceinline__ void unit_by_token(const DecodeUnit& u, float& m_run,
       for (int db = 0; db < 8; ++db) {
         const floatx4 y = four(u.v + off + 16 * db);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[db][i] = fmaf(acc[db][i], alpha, p * y[i]);
+        for (int i = 0; i < 4; ++i)
+          acc[db][i] = fmaf(acc[db][i], alpha, s == -INFINITY ? 0.f : p * y[i]);
       }
     }
   }

@@ -76,9 +76,9 @@ __device__ __forceinline__ Range window_range(const TileArgs& a, int p0, int i0,
 }
 
 // The same token by token, for the rare sums that hold infinities or NaNs: of rows that
-// a query does not see, they are selected away.  The wavefront's tokens are j0 .. j0 + run
-// - 1 and those `step` further on, up to j1.  A lane has the dimensions 32 db + 8 e + 4 kg
-// .. + 3 of its row, as the accumulators do.
+// a query does not see, or whose logit is -inf, they are selected away.  The wavefront's
+// tokens are j0 .. j0 + run - 1 and those `step` further on, up to j1.  A lane has the
+// dimensions 32 db + 8 e + 4 kg .. + 3 of its row, as the accumulators do.
 template <bool WINDOW, class TokenOf>
 __device__ __forceinline__ void attend_by_token(const TileArgs& a, const uint16_t* q,
                                                 const uint16_t* k, const uint16_t* v, int64_t rs,
@@ -123,7 +123,7 @@ __device__ __forceinline__ void attend_by_token(const TileArgs& a, const uint16_
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         acc[e >> 2][4 * (e & 3) + i] =
-            acc[e >> 2][4 * (e & 3) + i] * alpha + (see ? p * y[i] : 0.f);
+            acc[e >> 2][4 * (e & 3) + i] * alpha + (s == -INFINITY ? 0.f : p * y[i]);
     }
   }
 }
@@ -390,9 +390,9 @@ void tile_attn_kernel(TileArgs a) {
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));  // loads past the last tile, before LDS is
   __syncthreads();                            // used anew or given back
   // Where an infinity or a NaN got into the sums, they are taken again without the matrix
-  // cores: a weight of 0 does not keep one of a row that this query does not see out of
-  // them (0 x NaN), nor is an infinity of one that it sees the product with a weight's
-  // parts.
+  // cores: a weight of 0 does not keep one of a row that this query does not see, or whose
+  // logit is -inf, out of them (0 x NaN), nor is an infinity of one that it sees the
+  // product with a weight's parts.
   {
     float odd = 0.f;
 #pragma unroll
