@@ -548,7 +548,10 @@ SPEC_API spec_status spec_window_attn(const spec_dense_dims* dm, const uint16_t*
  * [n_layers][P_cap][H_kv][d] and then the L_b = seq_lens[b] rows of its own cache,
  * one softmax over both.  The prefix is read once for the whole batch.  q, out,
  * lse and the own caches as for spec_window_decode_attn.  P = L_b = 0 gives out
- * = 0 and lse = -inf.                                                          */
+ * = 0 and lse = -inf.  fp32 accumulation; over the prefix the softmax weights enter
+ * the matrix cores as three bf16 numbers (2^-26) where B H_q / H_kv is 32 or less, as
+ * two (2^-17) above, so that a sequence's results depend on the size of the batch in
+ * their last bits.                                                              */
 SPEC_API spec_status spec_prefix_decode_attn(const spec_dense_dims* dm, const uint16_t* q,
                                 const uint16_t* k_prefix, const uint16_t* v_prefix,
                                 const int32_t* prefix_len, const uint16_t* k_cache,

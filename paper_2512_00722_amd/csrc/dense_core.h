@@ -246,9 +246,9 @@ __device__ __forceinline__ void decode_unit(const DecodeUnit& u, uint16_t* V, fl
     }
 #pragma unroll
     for (int db = 0; db < 8; ++db) acc[db] *= alpha;
-    // Weights enter as three bf16 numbers, 2^-26 relative: a pair's 2^-18 would be most of
-    // the result's error, and the third is free in a kernel bound by memory (321 us with
-    // either; 32 layers x 8 sequences x 2048 tokens).
+    // Weights enter as three bf16 numbers, 2^-26 relative at most: a pair's 2^-17 would be
+    // most of the result's error over some thousand tokens, and the third is free in a kernel
+    // bound by memory (321 us with either; 32 layers x 8 sequences x 2048 tokens).
     const bf16x8 ph = to_bf16x8(p), pl = next_bf16x8(p, ph), pt = next_bf16x8(p, pl);
     wave_sync_lds();
     if constexpr (HALF) {

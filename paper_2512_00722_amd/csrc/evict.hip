@@ -15,10 +15,10 @@
 // thread keeps the keys of a run of consecutive slots in registers, and the E-th
 // largest key is found from counts in LDS of its digits of 11, 11 and 10 bits, done
 // early once the keys that share the digits found all stay (32 sets of 8192 slots:
-// the plan takes 13 us).  Where only a few rows go, as in a decode step, they are
-// searched for one after another instead (2048 sets of 2048 slots: 12.8 us in all,
-// 24.1 by digits).  Many new rows are moved by a launch of its own at the rate of a
-// copy (32 sets x 512 rows of 4 KB: 29 us, 4.6 TB/s).
+// the plan takes 11.5 us).  Where only a few rows go, as in a decode step, they are
+// searched for one after another instead (2048 sets of 2048 slots, one row: 15.8 us a
+// call, 27.8 by digits; the launch alone 13.1).  Many new rows are moved by a launch of
+// its own at the rate of a copy (32 sets x 512 rows of 4 KB: 27.5 us, 4.9 TB/s).
 #include <type_traits>
 
 #include "device_common.h"
@@ -167,8 +167,8 @@ __device__ __forceinline__ int sum_of(const int* v) {
 }
 
 // Rows that go which are searched for one by one: eight take as long as the digits do
-// (us, 2048 sets of 2048 slots: 1 14.7, 4 19.4, 8 25.2 against 28.0; of 8192: 38, 46, 56
-// against 54).
+// (us a call, 2048 sets of 2048 slots: 1 row 15.8, 4 20.5, 6 24, 8 27.5 against 27 to 30; 512
+// sets of 8192: 17, 21, 23, 25.4 against 24).
 constexpr int kFewEvicted = 6;
 
 constexpr int kDigitBins = 2048;
@@ -431,9 +431,9 @@ size_t list_bytes(const DenseDims& d, int64_t sets) {
 constexpr int kMoveInPlan = 32;
 
 // Slots of a thread: few enough that its loads are in flight together, and as many
-// threads as leave other workgroups their places (us: 2048 sets of 8192 slots, one new row,
-// by 256 threads 54.4, 512 37.1, 1024 52; 64 such sets of which 8 rows go 19.7, 15.5, 15.1;
-// 2048 sets of 2048 slots by 128 threads 15.5, 256 14.6, 512 19.5).
+// threads as leave other workgroups their places (us a call, one new row: 2048 sets of 2048
+// slots by 128 threads 16.9, 256 15.8, 512 19.9; 512 sets of 8192 by 256 threads 23.9, 512
+// 17.2, 1024 18.7; 32 sets of 8192 12.7, 9.9, 9.5).
 template <bool MOVE>
 void launch_plan(int64_t sets, const EvictKernelArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)sets);

@@ -150,10 +150,12 @@ __device__ __forceinline__ void load_to_lds(const void* g, const void* lds) {
 
 // RW x TW wavefronts: RW groups of 32 rows, TW parts of each tile's tokens.
 // WINDOW: masked rows of a sequence; else every row sees all tokens.  SPLITP:
-// weights as a bf16 pair (~2^-18 relative) for fp32 results, or with few rows, which
+// weights as a bf16 pair (2^-17 relative) for fp32 results, or with few rows, which
 // leave the matrix cores idle, as three bf16 numbers (2 % of the time of 32 rows, but 9 %
-// of that of 64 and 13 % of that of 256); else rounded to bf16 once (2^-9), which the
-// rounding of a bf16 result hides.
+// of that of 64 and 13 % of that of 256); else rounded to bf16 once (2^-8), as the result
+// is, for that takes the matrix cores: 2 x 4096 tokens 277 us, with a pair 373; 8192, window
+// 1024, 157 and 205; 5 x 257 at most 24.1 and 27.3.  It makes the error of the whole output
+// 2.3e-3 (root of mean squares) instead of the 1.7e-3 of rounding the exact one.
 template <int RW, int TW, int TOK, bool WINDOW, bool SPLITP>
 __global__ __launch_bounds__(RW* TW * 64) __attribute__((amdgpu_waves_per_eu(TOK == 64 ? 2 : 1)))
 void tile_attn_kernel(TileArgs a) {
@@ -161,9 +163,11 @@ void tile_attn_kernel(TileArgs a) {
   constexpr int NB = TOK / (32 * TW);      // 32-token blocks of a wavefront
   constexpr int LD = TOK / 4 / (RW * TW);  // loads of a wavefront for K, and for V: 4 rows each
   // Tiles in LDS: a workgroup of eight wavefronts is alone on its CU, with room for a third
-  // (2 x 4096 tokens not in the caches: 302 us, with two 307), and 64 rows on a prefix,
-  // which wait for memory, are faster so than two workgroups of two stages (2 layers of
-  // 20011 tokens, 16 sequences: 60.0 us, 62.9).
+  // (2 x 4096 tokens not in the caches: 302 us, with two 307), and 64 rows on a long prefix,
+  // which wait for memory, are faster so than two workgroups of two stages (us, 16
+  // sequences: 8 layers of 32768 tokens 266, with two stages 291; one of 65536 70 and 76; 2
+  // of 20011 63.8 and 66.7; one of 1000 14.6 and 14.6; slower where the own tokens are many
+  // beside it, 4 of 16384 and 1024 own ones 116 and 110, one of 4096 and 777 28.4 and 25.4).
   constexpr int STAGES = RW * TW == 8 || (!WINDOW && RW == 2) ? 3 : 2;
   __shared__ __align__(16) uint16_t lds[STAGES][2][TOK * kD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -536,6 +540,10 @@ struct TilePlan {
   int rows, tok, n_rt, n_split, split_tok;
 };
 
+// Tokens of a part at least.  us with 128 / 256 / 512: 4 sequences on a prefix of 500
+// tokens 11.7 / 12.9 / 15.5, 1000 13.8 / 14.0 / 16.8, 2000 14.9 / 16.3 / 18.7, 4000 20.7 /
+// 17.0 / 20.4; 16 sequences on 4000 23.0 / 18.7 / 20.8; 16 queries over 4096 tokens 17.4 /
+// 17.3 / 19.6.
 constexpr int kMinSplit = 256;
 
 // Splits a row tile's `most` tokens into about n parts.
@@ -630,7 +638,14 @@ TilePlan window_plan(const DenseDims& d) {
 }
 
 // Prefix: units are (layer, KV head), rows the batch's query rows of a unit.  Few
-// rows fill the chip by splits of the prefix alone.
+// rows fill the chip by splits of the prefix alone: into a workgroup per CU, or two of 128
+// rows, which share one.  us, 2 layers of 20011 tokens, rows of a workgroup / workgroups
+// per CU:
+//    64 query rows   64/1  49   64/2  59  128/1  58  128/2  55  256/1  70
+//    96              64/1  68   64/2  81  128/1  71  128/2  62  256/1  74
+//   136              64/2 110             128/1 106  128/2  80  256/1  81  256/2  95
+//   256              64/1 111  64/2 120   128/1  99  128/2  93  256/1  91  256/2 115
+//   264              64/2 160             128/1 136  128/2 122  256/1 126  256/2 139
 TilePlan prefix_plan(const DenseDims& d) {
   const int64_t units = (int64_t)d.n_layers * d.H_kv, rows = (int64_t)d.B * d.G;
   TilePlan p{};
@@ -638,7 +653,7 @@ TilePlan prefix_plan(const DenseDims& d) {
   p.tok = p.rows == 32 ? 128 : 64;
   p.n_rt = (int)((rows + p.rows - 1) / p.rows);
   const int64_t wgs = units * p.n_rt;
-  const int64_t target = p.rows == 128 ? 2 * kCUs : kCUs;  // workgroups: two share a CU, or one
+  const int64_t target = p.rows == 128 ? 2 * kCUs : kCUs;
   int64_t ns = (target + wgs - 1) / wgs;
   const int64_t cap = ((int64_t)d.P_cap + kMinSplit - 1) / kMinSplit;
   if (ns > cap) ns = cap;
@@ -678,9 +693,10 @@ hipError_t launch_window(const DenseDims& d, const uint16_t* q, const uint16_t* 
 namespace {
 
 // The own tokens' workgroups, of as many wavefronts as the tiles': hb column groups each,
-// over n_split of them.  Four groups side by side where that leaves a workgroup per CU
-// (16 sequences of 777 tokens at most on a prefix of 20011 58.5 -> 57.6 us, 64 of 1024 on
-// one of 32768 321 -> 312), and a few chunks to a wavefront.
+// over n_split of them.  Four groups side by side where that leaves a workgroup per CU,
+// and a few chunks to a wavefront (us with four groups, and one: 2 layers of 20011 tokens
+// and 16 sequences of 777 64.8 and 67.2, 4 of 16384 and 32 of 512 127 and 138, 4 of 32768
+// and 64 of 1024 398 and 409, one of 4096 and 16 of 777 29.0 and 28.4).
 struct OwnPlan {
   int hb, n_split;
 };
