@@ -601,6 +601,108 @@ SPEC_API spec_status spec_evict(const spec_dense_dims* dm, const spec_bounded* c
                                 const uint16_t* v_new, const int32_t* n_new, void* ws,
                                 size_t ws_bytes, spec_stream stream);
 
+/* ---- caches held in 4 or 8 bits -----------------------------------------------
+ * KV caches whose rows are held in groups of 32 along the head dimension, as
+ * elements of 4 or 8 bits times a power of two per group (the microscaling formats
+ * whose elements are e2m1 and e4m3 and whose scales are e8m0).  With A the largest
+ * magnitude of a group,
+ *     x^ = 2^X e(x 2^-X),  X the least integer with A <= 7 2^X (4 bits) or 448 2^X (8),
+ * where e() rounds to the nearest element, ties to the even one, and beyond the
+ * largest, 6 or 448, gives that: no element is off by more than half the spacing of
+ * the elements at its magnitude.  X is clamped to [-111, 125] (8 bits: [-111, 119]).  A
+ * group that holds a NaN or an infinity is NaN throughout.  Every x^ is a bf16 number (bytes
+ * that spec_quant_append does not write may stand for others: they are rounded to bf16).
+ *     k, v    uint8 [n_layers][B][L_cap][H_kv][d bits / 8]: byte i of 4-bit rows holds
+ *             dimension 2 i in its low half (sign, two bits of exponent, one of mantissa)
+ *             and 2 i + 1 in its high half;
+ *     scales  uint8 [n_layers][B][L_cap][H_kv][2][d / 32]: X + 127 (255: NaN) of the
+ *             groups of the token's K and then of its V.
+ * All bytes of such tensors are valid.  The conventions above hold, with the
+ * differences of the entry points over caches read in full (any G up to 128, any
+ * H_kv, workspaces of the size that spec_quant_workspace_size() gives).  k and v must
+ * be 16-byte aligned and scales 8-byte aligned, and their strides multiples of that.
+ *
+ * Sizes beyond a launch give SPEC_ERR_UNSUPPORTED: those of the decode entry points
+ * above (B, n_layers or H_kv above 65535; n_layers B H_kv above 2^21; n_layers B H_q above
+ * 2^26; more than 2^22 groups of query heads), L_cap or T above 2^30, and for
+ * spec_quant_append and spec_quant_read n_layers B ceil(n H_kv / 64) above 2^24 - 1 for
+ * n = T or k_max.                                                                */
+typedef struct spec_quant_dims {
+  int32_t B;         /* sequences in the batch                                 */
+  int32_t L_cap;     /* token capacity of every cache row                      */
+  int32_t n_layers;  /* layers of the call                                     */
+  int32_t H_q;       /* query heads (decode entry points)                      */
+  int32_t H_kv;      /* KV heads; query head h reads KV head h / (H_q / H_kv)  */
+  int32_t d;         /* head dimension (128)                                   */
+  int32_t bits;      /* 4 or 8                                                 */
+  int32_t T;         /* spec_quant_append: new tokens per sequence, > 0        */
+  int32_t window;    /* spec_quant_decode_attn: tokens that the query sees, itself
+                        included, > 0 (L_cap or more: all before it)           */
+  int32_t n_sink;    /* ... and first tokens that stay visible, >= 0           */
+  int32_t k_max;     /* spec_quant_sparse_decode_attn, spec_quant_read: row length
+                        of idx, > 0, <= L_cap (without idx: rows of the outputs) */
+  int32_t n_sets;    /* token sets per sequence of idx: 1 or H_kv              */
+  int64_t kv_stride_layer;    /* bytes between layers of k/v; 0 = B*kv_stride_b */
+  int64_t kv_stride_b;        /* bytes between sequences; 0 = dense            */
+  int64_t scale_stride_layer; /* bytes between layers of scales; 0 = B*scale_stride_b */
+  int64_t scale_stride_b;     /* bytes between sequences; 0 = dense            */
+  float scale;       /* softmax scale; 0 = 1/sqrt(d)                           */
+  int32_t reserved;  /* must be 0                                              */
+} spec_quant_dims;
+
+/* The caches (host struct of device pointers).                               */
+typedef struct spec_quant_cache {
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* scales;
+} spec_quant_cache;
+
+typedef enum spec_quant_op {
+  SPEC_QUANT_APPEND = 0,
+  SPEC_QUANT_READ = 1,
+  SPEC_QUANT_DECODE = 2,
+  SPEC_QUANT_SPARSE_DECODE = 3
+} spec_quant_op;
+
+/* Workspace bytes of a quantised cache's entry point (0 where it takes none).
+ * Returns the same validation status as the entry point itself.               */
+SPEC_API spec_status spec_quant_workspace_size(const spec_quant_dims* dm, spec_quant_op op,
+                                size_t* bytes);
+
+/* Quantises the rows of n_b = n_new[b] (NULL: T) new tokens into the caches, token i at
+ * row pos[b] + i where that lies in [0, L_cap) (others are not written; rows that no
+ * new token has are left as they were).  k_new, v_new [n_layers][B][T][H_kv][d] bf16, pos,
+ * n_new [B] int32.  No workspace.                                              */
+SPEC_API spec_status spec_quant_append(const spec_quant_dims* dm, const spec_quant_cache* cache,
+                                const uint16_t* k_new, const uint16_t* v_new,
+                                const int32_t* pos, const int32_t* n_new, spec_stream stream);
+
+/* Reads rows back: for j < counts[b]
+ *     k_out[l,b,j,g,:] = K^[l,b,t,g,:],  v_out likewise,
+ * with t = idx[b,s,j] (s = 0 for n_sets = 1 and s = g for n_sets = H_kv; clamped into
+ * [0, L_cap)), or t = j where idx is NULL.  k_out, v_out [n_layers][B][k_max][H_kv][d] bf16,
+ * exact; rows j >= counts[b] are left as they were.  The outputs are what compact-mode
+ * spec_sparse_decode_attn and spec_window_attn read.  No workspace.            */
+SPEC_API spec_status spec_quant_read(const spec_quant_dims* dm, const spec_quant_cache* cache,
+                                const int32_t* idx, const int32_t* counts, uint16_t* k_out,
+                                uint16_t* v_out, spec_stream stream);
+
+/* Decode attention with a sliding window and sinks over a quantised cache: as
+ * spec_window_decode_attn over K^ and V^, which are formed in registers.       */
+SPEC_API spec_status spec_quant_decode_attn(const spec_quant_dims* dm, const uint16_t* q,
+                                const spec_quant_cache* cache, const int32_t* seq_lens,
+                                float* out, float* lse, void* ws, size_t ws_bytes,
+                                spec_stream stream);
+
+/* Decode attention over selected rows of a quantised cache: as indexed-mode
+ * spec_sparse_decode_attn over K^ and V^, j < counts[b] (clamped into [0, k_max]), idx
+ * [B][n_sets][k_max] int32 (clamped into [0, L_cap); an index may occur again, and
+ * counts again).                                                               */
+SPEC_API spec_status spec_quant_sparse_decode_attn(const spec_quant_dims* dm, const uint16_t* q,
+                                const spec_quant_cache* cache, const int32_t* idx,
+                                const int32_t* counts, float* out, float* lse, void* ws,
+                                size_t ws_bytes, spec_stream stream);
+
 /* Workspace bytes needed by `op` for dimensions `dm` (0 for SPEC_OP_GATHER).
  * Returns the same validation status as the op itself.                      */
 SPEC_API spec_status spec_workspace_size(const spec_dims* dm, spec_op op,

@@ -32,6 +32,9 @@ __all__ = [
     "DenseDims", "dense_workspace_size", "window_decode_attn", "window_attn",
     "prefix_decode_attn", "accum_decode_attn", "evict", "DENSE_WINDOW_DECODE", "DENSE_WINDOW",
     "DENSE_PREFIX_DECODE", "DENSE_ACCUM_DECODE", "DENSE_EVICT",
+    "QuantDims", "QuantCache", "quant_workspace_size", "quant_append", "quant_read",
+    "quant_decode_attn", "quant_sparse_decode_attn", "QUANT_APPEND", "QUANT_READ",
+    "QUANT_DECODE", "QUANT_SPARSE_DECODE",
     "EXPORTED_SYMBOLS",
 ]
 
@@ -42,6 +45,7 @@ lib_path = os.path.join(_PKG, "libspecctx.so")
  OP_STEP_NOALLOC) = range(9)
 (DENSE_WINDOW_DECODE, DENSE_WINDOW, DENSE_PREFIX_DECODE, DENSE_ACCUM_DECODE,
  DENSE_EVICT) = range(5)
+QUANT_APPEND, QUANT_READ, QUANT_DECODE, QUANT_SPARSE_DECODE = range(4)
 STATUS = {0: "SPEC_OK", 1: "SPEC_ERR_INVALID", 2: "SPEC_ERR_UNSUPPORTED",
           3: "SPEC_ERR_WORKSPACE", 4: "SPEC_ERR_HIP", 5: "SPEC_ERR_TOO_LARGE"}
 
@@ -52,6 +56,8 @@ EXPORTED_SYMBOLS = ["spec_score", "spec_topk", "spec_gather", "spec_sparse_decod
                     "spec_mla_sparse_decode_attn", "spec_mla_workspace_size", "spec_workspace_size",
                     "spec_dense_workspace_size", "spec_window_decode_attn", "spec_window_attn",
                     "spec_prefix_decode_attn", "spec_accum_decode_attn", "spec_evict",
+                    "spec_quant_workspace_size", "spec_quant_append", "spec_quant_read",
+                    "spec_quant_decode_attn", "spec_quant_sparse_decode_attn",
                     "spec_status_string", "spec_last_hip_error", "spec_version"]
 
 
@@ -147,12 +153,36 @@ class Bounded(ctypes.Structure):
                 ("tokens", ctypes.c_void_p), ("counts", ctypes.c_void_p)]
 
 
+class QuantDims(ctypes.Structure):
+    """Mirror of `spec_quant_dims`."""
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("B", "L_cap", "n_layers", "H_q", "H_kv", "d", "bits", "T", "window", "n_sink",
+                 "k_max", "n_sets")] + [
+        (n, ctypes.c_int64) for n in ("kv_stride_layer", "kv_stride_b", "scale_stride_layer",
+                                      "scale_stride_b")] + [
+        ("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+    @classmethod
+    def make(cls, B, L_cap, n_layers=1, H_q=8, H_kv=8, d=128, bits=4, T=1, window=0, n_sink=0,
+             k_max=0, n_sets=1, kv_stride_layer=0, kv_stride_b=0, scale_stride_layer=0,
+             scale_stride_b=0, scale=0.0):
+        return cls(B, L_cap, n_layers, H_q, H_kv, d, bits, T, window, n_sink, k_max, n_sets,
+                   kv_stride_layer, kv_stride_b, scale_stride_layer, scale_stride_b, scale, 0)
+
+
+class QuantBuffers(ctypes.Structure):
+    """Mirror of `spec_quant_cache`."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
 _lib = None
 _fast = None  # native marshalling (binding/fast.cpp), loaded with the library if built
 # its entry points, in the order its init() takes their addresses
 _FAST_API = ["spec_score", "spec_topk", "spec_sparse_decode_attn", "spec_step",
              "spec_retrieval_qk", "spec_mla_sparse_decode_attn", "spec_window_decode_attn",
-             "spec_window_attn", "spec_prefix_decode_attn", "spec_accum_decode_attn", "spec_evict"]
+             "spec_window_attn", "spec_prefix_decode_attn", "spec_accum_decode_attn", "spec_evict",
+             "spec_quant_append", "spec_quant_read", "spec_quant_decode_attn",
+             "spec_quant_sparse_decode_attn"]
 
 
 def load_library(path: Optional[str] = None):
@@ -171,6 +201,8 @@ def load_library(path: Optional[str] = None):
     F = ctypes.POINTER(Frontend)
     M = ctypes.POINTER(MlaDims)
     N = ctypes.POINTER(DenseDims)
+    Q = ctypes.POINTER(QuantDims)
+    C = ctypes.POINTER(QuantBuffers)
     sig = {
         "spec_score": [D, P, P, P, P, P, S, P],
         "spec_topk": [D, P, P, P, P, P, P, S, P],
@@ -193,6 +225,11 @@ def load_library(path: Optional[str] = None):
         "spec_prefix_decode_attn": [N, P, P, P, P, P, P, P, P, P, P, S, P],
         "spec_accum_decode_attn": [N, P, P, P, P, P, P, P, P, S, P],
         "spec_evict": [N, ctypes.POINTER(Bounded), P, P, P, P, P, P, S, P],
+        "spec_quant_workspace_size": [Q, I, ctypes.POINTER(S)],
+        "spec_quant_append": [Q, C, P, P, P, P, P],
+        "spec_quant_read": [Q, C, P, P, P, P, P],
+        "spec_quant_decode_attn": [Q, P, C, P, P, P, P, S, P],
+        "spec_quant_sparse_decode_attn": [Q, P, C, P, P, P, P, P, S, P],
     }
     for name, args in sig.items():
         f = getattr(lib, name)
@@ -1155,3 +1192,242 @@ def evict(K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, tokens: torch
         _check(lib.spec_evict(ctypes.byref(dims), ctypes.byref(cache), _p(keep), _p(pos),
                               _p(k_new), _p(v_new), _p(n_new), _p(ws), nws, _stream(K)),
                "spec_evict")
+
+
+# ------------------------------------------------------------------ caches in 4 or 8 bits
+
+class QuantCache:
+    """KV caches held in 4 or 8 bits: elements times a power of two per 32 of them along
+    the head dimension (the formats are documented in include/spec.h).  The tensors, all
+    uint8 and of n_layers layers and B sequences:
+        k, v    [n_layers, B, L_cap, H_kv, d * bits / 8]   elements
+        scales  [n_layers, B, L_cap, H_kv, 2, d / 32]      K's and V's, 8 bytes together
+    They start as zeros.  The first two dims may be strided."""
+
+    def __init__(self, n_layers: int, B: int, L_cap: int, H_kv: int, d: int = 128, bits: int = 4,
+                 device="cuda"):
+        if bits not in (4, 8):
+            raise ValueError("bits must be 4 or 8")
+        if d != 128:
+            raise ValueError("d must be 128")
+        self._set(*(torch.zeros((n_layers, B, L_cap, H_kv, *last), dtype=torch.uint8,
+                                device=device)
+                    for last in ((d * bits // 8,), (d * bits // 8,), (2, d // 32))))
+
+    @classmethod
+    def of(cls, k: torch.Tensor, v: torch.Tensor, scales: torch.Tensor) -> "QuantCache":
+        """The caches that a program's own tensors hold; nothing is copied."""
+        for t, name, ndim in ((k, "k", 5), (v, "v", 5), (scales, "scales", 6)):
+            if not isinstance(t, torch.Tensor):
+                raise TypeError(f"{name} must be a tensor")
+            if t.dtype != torch.uint8:
+                raise TypeError(f"{name} must be {torch.uint8}, got {t.dtype}")
+            if t.dim() != ndim:
+                raise ValueError(f"{name} must have {ndim} dims, got shape {tuple(t.shape)}")
+        if k.shape[4] not in (64, 128):
+            raise ValueError("k must be [n_layers, B, L_cap, H_kv, 64 (4 bits) or 128 (8 bits)]")
+        if k.shape != v.shape or k.stride() != v.stride():
+            raise ValueError("k and v must have the same shape and strides")
+        if tuple(scales.shape) != (*k.shape[:4], 2, 4):
+            raise ValueError("scales must be [n_layers, B, L_cap, H_kv, 2, 4]")
+        if v.device != k.device or scales.device != k.device:
+            raise ValueError(f"v and scales must be on {k.device}")
+        _inner_contig(k, "k", 3)
+        _inner_contig(scales, "scales", 4)
+        self = cls.__new__(cls)
+        self._set(k, v, scales)
+        return self
+
+    def _set(self, k, v, scales):
+        self._k, self._v, self._scales = k, v, scales
+
+    k = property(lambda self: self._k)
+    v = property(lambda self: self._v)
+    scales = property(lambda self: self._scales)
+    bits = property(lambda self: self._k.shape[4] // 16)
+    device = property(lambda self: self._k.device)
+
+    def layers(self, start: int, stop: int) -> "QuantCache":
+        """Layers start .. stop - 1, the same memory."""
+        return QuantCache.of(self._k[start:stop], self._v[start:stop], self._scales[start:stop])
+
+
+def quant_workspace_size(dims: QuantDims, op: int) -> int:
+    lib = load_library()
+    n = ctypes.c_size_t(0)
+    _check(lib.spec_quant_workspace_size(ctypes.byref(dims), op, ctypes.byref(n)),
+           "spec_quant_workspace_size")
+    return int(n.value)
+
+
+def _quant_workspace(dims: QuantDims, op: int, device, ws: Optional[torch.Tensor]):
+    if ws is not None:
+        return ws, _bytes(ws, device)
+    need = quant_workspace_size(dims, op)
+    return torch.empty(max(need, 16), dtype=torch.uint8, device=device), need
+
+
+def _quant_dims(cache: QuantCache, **kw) -> QuantDims:
+    """The dims of a call on the caches, whose tensors are checked anew."""
+    if not isinstance(cache, QuantCache):
+        raise TypeError("cache must be a QuantCache")
+    QuantCache.of(cache.k, cache.v, cache.scales)
+    n_layers, B, L_cap, H_kv, width = cache.k.shape
+    return QuantDims.make(B=B, L_cap=L_cap, n_layers=n_layers, H_kv=H_kv, bits=width // 16,
+                          kv_stride_layer=_stride(cache.k, 0), kv_stride_b=_stride(cache.k, 1),
+                          scale_stride_layer=_stride(cache.scales, 0),
+                          scale_stride_b=_stride(cache.scales, 1), **kw)
+
+
+def _quant_buffers(cache: QuantCache) -> QuantBuffers:
+    if cache.k.device.type != "cuda":
+        raise ValueError("cache must be on a device")
+    return QuantBuffers(cache.k.data_ptr(), cache.v.data_ptr(), cache.scales.data_ptr())
+
+
+def quant_append(cache: QuantCache, k_new: torch.Tensor, v_new: torch.Tensor, pos: torch.Tensor,
+                 n_new: Optional[torch.Tensor] = None):
+    """Quantises new tokens' rows into the caches: row i < n_new[b] (None: T) of k_new/v_new
+    [n_layers, B, T, H_kv, d] bf16 becomes row pos[b] + i, where the caches have one.  pos,
+    n_new int32 [B].  Other rows stay as they are."""
+    lib = load_library()
+    if type(cache) is QuantCache and _native(k_new):
+        st = _fast.quant_append(cache._k, cache._v, cache._scales, k_new, v_new, pos, n_new,
+                                _raw_stream(k_new))
+        if st is not None:
+            _check(st, "spec_quant_append")
+            return
+    T = k_new.shape[2] if isinstance(k_new, torch.Tensor) and k_new.dim() == 5 else 1
+    dims = _quant_dims(cache, T=T)
+    for t, nm in ((k_new, "k_new"), (v_new, "v_new")):
+        _need(t, nm, torch.bfloat16, 5)
+        if tuple(t.shape) != (dims.n_layers, dims.B, T, dims.H_kv, dims.d) \
+                or not t.is_contiguous():
+            raise ValueError(f"{nm} must be contiguous [n_layers, B, T, H_kv, d]")
+    _i32(pos, "pos", dims.B)
+    if n_new is not None:
+        _i32(n_new, "n_new", dims.B)
+    _same_device(k_new, cache=cache.k, v_new=v_new, pos=pos, n_new=n_new)
+    c = _quant_buffers(cache)
+    with torch.cuda.device(k_new.device):
+        _check(lib.spec_quant_append(ctypes.byref(dims), ctypes.byref(c), _p(k_new), _p(v_new),
+                                     _p(pos), _p(n_new), _stream(k_new)), "spec_quant_append")
+
+
+def _quant_sets(idx: torch.Tensor, B: int, H_kv: int) -> int:
+    n_sets = _sets_of(idx, H_kv)
+    if idx.shape[0] != B or not idx.is_contiguous():
+        raise ValueError("idx must be contiguous [B, k_max] or [B, H_kv, k_max]")
+    return n_sets
+
+
+def quant_read(cache: QuantCache, counts: torch.Tensor, idx: Optional[torch.Tensor] = None,
+               out: Optional[tuple] = None):
+    """Rows of the caches in bf16: (K, V) [n_layers, B, k_max, H_kv, d] whose rows j < counts[b]
+    are the caches' rows idx[b, j] (idx int32 [B, k_max], or [B, H_kv, k_max] with one set
+    per KV head), or their rows j (idx None; k_max = L_cap, or what `out` has).  Rows
+    beyond counts[b] are left as they are (zero when the outputs are allocated here); `out`
+    takes preallocated contiguous outputs."""
+    lib = load_library()
+    if out is not None and type(cache) is QuantCache and len(out) == 2 and _native(out[0]):
+        st = _fast.quant_read(cache._k, cache._v, cache._scales, idx, counts, out[0], out[1],
+                              _raw_stream(out[0]))
+        if st is not None:
+            _check(st, "spec_quant_read")
+            return tuple(out)
+    dims = _quant_dims(cache)
+    _i32(counts, "counts", dims.B)
+    if idx is not None:
+        dims.n_sets = _quant_sets(idx, dims.B, dims.H_kv)
+        dims.k_max = idx.shape[-1]
+    elif out is not None and isinstance(out[0], torch.Tensor) and out[0].dim() == 5:
+        dims.k_max = out[0].shape[2]
+    else:
+        dims.k_max = dims.L_cap
+    shape = (dims.n_layers, dims.B, dims.k_max, dims.H_kv, dims.d)
+    if out is None:
+        K, V = (torch.zeros(shape, dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+    else:
+        K, V = (_output(t, nm, shape, torch.bfloat16, cache.device)
+                for t, nm in zip(out, ("K", "V")))
+    _same_device(cache.k, counts=counts, idx=idx, K=K, V=V)
+    c = _quant_buffers(cache)
+    with torch.cuda.device(cache.device):
+        _check(lib.spec_quant_read(ctypes.byref(dims), ctypes.byref(c), _p(idx), _p(counts), _p(K),
+                                   _p(V), _stream(K)), "spec_quant_read")
+    return K, V
+
+
+def _quant_q(q: torch.Tensor, dims: QuantDims):
+    _need(q, "q", torch.bfloat16, 4)
+    if q.shape[0] != dims.n_layers or q.shape[1] != dims.B or q.shape[3] != dims.d \
+            or not q.is_contiguous():
+        raise ValueError("q must be contiguous [n_layers, B, H_q, d]")
+    dims.H_q = q.shape[2]
+
+
+def quant_decode_attn(q: torch.Tensor, cache: QuantCache, seq_lens: torch.Tensor,
+                      window: Optional[int] = None, n_sink: int = 0, scale: float = 0.0,
+                      out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                      with_lse: bool = True, ws: Optional[torch.Tensor] = None):
+    """Decode attention over a quantised cache: the query token at position seq_lens[b] - 1
+    sees all tokens up to itself (window None), or the first n_sink and the last `window`
+    of them.  q [n_layers, B, H_q, d] bf16.  Returns (out, lse) as window_decode_attn."""
+    lib = load_library()
+    if out is not None and ws is not None and (lse is not None or not with_lse) \
+            and type(cache) is QuantCache and _native(q):
+        st = _fast.quant_decode(q, cache._k, cache._v, cache._scales, seq_lens, window, n_sink,
+                                scale, out, lse, ws, _raw_stream(q))
+        if st is not None:
+            _check(st, "spec_quant_decode_attn")
+            return out, lse
+    dims = _quant_dims(cache, n_sink=_int32(n_sink), scale=scale)
+    dims.window = dims.L_cap if window is None else _int32(window)
+    _quant_q(q, dims)
+    _i32(seq_lens, "seq_lens", dims.B)
+    _same_device(q, cache=cache.k, seq_lens=seq_lens, out=out, lse=lse, ws=ws)
+    ws, nws = _quant_workspace(dims, QUANT_DECODE, q.device, ws)
+    out = _output(out, "out", q.shape, torch.float32, q.device)
+    if lse is not None or with_lse:
+        lse = _output(lse, "lse", q.shape[:-1], torch.float32, q.device)
+    c = _quant_buffers(cache)
+    with torch.cuda.device(q.device):
+        _check(lib.spec_quant_decode_attn(ctypes.byref(dims), _p(q), ctypes.byref(c),
+                                          _p(seq_lens), _p(out), _p(lse), _p(ws), nws,
+                                          _stream(q)), "spec_quant_decode_attn")
+    return out, lse
+
+
+def quant_sparse_decode_attn(q: torch.Tensor, cache: QuantCache, counts: torch.Tensor,
+                             idx: torch.Tensor, scale: float = 0.0,
+                             out: Optional[torch.Tensor] = None,
+                             lse: Optional[torch.Tensor] = None, with_lse: bool = True,
+                             ws: Optional[torch.Tensor] = None):
+    """Decode attention over the selected rows idx[b, 0 .. counts[b]) of a quantised cache:
+    idx int32 [B, k_max], or [B, H_kv, k_max] with one set per KV head.  q [n_layers, B, H_q,
+    d] bf16.  Returns (out, lse) as sparse_decode_attn."""
+    lib = load_library()
+    if out is not None and ws is not None and (lse is not None or not with_lse) \
+            and type(cache) is QuantCache and _native(q):
+        st = _fast.quant_sparse(q, cache._k, cache._v, cache._scales, counts, idx, scale, out,
+                                lse, ws, _raw_stream(q))
+        if st is not None:
+            _check(st, "spec_quant_sparse_decode_attn")
+            return out, lse
+    dims = _quant_dims(cache, scale=scale)
+    _quant_q(q, dims)
+    _i32(counts, "counts", dims.B)
+    dims.n_sets = _quant_sets(idx, dims.B, dims.H_kv)
+    dims.k_max = idx.shape[-1]
+    _same_device(q, cache=cache.k, counts=counts, idx=idx, out=out, lse=lse, ws=ws)
+    ws, nws = _quant_workspace(dims, QUANT_SPARSE_DECODE, q.device, ws)
+    out = _output(out, "out", q.shape, torch.float32, q.device)
+    if lse is not None or with_lse:
+        lse = _output(lse, "lse", q.shape[:-1], torch.float32, q.device)
+    c = _quant_buffers(cache)
+    with torch.cuda.device(q.device):
+        _check(lib.spec_quant_sparse_decode_attn(ctypes.byref(dims), _p(q), ctypes.byref(c),
+                                                 _p(idx), _p(counts), _p(out), _p(lse), _p(ws),
+                                                 nws, _stream(q)),
+               "spec_quant_sparse_decode_attn")
+    return out, lse

@@ -36,6 +36,10 @@ struct Api {
   decltype(&spec_prefix_decode_attn) prefix_decode;
   decltype(&spec_accum_decode_attn) accum_decode;
   decltype(&spec_evict) evict;
+  decltype(&spec_quant_append) quant_append;
+  decltype(&spec_quant_read) quant_read;
+  decltype(&spec_quant_decode_attn) quant_decode;
+  decltype(&spec_quant_sparse_decode_attn) quant_sparse;
 };
 Api api = {};
 
@@ -624,6 +628,145 @@ PyObject* fast_evict(PyObject*, PyObject* const* args, Py_ssize_t n) {
               ptr<uint16_t>(v_new), ptr<int32_t>(n_new), ws->data_ptr(), ws->nbytes(), stream);
 }
 
+// A quantised cache's tensors k, v and scales, as a call's dims and buffers.
+bool quant_cache(const at::Tensor* k, const at::Tensor* v, const at::Tensor* scales,
+                 spec_quant_dims* d, spec_quant_cache* c) {
+  if (!is(k, at::kByte, 5) || !is(v, at::kByte, 5) || !is(scales, at::kByte, 6) ||
+      k->sizes() != v->sizes() || k->strides() != v->strides() || !packed(*k, 3) ||
+      !packed(*scales, 4) || (k->size(4) != 64 && k->size(4) != 128))
+    return false;
+  for (int i = 0; i < 4; ++i)
+    if (scales->size(i) != k->size(i) || k->size(i) > INT32_MAX) return false;
+  if (scales->size(4) != 2 || scales->size(5) != 4 || !same_device(*k, {v, scales})) return false;
+  *d = {};
+  d->n_layers = (int32_t)k->size(0);
+  d->B = (int32_t)k->size(1);
+  d->L_cap = (int32_t)k->size(2);
+  d->H_q = d->H_kv = (int32_t)k->size(3);
+  d->d = 128;
+  d->bits = (int32_t)(k->size(4) / 16);
+  d->T = 1;
+  d->n_sets = 1;
+  d->kv_stride_layer = stride(*k, 0);
+  d->kv_stride_b = stride(*k, 1);
+  d->scale_stride_layer = stride(*scales, 0);
+  d->scale_stride_b = stride(*scales, 1);
+  *c = {ptr<uint8_t>(k), ptr<uint8_t>(v), ptr<uint8_t>(scales)};
+  return true;
+}
+
+#define QUANT_CACHE(i)                                  \
+  TENSOR(k, i);                                         \
+  TENSOR(v, i + 1);                                     \
+  TENSOR(scales, i + 2);                                \
+  spec_quant_dims d;                                    \
+  spec_quant_cache c;                                   \
+  EXPECT(quant_cache(k, v, scales, &d, &c))
+
+// idx [B][k_max] or [B][H_kv][k_max]: k_max and n_sets.
+bool quant_sets(const at::Tensor* idx, spec_quant_dims* d) {
+  if (!idx || idx->scalar_type() != at::kInt || !idx->is_contiguous()) return false;
+  if (idx->dim() != 2 && (idx->dim() != 3 || idx->size(1) != d->H_kv)) return false;
+  if (idx->size(0) != d->B || idx->size(-1) > INT32_MAX) return false;
+  d->k_max = (int32_t)idx->size(-1);
+  d->n_sets = idx->dim() == 3 ? d->H_kv : 1;
+  return true;
+}
+
+// q [n_layers][B][H_q][d], out alike in fp32, lse.
+bool quant_queries(const at::Tensor* q, const at::Tensor* out, const at::Tensor* lse,
+                   spec_quant_dims* d) {
+  if (!is(q, at::kBFloat16, 4) || !q->is_contiguous() || q->size(0) != d->n_layers ||
+      q->size(1) != d->B || q->size(3) != d->d || q->size(2) > INT32_MAX)
+    return false;
+  if (out->scalar_type() != at::kFloat || !out->is_contiguous() || out->sizes() != q->sizes() ||
+      (lse && (lse->scalar_type() != at::kFloat || !lse->is_contiguous() ||
+               lse->sizes() != q->sizes().slice(0, 3))))
+    return false;
+  d->H_q = (int32_t)q->size(2);
+  return true;
+}
+
+// quant_append(k, v, scales, k_new, v_new, pos, n_new|None, stream)
+PyObject* fast_quant_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  EXPECT(n == 8);
+  QUANT_CACHE(0);
+  TENSOR(k_new, 3);
+  TENSOR(v_new, 4);
+  TENSOR(pos, 5);
+  TENSOR_OR_NONE(n_new, 6);
+  bool ok;
+  void* stream = as_stream(args[7], &ok);
+  EXPECT(ok && is(k_new, at::kBFloat16, 5) && k_new->size(2) <= INT32_MAX);
+  const int64_t T = k_new->size(2);
+  EXPECT(has_shape(k_new, at::kBFloat16, {d.n_layers, d.B, T, d.H_kv, d.d}) &&
+         has_shape(v_new, at::kBFloat16, {d.n_layers, d.B, T, d.H_kv, d.d}) &&
+         has_shape(pos, at::kInt, {d.B}) && (!n_new || has_shape(n_new, at::kInt, {d.B})) &&
+         same_device(*k, {k_new, v_new, pos, n_new}));
+  d.T = (int32_t)T;
+  return call(api.quant_append, &d, &c, ptr<uint16_t>(k_new), ptr<uint16_t>(v_new),
+              ptr<int32_t>(pos), ptr<int32_t>(n_new), stream);
+}
+
+// quant_read(k, v, scales, idx|None, counts, k_out, v_out, stream)
+PyObject* fast_quant_read(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  EXPECT(n == 8);
+  QUANT_CACHE(0);
+  TENSOR_OR_NONE(idx, 3);
+  TENSOR(counts, 4);
+  TENSOR(k_out, 5);
+  TENSOR(v_out, 6);
+  bool ok;
+  void* stream = as_stream(args[7], &ok);
+  EXPECT(ok && is(k_out, at::kBFloat16, 5) && k_out->size(2) <= INT32_MAX);
+  d.k_max = (int32_t)k_out->size(2);
+  EXPECT(!idx || quant_sets(idx, &d));
+  EXPECT(has_shape(k_out, at::kBFloat16, {d.n_layers, d.B, d.k_max, d.H_kv, d.d}) &&
+         has_shape(v_out, at::kBFloat16, {d.n_layers, d.B, d.k_max, d.H_kv, d.d}) &&
+         has_shape(counts, at::kInt, {d.B}) && same_device(*k, {idx, counts, k_out, v_out}));
+  return call(api.quant_read, &d, &c, ptr<int32_t>(idx), ptr<int32_t>(counts),
+              ptr<uint16_t>(k_out), ptr<uint16_t>(v_out), stream);
+}
+
+// quant_decode(q, k, v, scales, seq_lens, window|None, n_sink, scale, out, lse|None, ws, stream)
+PyObject* fast_quant_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  EXPECT(n == 12);
+  TENSOR(q, 0);
+  QUANT_CACHE(1);
+  TENSOR(lens, 4);
+  TENSOR(out, 8);
+  TENSOR_OR_NONE(lse, 9);
+  WORKSPACE(ws, 10);
+  bool ok;
+  void* stream = as_stream(args[11], &ok);
+  EXPECT(ok && quant_queries(q, out, lse, &d));
+  d.window = d.L_cap;
+  EXPECT(args[5] == Py_None || as_int(args[5], &d.window));
+  EXPECT(as_int(args[6], &d.n_sink) && as_float(args[7], &d.scale));
+  EXPECT(has_shape(lens, at::kInt, {d.B}) && same_device(*q, {k, lens, out, lse, ws}));
+  return call(api.quant_decode, &d, ptr<uint16_t>(q), &c, ptr<int32_t>(lens), ptr<float>(out),
+              ptr<float>(lse), ws->data_ptr(), ws->nbytes(), stream);
+}
+
+// quant_sparse(q, k, v, scales, counts, idx, scale, out, lse|None, ws, stream)
+PyObject* fast_quant_sparse(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  EXPECT(n == 11);
+  TENSOR(q, 0);
+  QUANT_CACHE(1);
+  TENSOR(counts, 4);
+  TENSOR(idx, 5);
+  TENSOR(out, 7);
+  TENSOR_OR_NONE(lse, 8);
+  WORKSPACE(ws, 9);
+  bool ok;
+  void* stream = as_stream(args[10], &ok);
+  EXPECT(ok && quant_queries(q, out, lse, &d) && quant_sets(idx, &d));
+  EXPECT(as_float(args[6], &d.scale));
+  EXPECT(has_shape(counts, at::kInt, {d.B}) && same_device(*q, {k, counts, idx, out, lse, ws}));
+  return call(api.quant_sparse, &d, ptr<uint16_t>(q), &c, ptr<int32_t>(idx), ptr<int32_t>(counts),
+              ptr<float>(out), ptr<float>(lse), ws->data_ptr(), ws->nbytes(), stream);
+}
+
 // init(addresses of the entry points, in Api's order)
 PyObject* fast_init(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != (Py_ssize_t)(sizeof(Api) / sizeof(void*))) {
@@ -672,6 +815,10 @@ PyMethodDef methods[] = {
     METHOD("prefix_decode", fast_prefix_decode),
     METHOD("accum_decode", fast_accum_decode),
     METHOD("evict", fast_evict),
+    METHOD("quant_append", fast_quant_append),
+    METHOD("quant_read", fast_quant_read),
+    METHOD("quant_decode", fast_quant_decode),
+    METHOD("quant_sparse", fast_quant_sparse),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast", nullptr, -1, methods};

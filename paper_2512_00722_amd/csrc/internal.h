@@ -285,6 +285,35 @@ struct EvictArgs {
 };
 hipError_t launch_evict(const DenseDims& d, const EvictArgs& x, void* ws, hipStream_t s);
 
+// ---- caches held in 4 or 8 bits ------------------------------------------
+// Dimensions of their entry points after validation.
+struct QuantDims {
+  int B, L_cap, n_layers, H_q, H_kv, G, bits, T, window, n_sink, k_max, n_sets;
+  int64_t kv_stride_layer, kv_stride_b, scale_stride_layer, scale_stride_b;
+  float scale;
+};
+struct QuantCache {
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* scales;
+};
+// Workgroups of spec_quant_append (rows = T) and spec_quant_read (k_max).
+int64_t quant_io_blocks(const QuantDims& d, int rows);
+hipError_t launch_quant_append(const QuantDims& d, const QuantCache& c, const uint16_t* k_new,
+                               const uint16_t* v_new, const int32_t* pos, const int32_t* n_new,
+                               hipStream_t s);
+hipError_t launch_quant_read(const QuantDims& d, const QuantCache& c, const int32_t* idx,
+                             const int32_t* counts, uint16_t* k_out, uint16_t* v_out,
+                             hipStream_t s);
+size_t quant_decode_ws_bytes(const QuantDims& d);
+hipError_t launch_quant_decode(const QuantDims& d, const uint16_t* q, const QuantCache& c,
+                               const int32_t* lens, float* out, float* lse, void* ws,
+                               hipStream_t s);
+size_t quant_sparse_ws_bytes(const QuantDims& d);
+hipError_t launch_quant_sparse_decode(const QuantDims& d, const uint16_t* q, const QuantCache& c,
+                                      const int32_t* idx, const int32_t* counts, float* out,
+                                      float* lse, void* ws, hipStream_t s);
+
 hipError_t launch_delta(const Dims& d, const int32_t* idx_now, const int32_t* counts,
                         const uint16_t* k_cache, const uint16_t* v_cache,
                         int32_t* slot_tok, int32_t* slot_src, uint16_t* kbuf, uint16_t* vbuf,

@@ -1,0 +1,217 @@
+// New rows into caches held in 4 or 8 bits, and rows back to bf16.
+//
+// Both are bound by memory.  A thread has eight elements of K and the same eight of V
+// (one 16-byte bf16 load or store each), four threads a group, sixteen a row of a head.
+#include "quant_core.h"
+
+namespace spec {
+namespace {
+
+constexpr int kRowThreads = 16;               // of a row of a head
+constexpr int kThreads = 256;
+constexpr int kUnroll = 4;                    // rows of a thread, loads of all in flight
+constexpr int kRowsPerBlock = kThreads / kRowThreads * kUnroll;
+
+struct QuantIoArgs {
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* scales;
+  const uint16_t* k_in;   // append: new rows
+  const uint16_t* v_in;
+  uint16_t* k_out;        // read
+  uint16_t* v_out;
+  const int32_t* idx;     // read: [B][n_sets][rows] or null
+  const int32_t* n;       // [B] rows of a sequence; null: all
+  const int32_t* pos;     // append: [B]
+  int64_t kv_stride_layer, kv_stride_b, scale_stride_layer, scale_stride_b;
+  int B, L_cap, H_kv, rows, n_sets, blocks;  // rows: T or k_max; blocks: of a (layer, sequence)
+};
+
+template <int BITS>
+__device__ __forceinline__ uint2 quantise8(const uint4& x, float scale) {
+  uint2 r = make_uint2(0, 0);
+  if constexpr (BITS == 4) {
+    r.x = elements2<4, 0>(r.x, x.x, scale);
+    r.x = elements2<4, 1>(r.x, x.y, scale);
+    r.x = elements2<4, 2>(r.x, x.z, scale);
+    r.x = elements2<4, 3>(r.x, x.w, scale);
+  } else {
+    r.x = elements2<8, 0>(r.x, x.x, scale);
+    r.x = elements2<8, 1>(r.x, x.y, scale);
+    r.y = elements2<8, 0>(r.y, x.z, scale);
+    r.y = elements2<8, 1>(r.y, x.w, scale);
+  }
+  return r;
+}
+
+// Largest magnitude (bf16 bits) of the eight elements of each of a quad's threads.
+__device__ __forceinline__ uint32_t quad_top(const uint4& x) {
+  typedef uint16_t ushortx2 __attribute__((ext_vector_type(2)));
+  auto mag = [](uint32_t w) { return __builtin_bit_cast(ushortx2, w & 0x7fff7fffu); };
+  ushortx2 m = __builtin_elementwise_max(__builtin_elementwise_max(mag(x.x), mag(x.y)),
+                                         __builtin_elementwise_max(mag(x.z), mag(x.w)));
+  uint32_t t = m[0] > m[1] ? m[0] : m[1];
+  uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)t, 0xB1, 0xf, 0xf, false);
+  t = t > o ? t : o;
+  o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)t, 0x4E, 0xf, 0xf, false);
+  return t > o ? t : o;
+}
+
+template <int BITS>
+__device__ __forceinline__ void store8(uint8_t* row, int piece, const uint2& e) {
+  if constexpr (BITS == 4) reinterpret_cast<uint32_t*>(row)[piece] = e.x;
+  else reinterpret_cast<uint2*>(row)[piece] = e;
+}
+
+// Rows (token, head) of a sequence's new tokens stand in the caches as they come, from
+// token pos on: those inside the caches are one range of rows.
+template <int BITS>
+__global__ __launch_bounds__(kThreads) void append_kernel(QuantIoArgs a) {
+  const int lb = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
+  const int layer = lb / a.B, b = lb % a.B;
+  const int64_t pos = a.pos[b];
+  const int n = a.n ? clampi(a.n[b], 0, a.rows) : a.rows;
+  const int64_t lo = (pos < 0 ? -pos : 0) * a.H_kv;
+  const int64_t hi = (pos + n < a.L_cap ? n : a.L_cap - pos) * a.H_kv;
+  const int piece = threadIdx.x % kRowThreads;
+  const int64_t r0 = (int64_t)block * kRowsPerBlock + threadIdx.x / kRowThreads;
+  const int64_t in0 = (int64_t)lb * a.rows * a.H_kv * kHeadDim + 8 * piece;
+  uint4 k[kUnroll], v[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int64_t r = r0 + u * (kThreads / kRowThreads);
+    if (r < lo || r >= hi) continue;
+    k[u] = ldg16_stream(a.k_in + in0 + r * kHeadDim);
+    v[u] = ldg16_stream(a.v_in + in0 + r * kHeadDim);
+  }
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int64_t r = r0 + u * (kThreads / kRowThreads);
+    if (r < lo || r >= hi) continue;  // uniform over a row's threads
+    const int64_t to = pos * a.H_kv + r;  // row of the sequence's caches
+    const int64_t at = layer * a.kv_stride_layer + b * a.kv_stride_b + to * row_bytes(BITS);
+    const int ks = scale_byte<BITS>(quad_top(k[u])), vs = scale_byte<BITS>(quad_top(v[u]));
+    store8<BITS>(a.k + at, piece, quantise8<BITS>(k[u], scale_of(ks, 0)));
+    store8<BITS>(a.v + at, piece, quantise8<BITS>(v[u], scale_of(vs, 0)));
+    if ((piece & 3) < 2)  // the first thread of a group has K's scale, the second V's
+      a.scales[layer * a.scale_stride_layer + b * a.scale_stride_b + to * kScaleBytes +
+               4 * (piece & 3) + piece / 4] = (uint8_t)((piece & 3) == 0 ? ks : vs);
+  }
+}
+
+template <int BITS>
+__device__ __forceinline__ uint2 load8(const uint8_t* row, int piece) {
+  if constexpr (BITS == 4) return make_uint2(reinterpret_cast<const uint32_t*>(row)[piece], 0);
+  else return reinterpret_cast<const uint2*>(row)[piece];
+}
+
+template <int BITS>
+__device__ __forceinline__ uint4 values8(const uint2& e, float scale) {
+  RowPart<BITS> p{};
+  p.w[0].x = e.x;
+  p.w[0].y = e.y;
+  return __builtin_bit_cast(uint4, elements8<BITS>(p, 0, scale));
+}
+
+template <int BITS, bool INDEXED>
+__global__ __launch_bounds__(kThreads) void read_kernel(QuantIoArgs a) {
+  const int lb = blockIdx.x / a.blocks, block = blockIdx.x % a.blocks;
+  const int layer = lb / a.B, b = lb % a.B;
+  const int64_t hi = (int64_t)clampi(a.n[b], 0, a.rows) * a.H_kv;
+  const int piece = threadIdx.x % kRowThreads;
+  const int64_t r0 = (int64_t)block * kRowsPerBlock + threadIdx.x / kRowThreads;
+  if ((int64_t)block * kRowsPerBlock >= hi) return;  // uniform
+  const int64_t kv0 = layer * a.kv_stride_layer + b * a.kv_stride_b;
+  const int64_t s0 = layer * a.scale_stride_layer + b * a.scale_stride_b;
+  int64_t from[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int64_t r = r0 + u * (kThreads / kRowThreads);
+    from[u] = r < hi ? r : hi - 1;
+    if (INDEXED) {
+      const int64_t j = from[u] / a.H_kv;
+      const int g = (int)(from[u] - j * a.H_kv), s = a.n_sets == 1 ? 0 : g;
+      from[u] = (int64_t)clampi(a.idx[((int64_t)b * a.n_sets + s) * a.rows + j], 0, a.L_cap - 1) *
+                    a.H_kv + g;
+    }
+  }
+  uint2 k[kUnroll], v[kUnroll];
+  uint8_t ks[kUnroll], vs[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    k[u] = load8<BITS>(a.k + kv0 + from[u] * row_bytes(BITS), piece);
+    v[u] = load8<BITS>(a.v + kv0 + from[u] * row_bytes(BITS), piece);
+    ks[u] = a.scales[s0 + from[u] * kScaleBytes + piece / 4];
+    vs[u] = a.scales[s0 + from[u] * kScaleBytes + 4 + piece / 4];
+  }
+  const int64_t out0 = (int64_t)lb * a.rows * a.H_kv * kHeadDim + 8 * piece;
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int64_t r = r0 + u * (kThreads / kRowThreads);
+    if (r >= hi) continue;
+    *reinterpret_cast<uint4*>(a.k_out + out0 + r * kHeadDim) =
+        values8<BITS>(k[u], scale_of(ks[u], 0));
+    *reinterpret_cast<uint4*>(a.v_out + out0 + r * kHeadDim) =
+        values8<BITS>(v[u], scale_of(vs[u], 0));
+  }
+}
+
+QuantIoArgs io_args(const QuantDims& d, const QuantCache& c, int rows) {
+  QuantIoArgs a{};
+  a.k = c.k;
+  a.v = c.v;
+  a.scales = c.scales;
+  a.kv_stride_layer = d.kv_stride_layer;
+  a.kv_stride_b = d.kv_stride_b;
+  a.scale_stride_layer = d.scale_stride_layer;
+  a.scale_stride_b = d.scale_stride_b;
+  a.B = d.B;
+  a.L_cap = d.L_cap;
+  a.H_kv = d.H_kv;
+  a.rows = rows;
+  a.n_sets = d.n_sets;
+  a.blocks = (int)(((int64_t)rows * d.H_kv + kRowsPerBlock - 1) / kRowsPerBlock);
+  return a;
+}
+
+}  // namespace
+
+int64_t quant_io_blocks(const QuantDims& d, int rows) {
+  return (int64_t)d.n_layers * d.B *
+         (((int64_t)rows * d.H_kv + kRowsPerBlock - 1) / kRowsPerBlock);
+}
+
+hipError_t launch_quant_append(const QuantDims& d, const QuantCache& c, const uint16_t* k_new,
+                               const uint16_t* v_new, const int32_t* pos, const int32_t* n_new,
+                               hipStream_t s) {
+  QuantIoArgs a = io_args(d, c, d.T);
+  a.k_in = k_new;
+  a.v_in = v_new;
+  a.n = n_new;
+  a.pos = pos;
+  const dim3 grid((unsigned)quant_io_blocks(d, d.T));
+  if (d.bits == 4) append_kernel<4><<<grid, kThreads, 0, s>>>(a);
+  else append_kernel<8><<<grid, kThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_quant_read(const QuantDims& d, const QuantCache& c, const int32_t* idx,
+                             const int32_t* counts, uint16_t* k_out, uint16_t* v_out,
+                             hipStream_t s) {
+  QuantIoArgs a = io_args(d, c, d.k_max);
+  a.k_out = k_out;
+  a.v_out = v_out;
+  a.idx = idx;
+  a.n = counts;
+  const dim3 grid((unsigned)quant_io_blocks(d, d.k_max));
+  if (d.bits == 4) {
+    if (idx) read_kernel<4, true><<<grid, kThreads, 0, s>>>(a);
+    else read_kernel<4, false><<<grid, kThreads, 0, s>>>(a);
+  } else {
+    if (idx) read_kernel<8, true><<<grid, kThreads, 0, s>>>(a);
+    else read_kernel<8, false><<<grid, kThreads, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace spec

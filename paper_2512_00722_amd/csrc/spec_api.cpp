@@ -22,6 +22,7 @@ thread_local int g_last_hip_error = 0;
 constexpr int kMaxElasticLcap = 245760;  // two LDS bitmaps of L_cap bits <= 60 KiB
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // Query heads per KV head: a power of two up to 128 (more than 16 run as
@@ -443,6 +444,99 @@ spec_status debug_range(const int32_t* p, size_t n, int32_t lo, int32_t hi, hipS
   return SPEC_OK;
 }
 
+spec_status resolve_quant(const spec_quant_dims* dm, spec_quant_op op, spec::QuantDims* o) {
+  if (!dm || dm->reserved != 0) return SPEC_ERR_INVALID;
+  const bool attn = op == SPEC_QUANT_DECODE || op == SPEC_QUANT_SPARSE_DECODE;
+  const bool rows = op == SPEC_QUANT_READ || op == SPEC_QUANT_SPARSE_DECODE;
+  if (dm->B <= 0 || dm->L_cap <= 0 || dm->n_layers <= 0 || dm->H_kv <= 0 || dm->d <= 0)
+    return SPEC_ERR_INVALID;
+  if (attn && (dm->H_q <= 0 || dm->H_q % dm->H_kv != 0)) return SPEC_ERR_INVALID;
+  if (dm->kv_stride_layer < 0 || dm->kv_stride_b < 0 || dm->scale_stride_layer < 0 ||
+      dm->scale_stride_b < 0)
+    return SPEC_ERR_INVALID;
+  if (!isfinite(dm->scale) || dm->scale < 0.f) return SPEC_ERR_INVALID;
+  if (op == SPEC_QUANT_DECODE && (dm->window <= 0 || dm->n_sink < 0)) return SPEC_ERR_INVALID;
+  if (op == SPEC_QUANT_APPEND && dm->T <= 0) return SPEC_ERR_INVALID;
+  if (rows && (dm->k_max <= 0 || dm->k_max > dm->L_cap)) return SPEC_ERR_INVALID;
+
+  if (dm->d != spec::kHeadDim || (dm->bits != 4 && dm->bits != 8)) return SPEC_ERR_UNSUPPORTED;
+  if (attn && dm->H_q / dm->H_kv > 128) return SPEC_ERR_UNSUPPORTED;
+  if (rows && dm->n_sets != 1 && dm->n_sets != dm->H_kv) return SPEC_ERR_UNSUPPORTED;
+  if (dm->B > 65535 || dm->n_layers > 65535 || dm->H_kv > 65535) return SPEC_ERR_UNSUPPORTED;
+  const int64_t lb = (int64_t)dm->n_layers * dm->B;
+  if (lb * dm->H_kv > 1 << 21) return SPEC_ERR_UNSUPPORTED;
+  if (attn && (lb * dm->H_q > 1 << 26 ||
+               lb * dm->H_q / spec::group_heads(dm->H_q / dm->H_kv) > 1 << 22))
+    return SPEC_ERR_UNSUPPORTED;
+  if (dm->L_cap > 1 << 30 || (op == SPEC_QUANT_APPEND && dm->T > 1 << 30))
+    return SPEC_ERR_UNSUPPORTED;
+
+  o->B = dm->B;
+  o->L_cap = dm->L_cap;
+  o->n_layers = dm->n_layers;
+  o->H_q = attn ? dm->H_q : dm->H_kv;
+  o->H_kv = dm->H_kv;
+  o->G = o->H_q / dm->H_kv;
+  o->bits = dm->bits;
+  o->T = dm->T;
+  o->window = dm->window < dm->L_cap ? dm->window : dm->L_cap;
+  o->n_sink = dm->n_sink < dm->L_cap ? dm->n_sink : dm->L_cap;
+  o->k_max = dm->k_max;
+  o->n_sets = dm->n_sets;
+  if (!attn &&
+      spec::quant_io_blocks(*o, op == SPEC_QUANT_APPEND ? dm->T : dm->k_max) >= 1 << 24)
+    return SPEC_ERR_UNSUPPORTED;  // threads of a launch
+  const int64_t kv = (int64_t)dm->L_cap * dm->H_kv * (dm->d * dm->bits / 8);
+  const int64_t sc = (int64_t)dm->L_cap * dm->H_kv * (2 * dm->d / 32);
+  o->kv_stride_b = dm->kv_stride_b ? dm->kv_stride_b : kv;
+  o->kv_stride_layer = dm->kv_stride_layer ? dm->kv_stride_layer : (int64_t)dm->B * o->kv_stride_b;
+  o->scale_stride_b = dm->scale_stride_b ? dm->scale_stride_b : sc;
+  o->scale_stride_layer =
+      dm->scale_stride_layer ? dm->scale_stride_layer : (int64_t)dm->B * o->scale_stride_b;
+  if (o->kv_stride_b < kv || o->kv_stride_b % 16 || o->kv_stride_layer < kv ||
+      o->kv_stride_layer % 16 || o->scale_stride_b < sc || o->scale_stride_b % 8 ||
+      o->scale_stride_layer < sc || o->scale_stride_layer % 8)
+    return SPEC_ERR_INVALID;
+  o->scale = dm->scale > 0.f ? dm->scale : 1.0f / sqrtf((float)dm->d);
+  return SPEC_OK;
+}
+
+// New tokens' rows inside the caches: pos[b] in [0, L_cap - n_new[b]] (null: T).
+spec_status debug_append(const spec::QuantDims& d, const int32_t* pos, const int32_t* n_new,
+                         hipStream_t s) {
+  std::vector<int32_t> p, n((size_t)d.B, d.T);
+  if (!d2h(p, pos, (size_t)d.B, s) || (n_new && !d2h(n, n_new, (size_t)d.B, s)))
+    return SPEC_ERR_HIP;
+  for (int b = 0; b < d.B; ++b)
+    if (p[b] < 0 || (int64_t)p[b] + n[b] > d.L_cap) return SPEC_ERR_INVALID;
+  return SPEC_OK;
+}
+
+spec_status resolve_quant_cache(const spec_quant_cache* c, spec::QuantCache* o) {
+  if (!c || !c->k || !c->v || !c->scales) return SPEC_ERR_INVALID;
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned8(c->scales)) return SPEC_ERR_INVALID;
+  *o = {c->k, c->v, c->scales};
+  return SPEC_OK;
+}
+
+size_t quant_ws_bytes(const spec::QuantDims& d, spec_quant_op op) {
+  switch (op) {
+    case SPEC_QUANT_APPEND:
+    case SPEC_QUANT_READ: return 0;
+    case SPEC_QUANT_DECODE: return spec::quant_decode_ws_bytes(d);
+    case SPEC_QUANT_SPARSE_DECODE: return spec::quant_sparse_ws_bytes(d);
+  }
+  return 0;
+}
+
+spec_status check_quant_ws(const spec::QuantDims& d, spec_quant_op op, const void* ws,
+                           size_t ws_bytes) {
+  const size_t need = quant_ws_bytes(d, op);
+  if (need == 0) return SPEC_OK;
+  if (!ws || ws_bytes < need) return SPEC_ERR_WORKSPACE;
+  return aligned16(ws) ? SPEC_OK : SPEC_ERR_INVALID;
+}
+
 // Host checks shared by the step entry points (before any HIP call).
 spec_status check_step(const spec_dims* dm, spec::Dims* d, const uint16_t* q_r,
                        const uint16_t* k_r, const int32_t* seq_lens, const int32_t* ks,
@@ -667,6 +761,93 @@ spec_status spec_evict(const spec_dense_dims* dm, const spec_bounded* cache, con
   const spec::EvictArgs x{cache->k, cache->v, cache->weights, cache->tokens, cache->counts,
                           keep,     pos,      k_new,          v_new,         n_new};
   return finish(hip_status(spec::launch_evict(d, x, ws, s)), s);
+}
+
+spec_status spec_quant_workspace_size(const spec_quant_dims* dm, spec_quant_op op,
+                                      size_t* bytes) {
+  if (!bytes) return SPEC_ERR_INVALID;
+  if ((int)op < SPEC_QUANT_APPEND || (int)op > SPEC_QUANT_SPARSE_DECODE) return SPEC_ERR_INVALID;
+  spec::QuantDims d;
+  const spec_status st = resolve_quant(dm, op, &d);
+  if (st != SPEC_OK) return st;
+  *bytes = quant_ws_bytes(d, op);
+  return SPEC_OK;
+}
+
+spec_status spec_quant_append(const spec_quant_dims* dm, const spec_quant_cache* cache,
+                              const uint16_t* k_new, const uint16_t* v_new, const int32_t* pos,
+                              const int32_t* n_new, spec_stream stream) {
+  spec::QuantDims d;
+  spec::QuantCache c;
+  spec_status st = resolve_quant(dm, SPEC_QUANT_APPEND, &d);
+  if (st != SPEC_OK) return st;
+  if ((st = resolve_quant_cache(cache, &c)) != SPEC_OK) return st;
+  if (!k_new || !v_new || !pos) return SPEC_ERR_INVALID;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned4(pos) || (n_new && !aligned4(n_new)))
+    return SPEC_ERR_INVALID;
+  const hipStream_t s = as_stream(stream);
+  if (debug_on() && ((st = debug_range(n_new, d.B, 0, d.T, s)) != SPEC_OK ||
+                     (st = debug_append(d, pos, n_new, s)) != SPEC_OK))
+    return st;
+  return finish(hip_status(spec::launch_quant_append(d, c, k_new, v_new, pos, n_new, s)), s);
+}
+
+spec_status spec_quant_read(const spec_quant_dims* dm, const spec_quant_cache* cache,
+                            const int32_t* idx, const int32_t* counts, uint16_t* k_out,
+                            uint16_t* v_out, spec_stream stream) {
+  spec::QuantDims d;
+  spec::QuantCache c;
+  spec_status st = resolve_quant(dm, SPEC_QUANT_READ, &d);
+  if (st != SPEC_OK) return st;
+  if ((st = resolve_quant_cache(cache, &c)) != SPEC_OK) return st;
+  if (!counts || !k_out || !v_out) return SPEC_ERR_INVALID;
+  if (!aligned16(k_out) || !aligned16(v_out) || !aligned4(counts) || (idx && !aligned4(idx)))
+    return SPEC_ERR_INVALID;
+  const hipStream_t s = as_stream(stream);
+  if (debug_on() &&
+      (st = debug_selection(d.B, d.k_max, d.n_sets, idx, counts, d.L_cap, s)) != SPEC_OK)
+    return st;
+  return finish(hip_status(spec::launch_quant_read(d, c, idx, counts, k_out, v_out, s)), s);
+}
+
+spec_status spec_quant_decode_attn(const spec_quant_dims* dm, const uint16_t* q,
+                                   const spec_quant_cache* cache, const int32_t* seq_lens,
+                                   float* out, float* lse, void* ws, size_t ws_bytes,
+                                   spec_stream stream) {
+  spec::QuantDims d;
+  spec::QuantCache c;
+  spec_status st = resolve_quant(dm, SPEC_QUANT_DECODE, &d);
+  if (st != SPEC_OK) return st;
+  if ((st = resolve_quant_cache(cache, &c)) != SPEC_OK) return st;
+  if (!q || !seq_lens || !out) return SPEC_ERR_INVALID;
+  if (!aligned16(q) || !aligned4(seq_lens) || !aligned16(out) || (lse && !aligned4(lse)))
+    return SPEC_ERR_INVALID;
+  if ((st = check_quant_ws(d, SPEC_QUANT_DECODE, ws, ws_bytes)) != SPEC_OK) return st;
+  const hipStream_t s = as_stream(stream);
+  if (debug_on() && (st = debug_range(seq_lens, d.B, 0, d.L_cap, s)) != SPEC_OK) return st;
+  return finish(hip_status(spec::launch_quant_decode(d, q, c, seq_lens, out, lse, ws, s)), s);
+}
+
+spec_status spec_quant_sparse_decode_attn(const spec_quant_dims* dm, const uint16_t* q,
+                                          const spec_quant_cache* cache, const int32_t* idx,
+                                          const int32_t* counts, float* out, float* lse, void* ws,
+                                          size_t ws_bytes, spec_stream stream) {
+  spec::QuantDims d;
+  spec::QuantCache c;
+  spec_status st = resolve_quant(dm, SPEC_QUANT_SPARSE_DECODE, &d);
+  if (st != SPEC_OK) return st;
+  if ((st = resolve_quant_cache(cache, &c)) != SPEC_OK) return st;
+  if (!q || !idx || !counts || !out) return SPEC_ERR_INVALID;
+  if (!aligned16(q) || !aligned4(idx) || !aligned4(counts) || !aligned16(out) ||
+      (lse && !aligned4(lse)))
+    return SPEC_ERR_INVALID;
+  if ((st = check_quant_ws(d, SPEC_QUANT_SPARSE_DECODE, ws, ws_bytes)) != SPEC_OK) return st;
+  const hipStream_t s = as_stream(stream);
+  if (debug_on() &&
+      (st = debug_selection(d.B, d.k_max, d.n_sets, idx, counts, d.L_cap, s)) != SPEC_OK)
+    return st;
+  return finish(
+      hip_status(spec::launch_quant_sparse_decode(d, q, c, idx, counts, out, lse, ws, s)), s);
 }
 
 spec_status spec_workspace_size(const spec_dims* dm, spec_op op, size_t* bytes) {
