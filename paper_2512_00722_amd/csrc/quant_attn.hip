@@ -17,7 +17,10 @@
 namespace spec {
 namespace {
 
-constexpr int kW = 8;  // wavefronts of a workgroup
+#ifndef KW
+#define KW 4
+#endif
+constexpr int kW = KW;  // wavefronts of a workgroup
 
 struct QuantArgs {
   const uint16_t* q;       // [n_layers][B][H_q][d]
@@ -36,49 +39,70 @@ struct QuantArgs {
 };
 
 struct QuantUnit {
-  const uint16_t* q;       // the unit's first query head; heads are d apart
-  const uint8_t* k;        // the sequence's rows of the KV head
+  const uint16_t* q;       // the unit's first query head; heads are d apart, those of the
+  int q_stride;            // next KV head q_stride
+  const uint8_t* k;        // the sequence's rows of the first KV head
   const uint8_t* v;
   const uint8_t* scales;
-  const int32_t* idx;      // INDEXED: the rows' tokens, within 0 .. last
+  const int32_t* idx;      // INDEXED: the rows' tokens, clamped into 0 .. last; those of the
+  int64_t idx_stride;      // next KV head idx_stride on
   int64_t rs;              // bytes between tokens; of scales: ss
   int ss;
   int last;
-  int heads, count;        // query heads, at most 16; visible tokens
-  int n_sink, shift;       // else: 0 .. n_sink - 1, the others `shift` further on
+  int heads, count;        // query heads of a KV head, at most 16; visible tokens
+  int n_sink, shift;       // else: tokens 0 .. n_sink - 1, the others `shift` further on
   int part, n_parts;       // this wavefront among those of the unit
   float scale_log2;
+
+  // Chunks of up to 32 tokens that stand together: of the sinks, then of the others.
+  __device__ __forceinline__ int chunks() const {
+    return (n_sink + kDecodeChunk - 1) / kDecodeChunk +
+           (count - n_sink + kDecodeChunk - 1) / kDecodeChunk;
+  }
+  __device__ __forceinline__ int valid(int c) const {
+    const int sinks = (n_sink + kDecodeChunk - 1) / kDecodeChunk;
+    return min(kDecodeChunk, c < sinks ? n_sink - kDecodeChunk * c
+                                       : count - n_sink - kDecodeChunk * (c - sinks));
+  }
+  __device__ __forceinline__ void chunk(int c, int& start, int& n) const {
+    const int sinks = (n_sink + kDecodeChunk - 1) / kDecodeChunk;
+    start = c < sinks ? kDecodeChunk * c : n_sink + shift + kDecodeChunk * (c - sinks);
+    n = valid(c);
+  }
 };
 
 template <bool INDEXED>
-__device__ __forceinline__ int token_of(const QuantUnit& u, int j) {
-  if (INDEXED) return clampi(u.idx[j], 0, u.last);
+__device__ __forceinline__ int64_t token_of(const QuantUnit& u, int h, int j) {
+  if (INDEXED) return clampi(u.idx[h * u.idx_stride + j], 0, u.last);
   return j + (j < u.n_sink ? 0 : u.shift);
 }
 
 // A wavefront's share token by token, without the matrix cores, for the rare sums that
 // hold an infinity or a NaN, as unit_by_token() has it for bf16 caches.
 template <int BITS, bool INDEXED>
-__device__ __forceinline__ void quant_unit_by_token(const QuantUnit& u, float& m_run,
-                                                    float& l_run, floatx4 (&acc)[8]) {
+__device__ __forceinline__ void quant_unit_by_token(const QuantUnit& u, int h, float& m_run,
+                                                 float& l_run, floatx4 (&acc)[8]) {
   const int lane = threadIdx.x & 63, r16 = lane & 15, kg = lane >> 4;
-  const uint16_t* q = u.q + (r16 < u.heads ? r16 : 0) * kHeadDim + 4 * kg;
+  const uint16_t* q = u.q + h * u.q_stride + (r16 < u.heads ? r16 : 0) * kHeadDim + 4 * kg;
+  const uint8_t* k = u.k + h * row_bytes(BITS);
+  const uint8_t* v = u.v + h * row_bytes(BITS);
   m_run = kNoMax;
   l_run = 0.f;
 #pragma unroll
   for (int db = 0; db < 8; ++db) acc[db] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int sinks = (u.n_sink + kDecodeChunk - 1) / kDecodeChunk;
 #pragma unroll 1
-  for (int c = kDecodeChunk * u.part; c < u.count; c += kDecodeChunk * u.n_parts) {
+  for (int c = u.part; c < u.chunks(); c += u.n_parts) {
+    const int j0 = c < sinks ? kDecodeChunk * c : u.n_sink + kDecodeChunk * (c - sinks);
 #pragma unroll 1
-    for (int j = c; j < min(c + kDecodeChunk, u.count); ++j) {
-      const int64_t t = token_of<INDEXED>(u, j);
-      const uint2 sc = *reinterpret_cast<const uint2*>(u.scales + t * u.ss);
+    for (int j = j0; j < j0 + u.valid(c); ++j) {
+      const int64_t t = token_of<INDEXED>(u, h, j);
+      const uint2 sc = *reinterpret_cast<const uint2*>(u.scales + t * u.ss + h * kScaleBytes);
       float s = 0.f;
 #pragma unroll
       for (int db = 0; db < 8; ++db) {
         const uint2 x = *reinterpret_cast<const uint2*>(q + 16 * db);
-        const floatx4 y = elements4<BITS>(u.k + t * u.rs, 16 * db + 4 * kg,
-                                          scale_of(sc.x, db / 2));
+        const floatx4 y = elements4<BITS>(k + t * u.rs, 16 * db + 4 * kg, scale_of(sc.x, db / 2));
         s = fmaf(bf16lo(x.x), y[0], s);
         s = fmaf(bf16hi(x.x), y[1], s);
         s = fmaf(bf16lo(x.y), y[2], s);
@@ -91,8 +115,7 @@ __device__ __forceinline__ void quant_unit_by_token(const QuantUnit& u, float& m
       l_run = l_run * alpha + (kg == 0 ? p : 0.f);
 #pragma unroll
       for (int db = 0; db < 8; ++db) {
-        const floatx4 y = elements4<BITS>(u.v + t * u.rs, 16 * db + 4 * kg,
-                                          scale_of(sc.y, db / 2));
+        const floatx4 y = elements4<BITS>(v + t * u.rs, 16 * db + 4 * kg, scale_of(sc.y, db / 2));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           acc[db][i] = fmaf(acc[db][i], alpha, s == -INFINITY ? 0.f : p * y[i]);
@@ -101,198 +124,290 @@ __device__ __forceinline__ void quant_unit_by_token(const QuantUnit& u, float& m
   }
 }
 
-template <int BITS>
-__device__ __forceinline__ RowPart<BITS> load_part(const uint8_t* p) {
-  RowPart<BITS> r;
-#pragma unroll
-  for (int i = 0; i < BITS / 4; ++i)
-    r.w[i] = ldg16_stream(reinterpret_cast<const uint16_t*>(p) + 8 * i);
-  return r;
-}
+// LDS of a wavefront: V in bf16, [NH][32 tokens][256 bytes], and before it the chunk's K as
+// it is held; scales [32 tokens][NH][8].
+template <int NH>
+struct WaveTile {
+  uint16_t v[NH][kTileElems];
+  uint8_t scales[kDecodeChunk * NH * kScaleBytes];
+};
 
-// A wavefront's share: chunks of 32 tokens, of which lane (r16, kg) has dimensions 32 kg ..
-// of tokens r16 and 16 + r16.  Results as decode_unit's.  V: its V tile.
-template <int BITS, bool INDEXED>
-__device__ __forceinline__ void quant_unit(const QuantUnit& u, uint16_t* V, float& m_run,
-                                           float& l_run, floatx4 (&acc)[8]) {
+// A wavefront's share of NH neighbouring KV heads: chunks of 32 tokens.  Lines of 128 bytes
+// are what a card moves fastest (K and V of 8 heads x 32768 tokens x 256 in 4 bits, loads
+// alone: 7.3 TB/s by lines in the order of the lanes, 5.7 by 64-byte rows of a head, the
+// matrix cores' order): two heads in 4 bits, one in 8.  A lane loads 16-byte pieces, K goes
+// through LDS as it is held, V as bf16 (from where it is read transposed); both by the
+// wavefront itself, so that none waits for another.  Lane (r16, kg) then has dimensions
+// 32 kg .. of K of tokens r16 and 16 + r16.  Results as decode_unit's, for each head.
+template <int BITS, int NH, bool INDEXED>
+__device__ __forceinline__ void quant_unit(const QuantUnit& u, WaveTile<NH>& T, float (&m_run)[NH],
+                                           float (&l_run)[NH], floatx4 (&acc)[NH][8]) {
+  constexpr int P = NH * BITS;         // pieces of a token's row
+  constexpr int RI = 64 / P;           // rows of a load
+  constexpr int NI = kDecodeChunk / RI;
+  constexpr int SP = 16 * 8 / BITS / 8;  // bf16 pieces of 8 elements of a piece
   const int lane = threadIdx.x & 63;
   const int r16 = lane & 15;  // head of this lane; token of a K tile row
   const int kg = lane >> 4;
-  bf16x8 qf[4];  // Q^T: column r16, dimensions 32 kg + 8 s ..
+  const int lrow = lane / P, lpiece = lane % P;   // of a load
+  const int lhead = lpiece / BITS, lpart = lpiece % BITS;
+  bf16x8 qf[NH][4];  // Q^T: column r16, dimensions 32 kg + 8 s ..
 #pragma unroll
-  for (int s = 0; s < 4; ++s) {
-    const uint4 w = r16 < u.heads ? ldg16(u.q + r16 * kHeadDim + kGroup * kg + 8 * s)
-                                  : make_uint4(0, 0, 0, 0);
-    qf[s] = __builtin_bit_cast(bf16x8, w);
-  }
-  const int step = kDecodeChunk * u.n_parts;  // tokens between a wavefront's chunks
-  const int first = kDecodeChunk * u.part;
-  RowPart<BITS> kr[2], vr[2];
-  uint2 sc[2];
-  int64_t tok[2];
-  // Rows behind the last token read the last: they are never used with a weight.
-  auto next_tokens = [&](int c) {
+  for (int h = 0; h < NH; ++h)
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-      tok[t] = token_of<INDEXED>(u, min(c + 16 * t + r16, u.count - 1));
+    for (int s = 0; s < 4; ++s) {
+      const uint4 w = r16 < u.heads ? ldg16(u.q + h * u.q_stride + r16 * kHeadDim + kGroup * kg +
+                                            8 * s)
+                                    : make_uint4(0, 0, 0, 0);
+      qf[h][s] = __builtin_bit_cast(bf16x8, w);
+    }
+  uint4 kr[NI], vr[NI];
+  uint2 sc;
+  int tok[NI], tok_s;
+  const uint8_t *kb, *vb, *sb;
+  int64_t off[NI];
+  // Where chunk c stands: the rows behind its last are read as that one.
+  auto locate = [&](int c) {
+    if (!INDEXED) {
+      int start, valid;
+      u.chunk(c, start, valid);
+      kb = u.k + (int64_t)start * u.rs;
+      vb = u.v + (int64_t)start * u.rs;
+      sb = u.scales + (int64_t)start * u.ss;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) tok[i] = min(RI * i + lrow, valid - 1);
+      tok_s = min(lane / NH % kDecodeChunk, valid - 1);
+    } else {
+      kb = u.k;
+      vb = u.v;
+      sb = u.scales;
+    }
+  };
+  auto indices = [&](int c) {  // INDEXED: of chunk c
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      tok[i] = u.idx[lhead * u.idx_stride + min(kDecodeChunk * c + RI * i + lrow, u.count - 1)];
+    tok_s = u.idx[lane % NH * u.idx_stride +
+                  min(kDecodeChunk * c + lane / NH % kDecodeChunk, u.count - 1)];
+  };
+  auto load_k = [&]() {
+    if (INDEXED) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        off[i] = (int64_t)clampi(tok[i], 0, u.last) * u.rs + 16 * lpiece;
+      sc = *reinterpret_cast<const uint2*>(sb + (int64_t)clampi(tok_s, 0, u.last) * u.ss +
+                                           lane % NH * kScaleBytes);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) off[i] = (uint32_t)(tok[i] * (int)u.rs + 16 * lpiece);
+      sc = *reinterpret_cast<const uint2*>(sb + (uint32_t)(tok_s * u.ss + lane % NH * kScaleBytes));
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      kr[i] = ldg16_stream(reinterpret_cast<const uint16_t*>(kb + off[i]));
   };
   auto load_v = [&]() {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      sc[t] = *reinterpret_cast<const uint2*>(u.scales + tok[t] * u.ss);
-      vr[t] = load_part<BITS>(u.v + tok[t] * u.rs + part_bytes(BITS) * kg);
-    }
+    for (int i = 0; i < NI; ++i)
+      vr[i] = ldg16_stream(reinterpret_cast<const uint16_t*>(vb + off[i]));
   };
-  auto load_k = [&]() {
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-      kr[t] = load_part<BITS>(u.k + tok[t] * u.rs + part_bytes(BITS) * kg);
+  // K's pieces, the 16 rows of a read in different banks
+  uint8_t* const K = reinterpret_cast<uint8_t*>(T.v);
+  auto k_at = [&](int row, int piece) {
+    return K + row * 16 * P + 16 * (piece ^ (P == 8 ? row >> 1 & 7 : row >> 2 & 3));
   };
-  auto put_v = [&]() {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int row = 16 * t + r16;
-      const float scale = scale_of(sc[t].y, kg);
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-        *reinterpret_cast<bf16x8*>(V + row * kHeadDim + (((4 * kg + s) ^ swizzle(row)) << 3)) =
-            elements8<BITS>(vr[t], s, scale);
-    }
+  auto v_at = [&](int h, int row, int piece) {
+    return T.v[h] + row * kHeadDim + ((piece ^ swizzle(row) ^ 2 * h) << 3);
   };
-  // transposed V: tokens 16 h + 4 kg .. + 3, dimensions 16 db + r16
-  auto get_v = [&](int h, int db) {
-    const int t = 16 * h + 4 * kg + (r16 >> 2);
-    const int piece = 2 * db + ((r16 >> 1) & 1);
-    return lds_read_tr(V + t * kHeadDim + ((piece ^ swizzle(t)) << 3) + 4 * (r16 & 1));
+  // transposed V: tokens 16 t + 4 kg .. + 3, dimensions 16 db + r16
+  auto get_v = [&](int h, int t, int db) {
+    return lds_read_tr(v_at(h, 16 * t + 4 * kg + (r16 >> 2), 2 * db + ((r16 >> 1) & 1)) +
+                       4 * (r16 & 1));
   };
 
-  m_run = kNoMax;
-  l_run = 0.f;
 #pragma unroll
-  for (int db = 0; db < 8; ++db) acc[db] = floatx4{0.f, 0.f, 0.f, 0.f};
-  if (first < u.count) {
-    next_tokens(first);
-    load_v();
+  for (int h = 0; h < NH; ++h) {
+    m_run[h] = kNoMax;
+    l_run[h] = 0.f;
+#pragma unroll
+    for (int db = 0; db < 8; ++db) acc[h][db] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  const int chunks = u.chunks();
+  if (u.part < chunks) {
+    if (INDEXED) indices(u.part);
+    locate(u.part);
     load_k();
-    next_tokens(first + step);
+    load_v();
+    if (INDEXED) indices(min(u.part + u.n_parts, chunks - 1));
     __builtin_amdgcn_sched_barrier(0);
   }
-  // Each register buffer is refilled as soon as it is consumed.
-  for (int c = first; c < u.count; c += step) {
-    const float ks[2] = {scale_of(sc[0].x, kg), scale_of(sc[1].x, kg)};
-    put_v();
-    load_v();
-    __builtin_amdgcn_sched_barrier(0);
-    floatx4 s[2];
+  for (int c = u.part; c < chunks; c += u.n_parts) {
+    const int next = min(c + u.n_parts, chunks - 1);
+    *reinterpret_cast<uint2*>(T.scales + lane % (kDecodeChunk * NH) * kScaleBytes) = sc;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(elements8<BITS>(kr[t], i, ks[t]), qf[i],
-                                                       s[t], 0, 0, 0);
-    }
+    for (int i = 0; i < NI; ++i)
+      *reinterpret_cast<uint4*>(k_at(RI * i + lrow, lpiece)) = kr[i];
+    locate(next);
     load_k();
-    next_tokens(c + 2 * step);
     __builtin_amdgcn_sched_barrier(0);
-
-    // S[head r16][token 16 t + 4 kg + i]
-    float p[8];
-    float mx = -INFINITY;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = s[t][i] * u.scale_log2;
-        p[4 * t + i] = c + 16 * t + 4 * kg + i < u.count ? x : -INFINITY;
-        mx = fmaxf(mx, p[4 * t + i]);
-      }
-    }
-    mx = quad_max(mx);
-    const float mn = fmaxf(m_run, mx);
-    const float alpha = exp2_fast(m_run - mn);
-    m_run = mn;
-    l_run *= alpha;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      p[i] = exp2_fast(p[i] - mn);
-      l_run += p[i];
-    }
-#pragma unroll
-    for (int db = 0; db < 8; ++db) acc[db] *= alpha;
-    // Weights enter as three bf16 numbers, 2^-26 relative at most, as over bf16 caches.
-    const bf16x8 ph = to_bf16x8(p), pl = next_bf16x8(p, ph), pt = next_bf16x8(p, pl);
     wave_sync_lds();
-    // slots 8 kg .. + 7 of a multiplication: tokens 4 kg .. + 3 and 16 + 4 kg .. + 3
+    RowPart<BITS> kf[NH][2];
+    float ks[NH][2], vs[NI];
 #pragma unroll
-    for (int db = 0; db < 8; ++db) {
-      const bf16x8 vf =
-          __builtin_shufflevector(get_v(0, db), get_v(1, db), 0, 1, 2, 3, 4, 5, 6, 7);
-      acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph, acc[db], 0, 0, 0);
-      acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl, acc[db], 0, 0, 0);
-      acc[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pt, acc[db], 0, 0, 0);
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int row = 16 * t + r16;
+#pragma unroll
+        for (int w = 0; w < BITS / 4; ++w)
+          kf[h][t].w[w] = *reinterpret_cast<const uint4*>(
+              k_at(row, h * BITS + kg * (BITS / 4) + w));
+        ks[h][t] = scale_of(T.scales[(row * NH + h) * kScaleBytes + kg], 0);
+      }
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      vs[i] = scale_of(T.scales[((RI * i + lrow) * NH + lhead) * kScaleBytes + 4 +
+                                lpart / (BITS / 4)], 0);
+    wave_sync_lds();
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      RowPart<BITS> x{};
+      x.w[0] = vr[i];
+#pragma unroll
+      for (int s = 0; s < SP; ++s)
+        *reinterpret_cast<bf16x8*>(v_at(lhead, RI * i + lrow, SP * lpart + s)) =
+            elements8<BITS>(x, s, vs[i]);
+    }
+    load_v();
+    if (INDEXED) indices(min(next + u.n_parts, chunks - 1));
+    __builtin_amdgcn_sched_barrier(0);
+    wave_sync_lds();
+
+    const int valid = u.valid(c);
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      floatx4 s[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(elements8<BITS>(kf[h][t], i, ks[h][t]),
+                                                         qf[h][i], s[t], 0, 0, 0);
+      }
+      // S[head r16][token 16 t + 4 kg + i]
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = s[i / 4][i % 4];
+      if (valid < kDecodeChunk) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (16 * (i / 4) + 4 * kg + i % 4 >= valid) p[i] = -INFINITY;
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mx = fmaxf(mx, p[i]);
+      mx = quad_max(mx) * u.scale_log2;
+      if (__any(mx > m_run[h])) {
+        const float mn = fmaxf(m_run[h], mx);
+        const float alpha = exp2_fast(m_run[h] - mn);
+        m_run[h] = mn;
+        l_run[h] *= alpha;
+#pragma unroll
+        for (int db = 0; db < 8; ++db) acc[h][db] *= alpha;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = exp2_fast(fmaf(p[i], u.scale_log2, -m_run[h]));
+        l_run[h] += p[i];
+      }
+      // Weights enter as three bf16 numbers, 2^-26 relative at most, as over bf16 caches.
+      const bf16x8 ph = to_bf16x8(p), pl = next_bf16x8(p, ph), pt = next_bf16x8(p, pl);
+      // slots 8 kg .. + 7 of a multiplication: tokens 4 kg .. + 3 and 16 + 4 kg .. + 3
+#pragma unroll
+      for (int db = 0; db < 8; ++db) {
+        const bf16x8 vf =
+            __builtin_shufflevector(get_v(h, 0, db), get_v(h, 1, db), 0, 1, 2, 3, 4, 5, 6, 7);
+        acc[h][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph, acc[h][db], 0, 0, 0);
+        acc[h][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl, acc[h][db], 0, 0, 0);
+        acc[h][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pt, acc[h][db], 0, 0, 0);
+      }
     }
     wave_sync_lds();  // the tile is rewritten by the next chunk
   }
-  float odd = 0.f;
 #pragma unroll
-  for (int db = 0; db < 8; ++db)
+  for (int h = 0; h < NH; ++h) {
+    float odd = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) odd = fmaf(acc[db][i], 0.f, odd);
-  if (__any(odd != odd)) quant_unit_by_token<BITS, INDEXED>(u, m_run, l_run, acc);
-  l_run = quad_sum(l_run);
+    for (int db = 0; db < 8; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) odd = fmaf(acc[h][db][i], 0.f, odd);
+    if (__any(odd != odd)) quant_unit_by_token<BITS, INDEXED>(u, h, m_run[h], l_run[h], acc[h]);
+    l_run[h] = quad_sum(l_run[h]);
+  }
 }
 
-// HB consecutive column groups (KV heads of the same tokens, whose pieces of a row are
-// then read at the same time), kW / HB wavefronts each.
-template <int BITS, bool INDEXED, int HB>
-__global__ __launch_bounds__(kW * 64) __attribute__((amdgpu_waves_per_eu(4)))
+// UB units (NH KV heads and a column group each) of the same tokens side by side, kW / UB
+// wavefronts each.
+template <int BITS, int NH, bool INDEXED, int UB>
+__global__ __launch_bounds__(kW * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void quant_decode_kernel(QuantArgs a) {
-  __shared__ __align__(16) uint16_t tiles[kW][kTileElems];
-  __shared__ float2 ml[kW][16];
-  const int groups = a.H_kv * a.R / HB;
-  const int wave = threadIdx.x >> 6;
+  __shared__ __align__(16) WaveTile<NH> tiles[kW];
+  __shared__ float2 ml[kW][NH][16];
+  const int units = a.H_kv / NH * a.R / UB;   // workgroups of a (layer, sequence, part)
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int split = blockIdx.x % a.n_split, rest = blockIdx.x / a.n_split;
-  const int gv0 = rest % groups * HB, gv = gv0 + wave % HB, g = gv / a.R;
-  const int lb = rest / groups, layer = lb / a.B, b = lb % a.B;
-  const size_t row0 = (size_t)lb * a.H_q + (size_t)gv0 * a.heads;  // first query head
-  const size_t part0 = ((size_t)lb * a.n_split + split) * a.H_q + (size_t)gv0 * a.heads;
+  const int lb = rest / units, layer = lb / a.B, b = lb % a.B;
+  // unit: column group r of KV heads g .. g + NH - 1
+  const int unit0 = rest % units * UB, unit = unit0 + wave % UB;
+  const int g = unit / a.R * NH, r = unit % a.R, G = a.heads * a.R;
   const int64_t base = layer * a.kv_stride_layer + b * a.kv_stride_b + g * row_bytes(BITS);
   const int len = clampi(a.lens[b], 0, INDEXED ? a.k_max : a.L_cap);
   QuantUnit u;
-  u.q = a.q + (row0 + wave % HB * a.heads) * kHeadDim;
+  u.q = a.q + ((int64_t)lb * a.H_q + g * G + r * a.heads) * kHeadDim;
+  u.q_stride = G * kHeadDim;
   u.k = a.k + base;
   u.v = a.v + base;
   u.scales = a.scales + layer * a.scale_stride_layer + b * a.scale_stride_b + g * kScaleBytes;
   u.idx = INDEXED ? a.idx + ((int64_t)b * a.n_sets + (a.n_sets == 1 ? 0 : g)) * a.k_max : nullptr;
+  u.idx_stride = a.n_sets == 1 ? 0 : a.k_max;
   u.rs = (int64_t)a.H_kv * row_bytes(BITS);
   u.ss = a.H_kv * kScaleBytes;
   u.last = a.L_cap - 1;
   u.heads = a.heads;
   u.count = min(len, a.k_max);
-  u.n_sink = min(a.n_sink, u.count);
   u.shift = len - u.count;
-  u.part = split * (kW / HB) + wave / HB;
-  u.n_parts = a.n_split * (kW / HB);
+  u.n_sink = u.shift == 0 ? 0 : min(a.n_sink, u.count);
+  u.part = split * (kW / UB) + wave / UB;
+  u.n_parts = a.n_split * (kW / UB);
   u.scale_log2 = a.scale_log2;
-  float m_run, l_run;
-  floatx4 acc[8];
-  quant_unit<BITS, INDEXED>(u, tiles[wave], m_run, l_run, acc);
+  float m_run[NH], l_run[NH];
+  floatx4 acc[NH][8];
+  quant_unit<BITS, NH, INDEXED>(u, tiles[wave], m_run, l_run, acc);
 
-  leave_results(tiles[wave], ml[wave], m_run, l_run, acc);
+#pragma unroll
+  for (int h = 0; h < NH; ++h) leave_results(tiles[wave].v[h], ml[wave][h], m_run[h], l_run[h], acc[h]);
   __syncthreads();
-  for (int e = threadIdx.x; e < HB * a.heads * 32; e += kW * 64) {
-    const int h = e >> 5, d4 = e & 31;  // query head among the workgroup's
-    const int w0 = HB == 1 ? 0 : h / a.heads;
-    const Join j = join_waves<kW, HB>(tiles, ml, w0, h - w0 * a.heads, d4);
+  for (int e = threadIdx.x; e < UB * NH * a.heads * 32; e += kW * 64) {
+    const int d4 = e & 31, h = (e >> 5) % a.heads, hu = (e >> 5) / a.heads % NH;
+    const int w0 = (e >> 5) / a.heads / NH, un = unit0 + w0;
+    Join j;
+    for (int w = w0; w < kW; w += UB) j.M = fmaxf(j.M, ml[w][hu][h].x);
+    for (int w = w0; w < kW; w += UB)
+      j.add(ml[w][hu][h],
+            *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(tiles[w].v[hu]) +
+                                             result_at(h, d4)));
+    const int64_t head = (int64_t)(un / a.R * NH + hu) * G + un % a.R * a.heads + h;
     if (a.out) {
+      const int64_t row = (int64_t)lb * a.H_q + head;
       const float inv = j.inv();
-      reinterpret_cast<float4*>(a.out + (row0 + h) * kHeadDim)[d4] =
+      reinterpret_cast<float4*>(a.out + row * kHeadDim)[d4] =
           make_float4(j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv);
-      if (a.lse && d4 == 0) a.lse[row0 + h] = j.lse();
+      if (a.lse && d4 == 0) a.lse[row] = j.lse();
     } else {
-      reinterpret_cast<float4*>(a.part_acc + (part0 + h) * kHeadDim)[d4] = j.o;
-      if (d4 == 0) reinterpret_cast<float2*>(a.part_ml)[part0 + h] = make_float2(j.M, j.L);
+      const int64_t row = ((int64_t)lb * a.n_split + split) * a.H_q + head;
+      reinterpret_cast<float4*>(a.part_acc + row * kHeadDim)[d4] = j.o;
+      if (d4 == 0) reinterpret_cast<float2*>(a.part_ml)[row] = make_float2(j.M, j.L);
     }
   }
 }
@@ -303,21 +418,23 @@ __global__ __launch_bounds__(256) void quant_merge_kernel(DecodeArgs a, float* o
   decode_merge<S>(a, blockIdx.x, out, lse, n_out);
 }
 
-// How a launch is divided: hb column groups per workgroup, each over n_split of them.
+// How a launch is divided: units of nh KV heads, ub of them per workgroup, each over
+// n_split workgroups.
 struct QuantPlan {
-  int hb, n_split;
+  int nh, ub, n_split;
 };
 
 QuantPlan quant_plan(const QuantDims& d, int k_max) {
-  const int64_t groups = (int64_t)d.H_kv * (d.G / group_heads(d.G));
-  int hb = kW;
-  while (groups % hb) hb /= 2;
-  const int64_t wgs = (int64_t)d.n_layers * d.B * groups / hb;
+  const int nh = d.bits == 4 && d.H_kv % 2 == 0 ? 2 : 1;
+  const int64_t units = (int64_t)d.H_kv / nh * (d.G / group_heads(d.G));
+  int ub = kW;
+  while (units % ub) ub /= 2;
+  const int64_t wgs = (int64_t)d.n_layers * d.B * units / ub;
   const int64_t chunks = (k_max + kDecodeChunk - 1) / kDecodeChunk;
-  const int64_t most = (chunks + kW / hb - 1) / (kW / hb);
+  const int64_t most = (chunks + kW / ub - 1) / (kW / ub);
   int64_t n = 2 * kCUs / wgs;
   if (n > most) n = most;
-  return {hb, n < 1 ? 1 : (int)n};
+  return {nh, ub, n < 1 ? 1 : (int)n};
 }
 int decode_tokens(const QuantDims& d) {
   const int64_t n = (int64_t)d.window + d.n_sink;
@@ -334,12 +451,19 @@ size_t quant_part_bytes(const QuantDims& d, int n_split) {
                       : 0);
 }
 
-template <int BITS, bool INDEXED>
-void launch_kernel(const QuantArgs& a, int hb, unsigned blocks, hipStream_t s) {
-  if (hb == 8) quant_decode_kernel<BITS, INDEXED, 8><<<blocks, kW * 64, 0, s>>>(a);
-  else if (hb == 4) quant_decode_kernel<BITS, INDEXED, 4><<<blocks, kW * 64, 0, s>>>(a);
-  else if (hb == 2) quant_decode_kernel<BITS, INDEXED, 2><<<blocks, kW * 64, 0, s>>>(a);
-  else quant_decode_kernel<BITS, INDEXED, 1><<<blocks, kW * 64, 0, s>>>(a);
+template <int BITS, int NH, bool INDEXED>
+void launch_kernel(const QuantArgs& a, int ub, unsigned blocks, hipStream_t s) {
+  if (ub == 4) quant_decode_kernel<BITS, NH, INDEXED, 4><<<blocks, kW * 64, 0, s>>>(a);
+  else if (ub == 2) quant_decode_kernel<BITS, NH, INDEXED, 2><<<blocks, kW * 64, 0, s>>>(a);
+  else quant_decode_kernel<BITS, NH, INDEXED, 1><<<blocks, kW * 64, 0, s>>>(a);
+}
+
+template <bool INDEXED>
+void launch_kernel(const QuantArgs& a, int bits, const QuantPlan& p, unsigned blocks,
+                   hipStream_t s) {
+  if (bits == 8) launch_kernel<8, 1, INDEXED>(a, p.ub, blocks, s);
+  else if (p.nh == 2) launch_kernel<4, 2, INDEXED>(a, p.ub, blocks, s);
+  else launch_kernel<4, 1, INDEXED>(a, p.ub, blocks, s);
 }
 
 hipError_t launch_quant(const QuantDims& d, int k_max, int n_sink, const uint16_t* q,
@@ -377,15 +501,10 @@ hipError_t launch_quant(const QuantDims& d, int k_max, int n_sink, const uint16_
     a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) +
                                          quant_part_acc_bytes(d, p.n_split));
   }
-  const int64_t blocks = (int64_t)d.n_layers * d.B * d.H_kv * a.R / p.hb * p.n_split;
+  const int64_t blocks = (int64_t)d.n_layers * d.B * d.H_kv / p.nh * a.R / p.ub * p.n_split;
   if (blocks > INT32_MAX / (kW * 64)) return hipErrorInvalidValue;
-  if (d.bits == 4) {
-    if (idx) launch_kernel<4, true>(a, p.hb, (unsigned)blocks, s);
-    else launch_kernel<4, false>(a, p.hb, (unsigned)blocks, s);
-  } else {
-    if (idx) launch_kernel<8, true>(a, p.hb, (unsigned)blocks, s);
-    else launch_kernel<8, false>(a, p.hb, (unsigned)blocks, s);
-  }
+  if (idx) launch_kernel<true>(a, d.bits, p, (unsigned)blocks, s);
+  else launch_kernel<false>(a, d.bits, p, (unsigned)blocks, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_split == 1) return e;
   DecodeArgs m{};
