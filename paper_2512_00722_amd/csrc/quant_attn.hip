@@ -124,6 +124,96 @@ __device__ __forceinline__ void quant_unit_by_token(const QuantUnit& u, int h, f
   }
 }
 
+// The matrix cores' 16 columns hold 16 / GW copies of the GW query heads of a KV head.
+// S^T comes out the same in every copy; of a lane's eight tokens copy L takes numbers
+// 8 GW / 16 L .., so that the softmax of a token is worked out once.  In the second
+// product a copy's column then has the tokens of its own as its lanes made them, and in
+// the places of the others', which it would leave empty, their weights' lower parts: the
+// copies' sums together are that of all tokens by weights of three bf16 numbers
+// (2^-26 relative at most), for GW = 4 in one multiplication instead of three, for GW = 8
+// in two (32 layers x 8 sequences x 32768 tokens, 4 heads of each of 8 KV heads, 4 bits: 1391
+// us, with three multiplications of everything 1583).
+template <int GW>
+struct Columns {
+  static constexpr int COPIES = 16 / GW, OWN = 8 / COPIES;  // tokens of a copy
+  static constexpr int MULS = GW == 4 ? 1 : GW == 8 ? 2 : 3;
+
+  // v of the copies in MASK (bits: lanes 4 b .. 4 b + 3 of 16), rotated by ROT lanes; else old
+  template <int ROT, int MASK>
+  static __device__ __forceinline__ uint32_t put(uint32_t old, uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)v, ROT == 0 ? 0xE4 : 0x120 + ROT,
+                                                 0xf, MASK, false);
+  }
+  template <int MASK>
+  static __device__ __forceinline__ float choose(float old, float v) {
+    return __uint_as_float(put<0, MASK>(__float_as_uint(old), __float_as_uint(v)));
+  }
+  // A lane's own values of its eight.
+  static __device__ __forceinline__ void own(const float (&p)[8], float (&q)[OWN]) {
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+      q[i] = p[i];
+      if constexpr (GW == 4) {
+        q[i] = choose<2>(q[i], p[2 + i]);
+        q[i] = choose<4>(q[i], p[4 + i]);
+        q[i] = choose<8>(q[i], p[6 + i]);
+      } else if constexpr (GW == 8) {
+        q[i] = choose<12>(q[i], p[4 + i]);
+      }
+    }
+  }
+  // The operands of the second product, of a lane's own weights (which are used up).
+  static __device__ __forceinline__ void weights(float (&q)[OWN], bf16x8 (&w)[MULS]) {
+    uint32_t part[3][OWN / 2];
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+#pragma unroll
+      for (int j = 0; j < OWN / 2; ++j) {
+        const bf16x2 x = __builtin_convertvector(floatx2{q[2 * j], q[2 * j + 1]}, bf16x2);
+        part[k][j] = __builtin_bit_cast(uint32_t, x);
+        q[2 * j] -= (float)x[0];
+        q[2 * j + 1] -= (float)x[1];
+      }
+    uint32_t r[MULS][4];
+    if constexpr (GW == 4) {
+      r[0][0] = put<8, 4>(put<4, 2>(put<0, 1>(0, part[0][0]), part[1][0]), part[2][0]);
+      r[0][1] = put<8, 8>(put<4, 4>(put<0, 2>(0, part[0][0]), part[1][0]), part[2][0]);
+      r[0][2] = put<8, 1>(put<4, 8>(put<0, 4>(0, part[0][0]), part[1][0]), part[2][0]);
+      r[0][3] = put<8, 2>(put<4, 1>(put<0, 8>(0, part[0][0]), part[1][0]), part[2][0]);
+    } else if constexpr (GW == 8) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        r[0][j] = put<8, 12>(part[0][j], part[1][j]);
+        r[0][2 + j] = put<8, 3>(part[0][j], part[1][j]);
+        r[1][j] = put<0, 3>(0, part[2][j]);
+        r[1][2 + j] = put<0, 12>(0, part[2][j]);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 3; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[k][j] = part[k][j];
+    }
+#pragma unroll
+    for (int k = 0; k < MULS; ++k)
+      w[k] = __builtin_bit_cast(bf16x8, make_uint4(r[k][0], r[k][1], r[k][2], r[k][3]));
+  }
+  // The sum of the copies.
+  static __device__ __forceinline__ float sum(float v) {
+    if constexpr (GW == 4) v += dpp_f<0x124>(v);
+    if constexpr (GW <= 8) v += dpp_f<0x128>(v);
+    return v;
+  }
+};
+
+// Where a 16-byte piece of a row of V in bf16 stands among the row's 16.  A transposing
+// read takes pieces 2 db and 2 db + 1 of eight rows 4 a .. 4 a + 3, 4 a + 4 .. at a time, over
+// all banks; a write takes 8 pieces 4 kg + s, kg = 0 .. 3, of a row of two heads (8 bits: of
+// one head 2 p + s, p = 0 .. 7), over half of them, so that those have to differ modulo 8.
+__device__ __forceinline__ int v_place(int h, int row, int piece) {
+  return piece ^ ((row & 3) << 2 | (row >> 2 & 1) << 1 | (row >> 3 & 1)) ^ (piece >> 3) ^ 2 * h;
+}
+
 // LDS of a wavefront: V in bf16, [NH][32 tokens][256 bytes], and before it the chunk's K as
 // it is held; scales [32 tokens][NH][8].
 template <int NH>
@@ -139,16 +229,18 @@ struct WaveTile {
 // through LDS as it is held, V as bf16 (from where it is read transposed); both by the
 // wavefront itself, so that none waits for another.  Lane (r16, kg) then has dimensions
 // 32 kg .. of K of tokens r16 and 16 + r16.  Results as decode_unit's, for each head.
-template <int BITS, int NH, bool INDEXED>
+template <int BITS, int NH, int GW, bool INDEXED>
 __device__ __forceinline__ void quant_unit(const QuantUnit& u, WaveTile<NH>& T, float (&m_run)[NH],
                                            float (&l_run)[NH], floatx4 (&acc)[NH][8]) {
+  using C = Columns<GW>;
   constexpr int P = NH * BITS;         // pieces of a token's row
   constexpr int RI = 64 / P;           // rows of a load
   constexpr int NI = kDecodeChunk / RI;
   constexpr int SP = 16 * 8 / BITS / 8;  // bf16 pieces of 8 elements of a piece
   const int lane = threadIdx.x & 63;
-  const int r16 = lane & 15;  // head of this lane; token of a K tile row
+  const int r16 = lane & 15;  // column of this lane; token of a K tile row
   const int kg = lane >> 4;
+  const int head = r16 % GW;
   const int lrow = lane / P, lpiece = lane % P;   // of a load
   const int lhead = lpiece / BITS, lpart = lpiece % BITS;
   bf16x8 qf[NH][4];  // Q^T: column r16, dimensions 32 kg + 8 s ..
@@ -156,9 +248,9 @@ __device__ __forceinline__ void quant_unit(const QuantUnit& u, WaveTile<NH>& T, 
   for (int h = 0; h < NH; ++h)
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const uint4 w = r16 < u.heads ? ldg16(u.q + h * u.q_stride + r16 * kHeadDim + kGroup * kg +
-                                            8 * s)
-                                    : make_uint4(0, 0, 0, 0);
+      const uint4 w = head < u.heads ? ldg16(u.q + h * u.q_stride + head * kHeadDim + kGroup * kg +
+                                             8 * s)
+                                     : make_uint4(0, 0, 0, 0);
       qf[h][s] = __builtin_bit_cast(bf16x8, w);
     }
   uint4 kr[NI], vr[NI];
@@ -217,7 +309,7 @@ __device__ __forceinline__ void quant_unit(const QuantUnit& u, WaveTile<NH>& T, 
     return K + row * 16 * P + 16 * (piece ^ (P == 8 ? row >> 1 & 7 : row >> 2 & 3));
   };
   auto v_at = [&](int h, int row, int piece) {
-    return T.v[h] + row * kHeadDim + ((piece ^ swizzle(row) ^ 2 * h) << 3);
+    return T.v[h] + row * kHeadDim + (v_place(h, row, piece) << 3);
   };
   // transposed V: tokens 16 t + 4 kg .. + 3, dimensions 16 db + r16
   auto get_v = [&](int h, int t, int db) {
@@ -283,65 +375,85 @@ __device__ __forceinline__ void quant_unit(const QuantUnit& u, WaveTile<NH>& T, 
     __builtin_amdgcn_sched_barrier(0);
     wave_sync_lds();
 
-    const int valid = u.valid(c);
+    // S[head r16][token 16 t + 4 kg + i], of all heads step by step: their chains of
+    // instructions fill each other's gaps.
+    float p[NH][8], mx[NH];
 #pragma unroll
-    for (int h = 0; h < NH; ++h) {
-      floatx4 s[2];
+    for (int h = 0; h < NH; ++h)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        s[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+        floatx4 s{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(elements8<BITS>(kf[h][t], i, ks[h][t]),
-                                                         qf[h][i], s[t], 0, 0, 0);
+          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(elements8<BITS>(kf[h][t], i, ks[h][t]),
+                                                      qf[h][i], s, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[h][4 * t + i] = s[i];
       }
-      // S[head r16][token 16 t + 4 kg + i]
-      float p[8];
+    const int valid = u.valid(c);
+    if (valid < kDecodeChunk) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = s[i / 4][i % 4];
-      if (valid < kDecodeChunk) {
+      for (int i = 0; i < 8; ++i)
+        if (16 * (i / 4) + 4 * kg + i % 4 >= valid)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (16 * (i / 4) + 4 * kg + i % 4 >= valid) p[i] = -INFINITY;
-      }
-      float mx = -INFINITY;
+          for (int h = 0; h < NH; ++h) p[h][i] = -INFINITY;
+    }
+    bool more = false;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) mx = fmaxf(mx, p[i]);
-      mx = quad_max(mx) * u.scale_log2;
-      if (__any(mx > m_run[h])) {
-        const float mn = fmaxf(m_run[h], mx);
+    for (int h = 0; h < NH; ++h) {
+      mx[h] = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mx[h] = fmaxf(mx[h], p[h][i]);
+      mx[h] = quad_max(mx[h]) * u.scale_log2;
+      more |= mx[h] > m_run[h];
+    }
+    if (__any(more)) {  // seldom but in the first chunks
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
+        const float mn = fmaxf(m_run[h], mx[h]);
         const float alpha = exp2_fast(m_run[h] - mn);
         m_run[h] = mn;
         l_run[h] *= alpha;
 #pragma unroll
         for (int db = 0; db < 8; ++db) acc[h][db] *= alpha;
       }
+    }
+    bf16x8 w[NH][C::MULS];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        p[i] = exp2_fast(fmaf(p[i], u.scale_log2, -m_run[h]));
-        l_run[h] += p[i];
+    for (int h = 0; h < NH; ++h) {
+      float q[C::OWN];
+      C::own(p[h], q);
+#pragma unroll
+      for (int i = 0; i < C::OWN; ++i) {
+        q[i] = exp2_fast(fmaf(q[i], u.scale_log2, -m_run[h]));
+        l_run[h] += q[i];
       }
-      // Weights enter as three bf16 numbers, 2^-26 relative at most, as over bf16 caches.
-      const bf16x8 ph = to_bf16x8(p), pl = next_bf16x8(p, ph), pt = next_bf16x8(p, pl);
-      // slots 8 kg .. + 7 of a multiplication: tokens 4 kg .. + 3 and 16 + 4 kg .. + 3
+      C::weights(q, w[h]);
+    }
+    // slots 8 kg .. + 7 of a multiplication: tokens 4 kg .. + 3 and 16 + 4 kg .. + 3
 #pragma unroll
-      for (int db = 0; db < 8; ++db) {
+    for (int db = 0; db < 8; ++db)
+#pragma unroll
+      for (int h = 0; h < NH; ++h) {
         const bf16x8 vf =
             __builtin_shufflevector(get_v(h, 0, db), get_v(h, 1, db), 0, 1, 2, 3, 4, 5, 6, 7);
-        acc[h][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph, acc[h][db], 0, 0, 0);
-        acc[h][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl, acc[h][db], 0, 0, 0);
-        acc[h][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pt, acc[h][db], 0, 0, 0);
+#pragma unroll
+        for (int k = 0; k < C::MULS; ++k)
+          acc[h][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, w[h][k], acc[h][db], 0, 0, 0);
       }
-    }
     wave_sync_lds();  // the tile is rewritten by the next chunk
   }
 #pragma unroll
   for (int h = 0; h < NH; ++h) {
     float odd = 0.f;
+    l_run[h] = C::sum(l_run[h]);
 #pragma unroll
     for (int db = 0; db < 8; ++db)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) odd = fmaf(acc[h][db][i], 0.f, odd);
+      for (int i = 0; i < 4; ++i) {
+        acc[h][db][i] = C::sum(acc[h][db][i]);
+        odd = fmaf(acc[h][db][i], 0.f, odd);
+      }
     if (__any(odd != odd)) quant_unit_by_token<BITS, INDEXED>(u, h, m_run[h], l_run[h], acc[h]);
     l_run[h] = quad_sum(l_run[h]);
   }
@@ -349,7 +461,7 @@ __device__ __forceinline__ void quant_unit(const QuantUnit& u, WaveTile<NH>& T, 
 
 // UB units (NH KV heads and a column group each) of the same tokens side by side, kW / UB
 // wavefronts each.
-template <int BITS, int NH, bool INDEXED, int UB>
+template <int BITS, int NH, int GW, bool INDEXED, int UB>
 __global__ __launch_bounds__(kW * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void quant_decode_kernel(QuantArgs a) {
   __shared__ __align__(16) WaveTile<NH> tiles[kW];
@@ -383,7 +495,7 @@ void quant_decode_kernel(QuantArgs a) {
   u.scale_log2 = a.scale_log2;
   float m_run[NH], l_run[NH];
   floatx4 acc[NH][8];
-  quant_unit<BITS, NH, INDEXED>(u, tiles[wave], m_run, l_run, acc);
+  quant_unit<BITS, NH, GW, INDEXED>(u, tiles[wave], m_run, l_run, acc);
 
 #pragma unroll
   for (int h = 0; h < NH; ++h) leave_results(tiles[wave].v[h], ml[wave][h], m_run[h], l_run[h], acc[h]);
@@ -451,19 +563,26 @@ size_t quant_part_bytes(const QuantDims& d, int n_split) {
                       : 0);
 }
 
+template <int BITS, int NH, int GW, bool INDEXED>
+void launch_units(const QuantArgs& a, int ub, unsigned blocks, hipStream_t s) {
+  if (ub == 4) quant_decode_kernel<BITS, NH, GW, INDEXED, 4><<<blocks, kW * 64, 0, s>>>(a);
+  else if (ub == 2) quant_decode_kernel<BITS, NH, GW, INDEXED, 2><<<blocks, kW * 64, 0, s>>>(a);
+  else quant_decode_kernel<BITS, NH, GW, INDEXED, 1><<<blocks, kW * 64, 0, s>>>(a);
+}
+
 template <int BITS, int NH, bool INDEXED>
-void launch_kernel(const QuantArgs& a, int ub, unsigned blocks, hipStream_t s) {
-  if (ub == 4) quant_decode_kernel<BITS, NH, INDEXED, 4><<<blocks, kW * 64, 0, s>>>(a);
-  else if (ub == 2) quant_decode_kernel<BITS, NH, INDEXED, 2><<<blocks, kW * 64, 0, s>>>(a);
-  else quant_decode_kernel<BITS, NH, INDEXED, 1><<<blocks, kW * 64, 0, s>>>(a);
+void launch_columns(const QuantArgs& a, int ub, unsigned blocks, hipStream_t s) {
+  if (a.heads <= 4) launch_units<BITS, NH, 4, INDEXED>(a, ub, blocks, s);
+  else if (a.heads <= 8) launch_units<BITS, NH, 8, INDEXED>(a, ub, blocks, s);
+  else launch_units<BITS, NH, 16, INDEXED>(a, ub, blocks, s);
 }
 
 template <bool INDEXED>
 void launch_kernel(const QuantArgs& a, int bits, const QuantPlan& p, unsigned blocks,
                    hipStream_t s) {
-  if (bits == 8) launch_kernel<8, 1, INDEXED>(a, p.ub, blocks, s);
-  else if (p.nh == 2) launch_kernel<4, 2, INDEXED>(a, p.ub, blocks, s);
-  else launch_kernel<4, 1, INDEXED>(a, p.ub, blocks, s);
+  if (bits == 8) launch_columns<8, 1, INDEXED>(a, p.ub, blocks, s);
+  else if (p.nh == 2) launch_columns<4, 2, INDEXED>(a, p.ub, blocks, s);
+  else launch_columns<4, 1, INDEXED>(a, p.ub, blocks, s);
 }
 
 hipError_t launch_quant(const QuantDims& d, int k_max, int n_sink, const uint16_t* q,
