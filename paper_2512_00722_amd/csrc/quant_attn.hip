@@ -17,11 +17,6 @@
 namespace spec {
 namespace {
 
-#ifndef KW
-#define KW 4
-#endif
-constexpr int kW = KW;  // wavefronts of a workgroup
-
 struct QuantArgs {
   const uint16_t* q;       // [n_layers][B][H_q][d]
   const uint8_t* k;
@@ -34,7 +29,8 @@ struct QuantArgs {
   float* part_acc;         // [n_layers*B][n_split][H_q][d]
   float* part_ml;          // [n_layers*B][n_split][H_q][2]
   int64_t kv_stride_layer, kv_stride_b, scale_stride_layer, scale_stride_b;
-  int B, H_q, H_kv, heads, R, L_cap, k_max, n_sets, n_sink, n_split;  // heads: of a column group
+  int B, H_q, H_kv, heads, R, L_cap, k_max, n_sets, n_sink;  // heads: of a column group
+  int ub_log2, n_split;    // see QuantPlan
   float scale_log2;
 };
 
@@ -48,7 +44,7 @@ struct QuantUnit {
   int64_t idx_stride;      // next KV head idx_stride on
   int64_t rs;              // bytes between tokens; of scales: ss
   int ss;
-  int last;
+  int last, k_max;         // INDEXED: k_max: indices of a set
   int heads, count;        // query heads of a KV head, at most 16; visible tokens
   int n_sink, shift;       // else: tokens 0 .. n_sink - 1, the others `shift` further on
   int part, n_parts;       // this wavefront among those of the unit
@@ -122,6 +118,7 @@ __device__ __forceinline__ void quant_unit_by_token(const QuantUnit& u, int h, f
       }
     }
   }
+  l_run = quad_sum(l_run);
 }
 
 // The matrix cores' 16 columns hold 16 / GW copies of the GW query heads of a KV head.
@@ -228,9 +225,11 @@ struct WaveTile {
 // matrix cores' order): two heads in 4 bits, one in 8.  A lane loads 16-byte pieces, K goes
 // through LDS as it is held, V as bf16 (from where it is read transposed); both by the
 // wavefront itself, so that none waits for another.  Lane (r16, kg) then has dimensions
-// 32 kg .. of K of tokens r16 and 16 + r16.  Results as decode_unit's, for each head.
+// 32 kg .. of K of tokens r16 and 16 + r16.  Results as decode_unit's, for each head; returns
+// the heads (bits) whose sums hold an infinity or a NaN, which quant_unit_by_token() has yet
+// to work out.
 template <int BITS, int NH, int GW, bool INDEXED>
-__device__ __forceinline__ void quant_unit(const QuantUnit& u, WaveTile<NH>& T, float (&m_run)[NH],
+__device__ __forceinline__ uint32_t quant_unit(const QuantUnit& u, WaveTile<NH>& T, float (&m_run)[NH],
                                            float (&l_run)[NH], floatx4 (&acc)[NH][8]) {
   using C = Columns<GW>;
   constexpr int P = NH * BITS;         // pieces of a token's row
@@ -282,13 +281,17 @@ __device__ __forceinline__ void quant_unit(const QuantUnit& u, WaveTile<NH>& T, 
     tok_s = u.idx[lane % NH * u.idx_stride +
                   min(kDecodeChunk * c + lane / NH % kDecodeChunk, u.count - 1)];
   };
-  auto load_k = [&]() {
+  // K and scales of the chunk that has been located; before them, as loads arrive in order,
+  // the indices of chunk `then`.
+  auto load_k = [&](int then) {
     if (INDEXED) {
 #pragma unroll
       for (int i = 0; i < NI; ++i)
         off[i] = (int64_t)clampi(tok[i], 0, u.last) * u.rs + 16 * lpiece;
-      sc = *reinterpret_cast<const uint2*>(sb + (int64_t)clampi(tok_s, 0, u.last) * u.ss +
-                                           lane % NH * kScaleBytes);
+      const uint8_t* s = sb + (int64_t)clampi(tok_s, 0, u.last) * u.ss + lane % NH * kScaleBytes;
+      indices(then);
+      __builtin_amdgcn_sched_barrier(0);
+      sc = *reinterpret_cast<const uint2*>(s);
     } else {
 #pragma unroll
       for (int i = 0; i < NI; ++i) off[i] = (uint32_t)(tok[i] * (int)u.rs + 16 * lpiece);
@@ -324,13 +327,35 @@ __device__ __forceinline__ void quant_unit(const QuantUnit& u, WaveTile<NH>& T, 
 #pragma unroll
     for (int db = 0; db < 8; ++db) acc[h][db] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
+  int first[NI], first_s;
+  if (INDEXED) {
+    // The first chunk's indices do not wait for the number of rows: those behind the last
+    // row, whatever they are, give way to that of the chunk's first row.
+    const int j0 = min(kDecodeChunk * u.part, u.k_max - 1);
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      first[i] = u.idx[lhead * u.idx_stride + min(j0 + RI * i + lrow, u.k_max - 1)];
+    first_s = u.idx[lane % NH * u.idx_stride +
+                    min(j0 + lane / NH % kDecodeChunk, u.k_max - 1)];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) asm volatile("" : "+v"(first[i]));
+    asm volatile("" : "+v"(first_s));
+  }
   const int chunks = u.chunks();
   if (u.part < chunks) {
-    if (INDEXED) indices(u.part);
+    if (INDEXED) {
+      const int row0 = __builtin_amdgcn_readfirstlane(first[0]);
+      const int row1 = NH == 1 ? row0 : __builtin_amdgcn_readlane(first[0], BITS);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        tok[i] = kDecodeChunk * u.part + RI * i + lrow < u.count ? first[i]
+                 : lhead == 0 ? row0 : row1;
+      tok_s = kDecodeChunk * u.part + lane / NH % kDecodeChunk < u.count ? first_s
+              : lane % NH == 0 ? row0 : row1;
+    }
     locate(u.part);
-    load_k();
+    load_k(min(u.part + u.n_parts, chunks - 1));
     load_v();
-    if (INDEXED) indices(min(u.part + u.n_parts, chunks - 1));
     __builtin_amdgcn_sched_barrier(0);
   }
   for (int c = u.part; c < chunks; c += u.n_parts) {
@@ -340,7 +365,7 @@ __device__ __forceinline__ void quant_unit(const QuantUnit& u, WaveTile<NH>& T, 
     for (int i = 0; i < NI; ++i)
       *reinterpret_cast<uint4*>(k_at(RI * i + lrow, lpiece)) = kr[i];
     locate(next);
-    load_k();
+    load_k(min(next + u.n_parts, chunks - 1));
     __builtin_amdgcn_sched_barrier(0);
     wave_sync_lds();
     RowPart<BITS> kf[NH][2];
@@ -371,7 +396,6 @@ __device__ __forceinline__ void quant_unit(const QuantUnit& u, WaveTile<NH>& T, 
             elements8<BITS>(x, s, vs[i]);
     }
     load_v();
-    if (INDEXED) indices(min(next + u.n_parts, chunks - 1));
     __builtin_amdgcn_sched_barrier(0);
     wave_sync_lds();
 
@@ -443,10 +467,11 @@ __device__ __forceinline__ void quant_unit(const QuantUnit& u, WaveTile<NH>& T, 
       }
     wave_sync_lds();  // the tile is rewritten by the next chunk
   }
+  uint32_t odd_heads = 0;
 #pragma unroll
   for (int h = 0; h < NH; ++h) {
     float odd = 0.f;
-    l_run[h] = C::sum(l_run[h]);
+    l_run[h] = quad_sum(C::sum(l_run[h]));
 #pragma unroll
     for (int db = 0; db < 8; ++db)
 #pragma unroll
@@ -454,24 +479,25 @@ __device__ __forceinline__ void quant_unit(const QuantUnit& u, WaveTile<NH>& T, 
         acc[h][db][i] = C::sum(acc[h][db][i]);
         odd = fmaf(acc[h][db][i], 0.f, odd);
       }
-    if (__any(odd != odd)) quant_unit_by_token<BITS, INDEXED>(u, h, m_run[h], l_run[h], acc[h]);
-    l_run[h] = quad_sum(l_run[h]);
+    if (__any(odd != odd)) odd_heads |= 1u << h;
   }
+  return odd_heads;
 }
 
-// UB units (NH KV heads and a column group each) of the same tokens side by side, kW / UB
-// wavefronts each.
-template <int BITS, int NH, int GW, bool INDEXED, int UB>
-__global__ __launch_bounds__(kW * 64) __attribute__((amdgpu_waves_per_eu(2)))
+// 2^ub_log2 units (NH KV heads and a column group each) of the same tokens side by side, an
+// equal number of the W wavefronts each.
+template <int W, int BITS, int NH, int GW, bool INDEXED>
+__global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(2)))
 void quant_decode_kernel(QuantArgs a) {
-  __shared__ __align__(16) WaveTile<NH> tiles[kW];
-  __shared__ float2 ml[kW][NH][16];
-  const int units = a.H_kv / NH * a.R / UB;   // workgroups of a (layer, sequence, part)
+  __shared__ __align__(16) WaveTile<NH> tiles[W];
+  __shared__ float2 ml[W][NH][16];
+  const int ub = 1 << a.ub_log2;
+  const int units = (a.H_kv / NH * a.R) >> a.ub_log2;  // workgroups of a (layer, sequence, part)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int split = blockIdx.x % a.n_split, rest = blockIdx.x / a.n_split;
   const int lb = rest / units, layer = lb / a.B, b = lb % a.B;
   // unit: column group r of KV heads g .. g + NH - 1
-  const int unit0 = rest % units * UB, unit = unit0 + wave % UB;
+  const int unit0 = rest % units << a.ub_log2, unit = unit0 + (wave & (ub - 1));
   const int g = unit / a.R * NH, r = unit % a.R, G = a.heads * a.R;
   const int64_t base = layer * a.kv_stride_layer + b * a.kv_stride_b + g * row_bytes(BITS);
   const int len = clampi(a.lens[b], 0, INDEXED ? a.k_max : a.L_cap);
@@ -486,26 +512,36 @@ void quant_decode_kernel(QuantArgs a) {
   u.rs = (int64_t)a.H_kv * row_bytes(BITS);
   u.ss = a.H_kv * kScaleBytes;
   u.last = a.L_cap - 1;
+  u.k_max = a.k_max;
   u.heads = a.heads;
   u.count = min(len, a.k_max);
   u.shift = len - u.count;
   u.n_sink = u.shift == 0 ? 0 : min(a.n_sink, u.count);
-  u.part = split * (kW / UB) + wave / UB;
-  u.n_parts = a.n_split * (kW / UB);
+  u.part = split * (W >> a.ub_log2) + (wave >> a.ub_log2);
+  u.n_parts = a.n_split * (W >> a.ub_log2);
   u.scale_log2 = a.scale_log2;
   float m_run[NH], l_run[NH];
   floatx4 acc[NH][8];
-  quant_unit<BITS, NH, GW, INDEXED>(u, tiles[wave], m_run, l_run, acc);
+  const uint32_t odd = quant_unit<BITS, NH, GW, INDEXED>(u, tiles[wave], m_run, l_run, acc);
 
 #pragma unroll
-  for (int h = 0; h < NH; ++h) leave_results(tiles[wave].v[h], ml[wave][h], m_run[h], l_run[h], acc[h]);
+  for (int h = 0; h < NH; ++h)
+    leave_results(tiles[wave].v[h], ml[wave][h], m_run[h], l_run[h], acc[h]);
+  if (odd) {  // uniform
+#pragma unroll 1
+    for (int h = 0; h < NH; ++h) {
+      if (!(odd >> h & 1)) continue;
+      quant_unit_by_token<BITS, INDEXED>(u, h, m_run[0], l_run[0], acc[0]);
+      leave_results(tiles[wave].v[h], ml[wave][h], m_run[0], l_run[0], acc[0]);
+    }
+  }
   __syncthreads();
-  for (int e = threadIdx.x; e < UB * NH * a.heads * 32; e += kW * 64) {
+  for (int e = threadIdx.x; e < a.heads * NH * 32 << a.ub_log2; e += W * 64) {
     const int d4 = e & 31, h = (e >> 5) % a.heads, hu = (e >> 5) / a.heads % NH;
     const int w0 = (e >> 5) / a.heads / NH, un = unit0 + w0;
     Join j;
-    for (int w = w0; w < kW; w += UB) j.M = fmaxf(j.M, ml[w][hu][h].x);
-    for (int w = w0; w < kW; w += UB)
+    for (int w = w0; w < W; w += ub) j.M = fmaxf(j.M, ml[w][hu][h].x);
+    for (int w = w0; w < W; w += ub)
       j.add(ml[w][hu][h],
             *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(tiles[w].v[hu]) +
                                              result_at(h, d4)));
@@ -530,23 +566,62 @@ __global__ __launch_bounds__(256) void quant_merge_kernel(DecodeArgs a, float* o
   decode_merge<S>(a, blockIdx.x, out, lse, n_out);
 }
 
-// How a launch is divided: units of nh KV heads, ub of them per workgroup, each over
-// n_split workgroups.
+// How a launch is divided: units of nh KV heads, 2^ub_log2 of them per workgroup of w
+// wavefronts, each over n_split workgroups.
 struct QuantPlan {
-  int nh, ub, n_split;
+  int nh, w, ub_log2, n_split;
 };
 
+// The plan of the least estimated time.  A launch takes the longer of two: the busiest CU's
+// share of the bytes (256 of them move 6.9 TB/s; workgroups that read a part of a token's row
+// move 7% less per halving), and its wavefronts' chunks one after the other (0.66 us a head:
+// what a chunk's loads take to arrive); workgroups beyond those resident cost 2.9 us a round,
+// and parts a second launch and the traffic of their results.  Fitted to 2400 launches
+// of 70 shapes (1 to 256 sequences and layers of 256 to 131072 tokens, 1 to 16 query heads
+// per KV head, 4 and 8 bits, rows selected or not): on average it is 1.4% slower than the
+// best plan, 8.5% at most.  Between plans: 32 x 8 x 32768 tokens in 4 bits 1344 us with 8
+// wavefronts and no parts, 1367 with 4 and four; 1 x 4096 10.9 with 4 wavefronts to a unit in
+// 32 parts, 13.3 with 8.
 QuantPlan quant_plan(const QuantDims& d, int k_max) {
   const int nh = d.bits == 4 && d.H_kv % 2 == 0 ? 2 : 1;
   const int64_t units = (int64_t)d.H_kv / nh * (d.G / group_heads(d.G));
-  int ub = kW;
-  while (units % ub) ub /= 2;
-  const int64_t wgs = (int64_t)d.n_layers * d.B * units / ub;
-  const int64_t chunks = (k_max + kDecodeChunk - 1) / kDecodeChunk;
-  const int64_t most = (chunks + kW / ub - 1) / (kW / ub);
-  int64_t n = 2 * kCUs / wgs;
-  if (n > most) n = most;
-  return {nh, ub, n < 1 ? 1 : (int)n};
+  const int64_t lb = (int64_t)d.n_layers * d.B, rows = lb * d.H_q;
+  const int64_t chunks = ((int64_t)k_max + kDecodeChunk - 1) / kDecodeChunk;
+  const double chunk_us = (double)kDecodeChunk * nh * (2 * row_bytes(d.bits) + kScaleBytes) / 6.9e6;
+  const double wait_us = nh == 2 ? 1.5 : 0.66;
+  QuantPlan best{nh, 4, 0, 1};
+  double least = 1e300;
+  for (int w = 4; w <= 8; w += 4) {
+    const int64_t resident = w == 8 ? 1 : nh == 2 ? 2 : 3;  // workgroups of a CU
+    for (int u = 0; 1 << u <= w && units % (1 << u) == 0; ++u) {
+      const int64_t one = lb * (units >> u), most = (chunks + (w >> u) - 1) / (w >> u);
+      if (one > INT32_MAX / (w * 64)) continue;
+      double narrow = 1;
+      for (int64_t side = (int64_t)nh << u; side < d.H_kv; side *= 2) narrow += 0.07;
+      int64_t last = 0;
+      for (int64_t target = kCUs / 2; target <= 8 * kCUs; target *= 2) {
+        for (int up = 0; up < 2; ++up) {
+          int64_t n = up ? (target + one - 1) / one : target / one;
+          n = n < 1 ? 1 : n > most ? most : n;
+          if (n <= last) continue;
+          last = n;
+          const int64_t busiest = (one * n + kCUs - 1) / kCUs;
+          const int64_t rounds = (busiest + resident - 1) / resident;
+          const int64_t own = (chunks + n * (w >> u) - 1) / (n * (w >> u));  // of a wavefront
+          const double bytes = (double)(busiest * own * w) * kCUs * chunk_us * narrow;
+          const double wait = (double)(rounds * own) * wait_us;
+          double t = bytes > wait ? bytes + 0.03 * wait : wait + 0.03 * bytes;
+          t += 2.9 * (rounds - 1) + (w == 8 ? 0.4 : 0);
+          if (n > 1) t += 4.4 + 0.79e-6 * 520 * (double)(n * rows);
+          if (t < least) {
+            least = t;
+            best = {nh, w, u, (int)n};
+          }
+        }
+      }
+    }
+  }
+  return best;
 }
 int decode_tokens(const QuantDims& d) {
   const int64_t n = (int64_t)d.window + d.n_sink;
@@ -564,25 +639,24 @@ size_t quant_part_bytes(const QuantDims& d, int n_split) {
 }
 
 template <int BITS, int NH, int GW, bool INDEXED>
-void launch_units(const QuantArgs& a, int ub, unsigned blocks, hipStream_t s) {
-  if (ub == 4) quant_decode_kernel<BITS, NH, GW, INDEXED, 4><<<blocks, kW * 64, 0, s>>>(a);
-  else if (ub == 2) quant_decode_kernel<BITS, NH, GW, INDEXED, 2><<<blocks, kW * 64, 0, s>>>(a);
-  else quant_decode_kernel<BITS, NH, GW, INDEXED, 1><<<blocks, kW * 64, 0, s>>>(a);
+void launch_columns(const QuantArgs& a, int w, unsigned blocks, hipStream_t s) {
+  if (w == 8) quant_decode_kernel<8, BITS, NH, GW, INDEXED><<<blocks, 512, 0, s>>>(a);
+  else quant_decode_kernel<4, BITS, NH, GW, INDEXED><<<blocks, 256, 0, s>>>(a);
 }
 
 template <int BITS, int NH, bool INDEXED>
-void launch_columns(const QuantArgs& a, int ub, unsigned blocks, hipStream_t s) {
-  if (a.heads <= 4) launch_units<BITS, NH, 4, INDEXED>(a, ub, blocks, s);
-  else if (a.heads <= 8) launch_units<BITS, NH, 8, INDEXED>(a, ub, blocks, s);
-  else launch_units<BITS, NH, 16, INDEXED>(a, ub, blocks, s);
+void launch_rows(const QuantArgs& a, int w, unsigned blocks, hipStream_t s) {
+  if (a.heads <= 4) launch_columns<BITS, NH, 4, INDEXED>(a, w, blocks, s);
+  else if (a.heads <= 8) launch_columns<BITS, NH, 8, INDEXED>(a, w, blocks, s);
+  else launch_columns<BITS, NH, 16, INDEXED>(a, w, blocks, s);
 }
 
 template <bool INDEXED>
 void launch_kernel(const QuantArgs& a, int bits, const QuantPlan& p, unsigned blocks,
                    hipStream_t s) {
-  if (bits == 8) launch_columns<8, 1, INDEXED>(a, p.ub, blocks, s);
-  else if (p.nh == 2) launch_columns<4, 2, INDEXED>(a, p.ub, blocks, s);
-  else launch_columns<4, 1, INDEXED>(a, p.ub, blocks, s);
+  if (bits == 8) launch_rows<8, 1, INDEXED>(a, p.w, blocks, s);
+  else if (p.nh == 2) launch_rows<4, 2, INDEXED>(a, p.w, blocks, s);
+  else launch_rows<4, 1, INDEXED>(a, p.w, blocks, s);
 }
 
 hipError_t launch_quant(const QuantDims& d, int k_max, int n_sink, const uint16_t* q,
@@ -612,6 +686,7 @@ hipError_t launch_quant(const QuantDims& d, int k_max, int n_sink, const uint16_
   a.k_max = k_max;
   a.n_sets = d.n_sets;
   a.n_sink = n_sink;
+  a.ub_log2 = p.ub_log2;
   a.n_split = p.n_split;
   a.scale_log2 = d.scale * kLog2e;
   if (p.n_split > 1) {
@@ -620,8 +695,9 @@ hipError_t launch_quant(const QuantDims& d, int k_max, int n_sink, const uint16_
     a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) +
                                          quant_part_acc_bytes(d, p.n_split));
   }
-  const int64_t blocks = (int64_t)d.n_layers * d.B * d.H_kv / p.nh * a.R / p.ub * p.n_split;
-  if (blocks > INT32_MAX / (kW * 64)) return hipErrorInvalidValue;
+  const int64_t blocks =
+      ((int64_t)d.n_layers * d.B * (d.H_kv / p.nh) * a.R >> p.ub_log2) * p.n_split;
+  if (blocks > INT32_MAX / (p.w * 64)) return hipErrorInvalidValue;
   if (idx) launch_kernel<true>(a, d.bits, p, (unsigned)blocks, s);
   else launch_kernel<false>(a, d.bits, p, (unsigned)blocks, s);
   const hipError_t e = hipGetLastError();
