@@ -625,8 +625,7 @@ SPEC_API spec_status spec_evict(const spec_dense_dims* dm, const spec_bounded* c
  * Sizes beyond a launch give SPEC_ERR_UNSUPPORTED: those of the decode entry points
  * above (B, n_layers or H_kv above 65535; n_layers B H_kv above 2^21; n_layers B H_q above
  * 2^26; more than 2^22 groups of query heads), L_cap or T above 2^30, and for
- * spec_quant_append and spec_quant_read n_layers B ceil(n H_kv / 64) above 2^24 - 1 for
- * n = T or k_max.                                                                */
+ * spec_quant_append and spec_quant_read n H_kv above 2^28 - 16 for n = T or k_max.   */
 typedef struct spec_quant_dims {
   int32_t B;         /* sequences in the batch                                 */
   int32_t L_cap;     /* token capacity of every cache row                      */

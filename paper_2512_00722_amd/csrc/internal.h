@@ -297,7 +297,8 @@ struct QuantCache {
   uint8_t* v;
   uint8_t* scales;
 };
-// Workgroups of spec_quant_append (rows = T) and spec_quant_read (k_max).
+// Workgroups, at most, of a layer and sequence of spec_quant_append (rows = T) and
+// spec_quant_read (k_max).
 int64_t quant_io_blocks(const QuantDims& d, int rows);
 hipError_t launch_quant_append(const QuantDims& d, const QuantCache& c, const uint16_t* k_new,
                                const uint16_t* v_new, const int32_t* pos, const int32_t* n_new,
