@@ -60,3 +60,10 @@ def compare(what, out, lse, q, k, v):
         err = np.abs(out[h] - want)
         assert (err <= tol).all(), (what, h, float((err / tol).max()))
         assert abs(lse[h] - wlse) <= tol_lse, (what, h, abs(lse[h] - wlse) / tol_lse)
+
+
+def read_head(cache, layer, b, g):
+    """K, V [L, D] float64 of one KV head, by the oracle."""
+    s = cache.scales[layer, b, :, g].cpu().numpy()
+    return tuple(qo.values(qo.unpack(t[layer, b, :, g].cpu().numpy(), cache.bits), s[:, j],
+                           cache.bits) for j, t in enumerate((cache.k, cache.v)))
