@@ -527,28 +527,6 @@ __device__ __forceinline__ Join join_parts(int n, At&& at) {
   return j;
 }
 
-// The partial results of a decode launch joined: 8 / S output rows per workgroup, 32
-// threads (4 dimensions each) and S of them.
-template <int S>
-__device__ __forceinline__ void decode_merge(const DecodeArgs& a, int block, float* out,
-                                             float* lse, int64_t n_out) {
-  const int64_t want = (int64_t)block * (8 / S) + (threadIdx.x >> 5) / S;
-  const int64_t orow = want < n_out ? want : n_out - 1;
-  const int d4 = threadIdx.x & 31;
-  const int h = (int)(orow % a.H_q);
-  const int64_t lb = orow / a.H_q;
-  const Join j = join_parts<S>(a.n_split, [&](int s, const float2*& ml, const float*& acc) {
-    const size_t prow = ((size_t)lb * a.n_split + s) * a.H_q + h;
-    ml = reinterpret_cast<const float2*>(a.part_ml) + prow;
-    acc = a.part_acc + prow * kHeadDim;
-  });
-  if (want >= n_out || (threadIdx.x >> 5) % S != 0) return;
-  const float inv = j.inv();
-  reinterpret_cast<float4*>(out + orow * kHeadDim)[d4] =
-      make_float4(j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv);
-  if (lse && d4 == 0) lse[orow] = j.lse();
-}
-
 // Groups of 32 threads that join a row of n partial results: one per eight, whose
 // loads are a single round trip.  Calls launch(integral constant).
 template <class F>

@@ -28,7 +28,7 @@ constexpr int kCUs = 256;
 
 // ---- workspace geometry (every region aligned to 256 bytes) -------------
 constexpr size_t kAlign = 256;
-inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+constexpr size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 // Retrieval scoring: tokens per workgroup of the logits kernel.  A CU streams
 // ~31 GB/s however many workgroups it holds, so the busiest CU sets the time:
@@ -286,12 +286,20 @@ struct EvictArgs {
 hipError_t launch_evict(const DenseDims& d, const EvictArgs& x, void* ws, hipStream_t s);
 
 // ---- caches held in 4 or 8 bits ------------------------------------------
+// How an attention launch is divided: units of nh KV heads, 2^ub_log2 of them per workgroup
+// of w wavefronts, each over n_split workgroups.
+struct QuantPlan {
+  int nh, w, ub_log2, n_split;
+  bool deal;  // n_split on average: sequences have parts by their lengths
+};
 // Dimensions of their entry points after validation.
 struct QuantDims {
   int B, L_cap, n_layers, H_q, H_kv, G, bits, T, window, n_sink, k_max, n_sets;
   int64_t kv_stride_layer, kv_stride_b, scale_stride_layer, scale_stride_b;
   float scale;
+  QuantPlan plan;  // attention: quant_plan()
 };
+QuantPlan quant_plan(const QuantDims& d, bool selected);
 struct QuantCache {
   uint8_t* k;
   uint8_t* v;
@@ -306,11 +314,10 @@ hipError_t launch_quant_append(const QuantDims& d, const QuantCache& c, const ui
 hipError_t launch_quant_read(const QuantDims& d, const QuantCache& c, const int32_t* idx,
                              const int32_t* counts, uint16_t* k_out, uint16_t* v_out,
                              hipStream_t s);
-size_t quant_decode_ws_bytes(const QuantDims& d);
+size_t quant_attn_ws_bytes(const QuantDims& d);
 hipError_t launch_quant_decode(const QuantDims& d, const uint16_t* q, const QuantCache& c,
                                const int32_t* lens, float* out, float* lse, void* ws,
                                hipStream_t s);
-size_t quant_sparse_ws_bytes(const QuantDims& d);
 hipError_t launch_quant_sparse_decode(const QuantDims& d, const uint16_t* q, const QuantCache& c,
                                       const int32_t* idx, const int32_t* counts, float* out,
                                       float* lse, void* ws, hipStream_t s);

@@ -26,11 +26,12 @@ struct QuantArgs {
   const int32_t* idx;      // [B][n_sets][k_max]
   float* out;              // [n_layers*B][H_q][d]; null: partial results are left
   float* lse;              // [n_layers*B][H_q] or null
-  float* part_acc;         // [n_layers*B][n_split][H_q][d]
-  float* part_ml;          // [n_layers*B][n_split][H_q][2]
+  float* part_acc;         // [n_layers][B n_split][H_q][d]: a layer's parts, by sequence
+  float* part_ml;          // [n_layers][B n_split][H_q][2]
   int64_t kv_stride_layer, kv_stride_b, scale_stride_layer, scale_stride_b;
   int B, H_q, H_kv, heads, R, L_cap, k_max, n_sets, n_sink;  // heads: of a column group
   int ub_log2, n_split;    // see QuantPlan
+  int32_t* parts;          // [B + 1], or null: where each sequence's parts begin (see Parts)
   float scale_log2;
 };
 
@@ -484,6 +485,79 @@ __device__ __forceinline__ uint32_t quant_unit(const QuantUnit& u, WaveTile<NH>&
   return odd_heads;
 }
 
+// Visible tokens of a sequence and how they lie.
+struct Visible {
+  int count, shift, n_sink;
+  __device__ __forceinline__ Visible(const QuantArgs& a, int b, int most) {
+    const int len = clampi(a.lens[b], 0, most);
+    count = min(len, a.k_max);
+    shift = len - count;
+    n_sink = shift == 0 ? 0 : min(a.n_sink, count);
+  }
+  __device__ __forceinline__ int chunks() const {
+    return (n_sink + kDecodeChunk - 1) / kDecodeChunk +
+           (count - n_sink + kDecodeChunk - 1) / kDecodeChunk;
+  }
+};
+
+// Sequences whose parts a wavefront can deal out (a lane each).  From the 64th of the
+// numbers of chunks, 2.9 times the mean and 63 more, or from 64, parts are at most B and a
+// third of all, so that one of them always fits where there are two per sequence.
+constexpr int kMostDealt = 64;
+
+// A layer's B n_split parts dealt to its sequences by their lengths, at least one each:
+// the least of 64 numbers q of chunks, from the mean up, with which parts of q chunks are
+// no more than there are.  Sequences of as many chunks have n_split each.  Every workgroup
+// works it out for itself (about 15 instructions a sequence): a ragged batch then takes as
+// long as its tokens, not as its longest sequence (us, 8 KV heads, at most: 8 layers x 16 of
+// 16384 tokens in 4 bits 209, with n_split each 232; 2 x 32 of 8192 67 and 85; 4 x 7 of 30000
+// in 8 bits 147 and 183).
+struct Parts {
+  int b, first, n;  // the sequence of part j, its first part and their number; b < 0: none
+  __device__ __forceinline__ Parts(const QuantArgs& a, int j, int most, int waves) {
+    const int lane = threadIdx.x & 63;
+    const int P = a.B * a.n_split;
+    const int own = lane < a.B ? (Visible(a, lane, most).chunks() + waves - 1) / waves : 0;
+    int start;  // of the lane's sequence
+    if (__all(lane >= a.B || own == __builtin_amdgcn_readfirstlane(own))) {
+      b = j / a.n_split;
+      first = b * a.n_split;
+      n = a.n_split;
+      start = min(lane, a.B) * a.n_split;
+    } else {
+      int64_t total = 0;
+      for (int s = 0; s < a.B; ++s) total += __builtin_amdgcn_readlane(own, s);
+      const int64_t mean = total < P ? 1 : total / P;
+      const float rq = 1.f / (float)(mean + mean * lane / 32 + lane);
+      auto parts = [](int chunks, float r) { return max(1, (int)ceilf((float)chunks * r)); };
+      int sum = 0;
+      for (int s = 0; s < a.B; ++s) sum += parts(__builtin_amdgcn_readlane(own, s), rq);
+      const uint64_t fits = __ballot(sum <= P);
+      const float r = __uint_as_float(
+          __builtin_amdgcn_readlane(__float_as_uint(rq), fits ? __builtin_ctzll(fits) : 63));
+      const int mine = parts(own, r);
+      b = -1;
+      first = n = start = 0;
+      int next = 0;
+      for (int s = 0; s < a.B; ++s) {
+        const int m = __builtin_amdgcn_readlane(mine, s);
+        if (lane == s) start = next;
+        if (j >= next && j < next + m) {
+          b = s;
+          first = next;
+          n = m;
+        }
+        next += m;
+      }
+      if (lane >= a.B) start = next;
+    }
+    if (blockIdx.x == 0 && threadIdx.x < 64) {
+      if (lane <= a.B) a.parts[lane] = min(start, P);
+      if (a.B == 64 && lane == 0) a.parts[64] = P;
+    }
+  }
+};
+
 // 2^ub_log2 units (NH KV heads and a column group each) of the same tokens side by side, an
 // equal number of the W wavefronts each.
 template <int W, int BITS, int NH, int GW, bool INDEXED>
@@ -494,13 +568,35 @@ void quant_decode_kernel(QuantArgs a) {
   const int ub = 1 << a.ub_log2;
   const int units = (a.H_kv / NH * a.R) >> a.ub_log2;  // workgroups of a (layer, sequence, part)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int split = blockIdx.x % a.n_split, rest = blockIdx.x / a.n_split;
-  const int lb = rest / units, layer = lb / a.B, b = lb % a.B;
+  const int most = INDEXED ? a.k_max : a.L_cap;
+  int layer, b, split, n_parts, group;
+  int64_t part;  // of all, where its results are left
+  if (a.parts) {  // parts by length: [layer][group of units][part]
+    const int per_layer = a.B * a.n_split, rest = blockIdx.x / per_layer;
+    const int j = blockIdx.x % per_layer;
+    group = rest % units;
+    layer = rest / units;
+    const Parts p(a, j, most, W >> a.ub_log2);
+    if (p.b < 0) return;  // uniform over the workgroup
+    b = p.b;
+    split = j - p.first;
+    n_parts = p.n;
+    part = (int64_t)layer * per_layer + j;
+  } else {        // [layer][sequence][group of units][part]
+    const int rest = blockIdx.x / a.n_split, lb = rest / units;
+    split = blockIdx.x % a.n_split;
+    n_parts = a.n_split;
+    group = rest % units;
+    layer = lb / a.B;
+    b = lb % a.B;
+    part = (int64_t)lb * a.n_split + split;
+  }
+  const int lb = layer * a.B + b;
   // unit: column group r of KV heads g .. g + NH - 1
-  const int unit0 = rest % units << a.ub_log2, unit = unit0 + (wave & (ub - 1));
+  const int unit0 = group << a.ub_log2, unit = unit0 + (wave & (ub - 1));
   const int g = unit / a.R * NH, r = unit % a.R, G = a.heads * a.R;
   const int64_t base = layer * a.kv_stride_layer + b * a.kv_stride_b + g * row_bytes(BITS);
-  const int len = clampi(a.lens[b], 0, INDEXED ? a.k_max : a.L_cap);
+  const Visible vis(a, b, most);
   QuantUnit u;
   u.q = a.q + ((int64_t)lb * a.H_q + g * G + r * a.heads) * kHeadDim;
   u.q_stride = G * kHeadDim;
@@ -514,11 +610,11 @@ void quant_decode_kernel(QuantArgs a) {
   u.last = a.L_cap - 1;
   u.k_max = a.k_max;
   u.heads = a.heads;
-  u.count = min(len, a.k_max);
-  u.shift = len - u.count;
-  u.n_sink = u.shift == 0 ? 0 : min(a.n_sink, u.count);
+  u.count = vis.count;
+  u.shift = vis.shift;
+  u.n_sink = vis.n_sink;
   u.part = split * (W >> a.ub_log2) + (wave >> a.ub_log2);
-  u.n_parts = a.n_split * (W >> a.ub_log2);
+  u.n_parts = n_parts * (W >> a.ub_log2);
   u.scale_log2 = a.scale_log2;
   float m_run[NH], l_run[NH];
   floatx4 acc[NH][8];
@@ -553,74 +649,117 @@ void quant_decode_kernel(QuantArgs a) {
           make_float4(j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv);
       if (a.lse && d4 == 0) a.lse[row] = j.lse();
     } else {
-      const int64_t row = ((int64_t)lb * a.n_split + split) * a.H_q + head;
+      const int64_t row = part * a.H_q + head;
       reinterpret_cast<float4*>(a.part_acc + row * kHeadDim)[d4] = j.o;
       if (d4 == 0) reinterpret_cast<float2*>(a.part_ml)[row] = make_float2(j.M, j.L);
     }
   }
 }
 
-template <int S>
-__global__ __launch_bounds__(256) void quant_merge_kernel(DecodeArgs a, float* out, float* lse,
-                                                          int64_t n_out) {
-  decode_merge<S>(a, blockIdx.x, out, lse, n_out);
-}
-
-// How a launch is divided: units of nh KV heads, 2^ub_log2 of them per workgroup of w
-// wavefronts, each over n_split workgroups.
-struct QuantPlan {
-  int nh, w, ub_log2, n_split;
+struct MergeArgs {
+  const float* part_acc;
+  const float* part_ml;
+  const int32_t* parts;
+  float* out;
+  float* lse;
+  int64_t n_out;
+  int B, H_q, n_split;
 };
+
+// 8 / S output rows per workgroup, 32 threads (4 dimensions each) and S of them.
+template <int S>
+__global__ __launch_bounds__(256) void quant_merge_kernel(MergeArgs a) {
+  const int64_t want = (int64_t)blockIdx.x * (8 / S) + (threadIdx.x >> 5) / S;
+  const int64_t orow = want < a.n_out ? want : a.n_out - 1;
+  const int d4 = threadIdx.x & 31;
+  const int h = (int)(orow % a.H_q);
+  const int64_t lb = orow / a.H_q;
+  int64_t first = lb * a.n_split;
+  int n = a.n_split;
+  if (a.parts) {
+    const int b = (int)(lb % a.B);
+    first = lb / a.B * a.B * a.n_split + a.parts[b];
+    n = a.parts[b + 1] - a.parts[b];
+  }
+  const Join j = join_parts<S>(n, [&](int s, const float2*& ml, const float*& acc) {
+    const int64_t row = (first + s) * a.H_q + h;
+    ml = reinterpret_cast<const float2*>(a.part_ml) + row;
+    acc = a.part_acc + row * kHeadDim;
+  });
+  if (want >= a.n_out || (threadIdx.x >> 5) % S != 0) return;
+  const float inv = j.inv();
+  reinterpret_cast<float4*>(a.out + orow * kHeadDim)[d4] =
+      make_float4(j.o.x * inv, j.o.y * inv, j.o.z * inv, j.o.w * inv);
+  if (a.lse && d4 == 0) a.lse[orow] = j.lse();
+}
 
 // The plan of the least estimated time.  A launch takes the longer of two: the busiest CU's
 // share of the bytes (256 of them move 6.9 TB/s; workgroups that read a part of a token's row
-// move 7% less per halving), and its wavefronts' chunks one after the other (0.66 us a head:
-// what a chunk's loads take to arrive); workgroups beyond those resident cost 2.9 us a round,
-// and parts a second launch and the traffic of their results.  Fitted to 2400 launches
-// of 70 shapes (1 to 256 sequences and layers of 256 to 131072 tokens, 1 to 16 query heads
-// per KV head, 4 and 8 bits, rows selected or not): on average it is 1.4% slower than the
-// best plan, 8.5% at most.  Between plans: 32 x 8 x 32768 tokens in 4 bits 1344 us with 8
-// wavefronts and no parts, 1367 with 4 and four; 1 x 4096 10.9 with 4 wavefronts to a unit in
-// 32 parts, 13.3 with 8.
-QuantPlan quant_plan(const QuantDims& d, int k_max) {
-  const int nh = d.bits == 4 && d.H_kv % 2 == 0 ? 2 : 1;
-  const int64_t units = (int64_t)d.H_kv / nh * (d.G / group_heads(d.G));
+// move 7% less per halving, and in 4 bits 45% where it is half a 128-byte line), and its
+// wavefronts' chunks one after the other (0.86 us, of two heads 1.5: what a chunk's loads
+// take to arrive); workgroups beyond those resident cost 2.9 us a round, and parts a second
+// launch and the traffic of their results.  Fitted to 4900 launches of 144 shapes (1 to 256
+// sequences and layers of 64 to 131072 tokens, 1 to 16 query heads per KV head, 4 and 8 bits,
+// rows selected or not): on average it is 1.6% slower than the best plan, 12% at most.
+// Between plans: 32 x 8 x 32768 tokens in 4 bits 1344 us with 8 wavefronts and no parts, 1367
+// with 4 and four; 1 x 4096 10.4 with 4 wavefronts to a unit in 24 parts, 13.3 with 8; 1 x 512
+// 8.3 in one part, 10.6 in two.
+QuantPlan make_plan(const QuantDims& d, int k_max, bool ragged) {
+  const int heads_groups = d.G / group_heads(d.G);
   const int64_t lb = (int64_t)d.n_layers * d.B, rows = lb * d.H_q;
-  const int64_t chunks = ((int64_t)k_max + kDecodeChunk - 1) / kDecodeChunk;
-  const double chunk_us = (double)kDecodeChunk * nh * (2 * row_bytes(d.bits) + kScaleBytes) / 6.9e6;
-  const double wait_us = nh == 2 ? 1.5 : 0.66;
-  QuantPlan best{nh, 4, 0, 1};
-  double least = 1e300;
-  for (int w = 4; w <= 8; w += 4) {
-    const int64_t resident = w == 8 ? 1 : nh == 2 ? 2 : 3;  // workgroups of a CU
-    for (int u = 0; 1 << u <= w && units % (1 << u) == 0; ++u) {
-      const int64_t one = lb * (units >> u), most = (chunks + (w >> u) - 1) / (w >> u);
-      if (one > INT32_MAX / (w * 64)) continue;
-      double narrow = 1;
-      for (int64_t side = (int64_t)nh << u; side < d.H_kv; side *= 2) narrow += 0.07;
-      int64_t last = 0;
-      for (int64_t target = kCUs / 2; target <= 8 * kCUs; target *= 2) {
-        for (int up = 0; up < 2; ++up) {
-          int64_t n = up ? (target + one - 1) / one : target / one;
-          n = n < 1 ? 1 : n > most ? most : n;
-          if (n <= last) continue;
-          last = n;
-          const int64_t busiest = (one * n + kCUs - 1) / kCUs;
-          const int64_t rounds = (busiest + resident - 1) / resident;
-          const int64_t own = (chunks + n * (w >> u) - 1) / (n * (w >> u));  // of a wavefront
-          const double bytes = (double)(busiest * own * w) * kCUs * chunk_us * narrow;
-          const double wait = (double)(rounds * own) * wait_us;
-          double t = bytes > wait ? bytes + 0.03 * wait : wait + 0.03 * bytes;
-          t += 2.9 * (rounds - 1) + (w == 8 ? 0.4 : 0);
-          if (n > 1) t += 4.4 + 0.79e-6 * 520 * (double)(n * rows);
-          if (t < least) {
-            least = t;
-            best = {nh, w, u, (int)n};
+  const int chunks = (k_max + kDecodeChunk - 1) / kDecodeChunk;
+  const int64_t all = lb * d.H_kv * chunks;  // of one head
+  QuantPlan best{1, 4, 0, 1, false};
+  float least = FLT_MAX;
+  int chunks_each = 1;
+  for (int nh = 1; nh <= 2; ++nh) {
+    if (nh == 2 && (d.bits == 8 || d.H_kv % 2)) continue;
+    // half lines pay for themselves only where a chunk or two of loads are all there is
+    if (nh == 1 && d.bits == 4 && d.H_kv % 2 == 0 && all > 64 * kCUs) continue;
+    const int64_t units = (int64_t)d.H_kv / nh * heads_groups;
+    const float chunk_us =
+        (float)kCUs * kDecodeChunk * nh * (2 * row_bytes(d.bits) + kScaleBytes) / 6.9e6f;
+    const float wait_us = nh == 2 ? 1.5f : 0.86f;
+    for (int w = 4; w <= 8; w += 4) {
+      const int resident = w == 8 ? 1 : nh == 2 ? 2 : 3;  // workgroups of a CU
+      for (int u = 0; 1 << u <= w && units % (1 << u) == 0; ++u) {
+        const int64_t one = lb * (units >> u);
+        if (one > INT32_MAX / (w * 64)) continue;
+        const int waves = w >> u, most = (chunks + waves - 1) / waves;
+        float narrow = nh == 1 && d.bits == 4 && d.H_kv > 1 ? 1.45f : 1.f;
+        for (int64_t side = (int64_t)nh << u; side < d.H_kv; side *= 2) narrow += 0.07f;
+        int last = 0;
+        for (int target = 1; target <= 8 * kCUs; target = target == 1 ? 32 : 2 * target) {
+          for (int up = 0; up < 2; ++up) {
+            const int64_t want = up ? (target + one - 1) / one : target / one;
+            const int n = want < 1 ? 1 : want > most ? most : (int)want;
+            if (n <= last) continue;
+            last = n;
+            const int busiest = (int)((one * n + kCUs - 1) / kCUs);
+            const int rounds = (busiest + resident - 1) / resident;
+            const int own = (chunks + n * waves - 1) / (n * waves);  // of a wavefront
+            const float bytes = (float)busiest * own * w * chunk_us * narrow;
+            const float wait = (float)rounds * own * wait_us;
+            float t = bytes > wait ? bytes + 0.02f * wait : wait + 0.02f * bytes;
+            t += 2.9f * (rounds - 1) + (w == 8 ? 0.4f : 0.f) + (nh == 2 ? 0.26f : 0.f);
+            if (n > 1) t += 4.7f + 0.71e-6f * 520 * (float)n * rows;
+            if (t < least) {
+              least = t;
+              best = {nh, w, u, n, false};
+              chunks_each = own;
+            }
           }
         }
       }
     }
   }
+  // Whole caches are seldom of one length: two parts per sequence to deal out where they are
+  // long (us, in 4 bits of equal and of ragged lengths: 8 layers x 32 of 8192 tokens at most 376
+  // and 244, not dealt 364 and 279; 32 x 8 of 32768 1398 and 928, 1389 and 945; in 8 bits 4 x 64
+  // of 4096 338 and 230, 350 and 250).
+  const bool dealt = d.B > 1 && d.B <= kMostDealt;
+  if (ragged && dealt && best.n_split == 1 && chunks_each >= 128) best.n_split = 2;
+  best.deal = dealt && best.n_split > 1 && chunks_each >= 8;
   return best;
 }
 int decode_tokens(const QuantDims& d) {
@@ -632,9 +771,11 @@ size_t quant_part_acc_bytes(const QuantDims& d, int n_split) {
                                 d.H_q)
                      : 0;
 }
+constexpr size_t kDealtBytes = align_up(sizeof(int32_t) * (kMostDealt + 1));
 size_t quant_part_bytes(const QuantDims& d, int n_split) {
   return quant_part_acc_bytes(d, n_split) +
-         (n_split > 1 ? align_up(sizeof(float) * 2 * (size_t)d.n_layers * d.B * n_split * d.H_q)
+         (n_split > 1 ? align_up(sizeof(float) * 2 * (size_t)d.n_layers * d.B * n_split * d.H_q) +
+                            kDealtBytes
                       : 0);
 }
 
@@ -662,7 +803,7 @@ void launch_kernel(const QuantArgs& a, int bits, const QuantPlan& p, unsigned bl
 hipError_t launch_quant(const QuantDims& d, int k_max, int n_sink, const uint16_t* q,
                         const QuantCache& c, const int32_t* idx, const int32_t* lens, float* out,
                         float* lse, void* ws, hipStream_t s) {
-  const QuantPlan p = quant_plan(d, k_max);
+  const QuantPlan p = d.plan;
   const int heads = group_heads(d.G);
   QuantArgs a{};
   a.q = q;
@@ -694,6 +835,9 @@ hipError_t launch_quant(const QuantDims& d, int k_max, int n_sink, const uint16_
     a.part_acc = static_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) +
                                          quant_part_acc_bytes(d, p.n_split));
+    if (p.deal)
+      a.parts = reinterpret_cast<int32_t*>(static_cast<char*>(ws) +
+                                           quant_part_bytes(d, p.n_split) - kDealtBytes);
   }
   const int64_t blocks =
       ((int64_t)d.n_layers * d.B * (d.H_kv / p.nh) * a.R >> p.ub_log2) * p.n_split;
@@ -702,26 +846,21 @@ hipError_t launch_quant(const QuantDims& d, int k_max, int n_sink, const uint16_
   else launch_kernel<false>(a, d.bits, p, (unsigned)blocks, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.n_split == 1) return e;
-  DecodeArgs m{};
-  m.part_acc = a.part_acc;
-  m.part_ml = a.part_ml;
-  m.n_split = p.n_split;
-  m.H_q = d.H_q;
   const int64_t n_out = (int64_t)d.n_layers * d.B * d.H_q;
+  const MergeArgs m{a.part_acc, a.part_ml, a.parts, out, lse, n_out, d.B, d.H_q, p.n_split};
   with_parts(p.n_split, [&](auto S) {
-    quant_merge_kernel<S.value><<<merge_grid(n_out, S.value), 256, 0, s>>>(m, out, lse, n_out);
+    quant_merge_kernel<S.value><<<merge_grid(n_out, S.value), 256, 0, s>>>(m);
   });
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t quant_decode_ws_bytes(const QuantDims& d) {
-  return quant_part_bytes(d, quant_plan(d, decode_tokens(d)).n_split);
+QuantPlan quant_plan(const QuantDims& d, bool selected) {
+  if (selected) return make_plan(d, d.k_max, false);
+  return make_plan(d, decode_tokens(d), decode_tokens(d) == d.L_cap);
 }
-size_t quant_sparse_ws_bytes(const QuantDims& d) {
-  return quant_part_bytes(d, quant_plan(d, d.k_max).n_split);
-}
+size_t quant_attn_ws_bytes(const QuantDims& d) { return quant_part_bytes(d, d.plan.n_split); }
 
 hipError_t launch_quant_decode(const QuantDims& d, const uint16_t* q, const QuantCache& c,
                                const int32_t* lens, float* out, float* lse, void* ws,

@@ -498,6 +498,7 @@ spec_status resolve_quant(const spec_quant_dims* dm, spec_quant_op op, spec::Qua
       o->scale_stride_layer < sc || o->scale_stride_layer % 8)
     return SPEC_ERR_INVALID;
   o->scale = dm->scale > 0.f ? dm->scale : 1.0f / sqrtf((float)dm->d);
+  if (attn) o->plan = spec::quant_plan(*o, op == SPEC_QUANT_SPARSE_DECODE);
   return SPEC_OK;
 }
 
@@ -519,19 +520,8 @@ spec_status resolve_quant_cache(const spec_quant_cache* c, spec::QuantCache* o) 
   return SPEC_OK;
 }
 
-size_t quant_ws_bytes(const spec::QuantDims& d, spec_quant_op op) {
-  switch (op) {
-    case SPEC_QUANT_APPEND:
-    case SPEC_QUANT_READ: return 0;
-    case SPEC_QUANT_DECODE: return spec::quant_decode_ws_bytes(d);
-    case SPEC_QUANT_SPARSE_DECODE: return spec::quant_sparse_ws_bytes(d);
-  }
-  return 0;
-}
-
-spec_status check_quant_ws(const spec::QuantDims& d, spec_quant_op op, const void* ws,
-                           size_t ws_bytes) {
-  const size_t need = quant_ws_bytes(d, op);
+spec_status check_quant_ws(const spec::QuantDims& d, const void* ws, size_t ws_bytes) {
+  const size_t need = spec::quant_attn_ws_bytes(d);
   if (need == 0) return SPEC_OK;
   if (!ws || ws_bytes < need) return SPEC_ERR_WORKSPACE;
   return aligned16(ws) ? SPEC_OK : SPEC_ERR_INVALID;
@@ -770,7 +760,7 @@ spec_status spec_quant_workspace_size(const spec_quant_dims* dm, spec_quant_op o
   spec::QuantDims d;
   const spec_status st = resolve_quant(dm, op, &d);
   if (st != SPEC_OK) return st;
-  *bytes = quant_ws_bytes(d, op);
+  *bytes = op == SPEC_QUANT_APPEND || op == SPEC_QUANT_READ ? 0 : spec::quant_attn_ws_bytes(d);
   return SPEC_OK;
 }
 
@@ -822,7 +812,7 @@ spec_status spec_quant_decode_attn(const spec_quant_dims* dm, const uint16_t* q,
   if (!q || !seq_lens || !out) return SPEC_ERR_INVALID;
   if (!aligned16(q) || !aligned4(seq_lens) || !aligned16(out) || (lse && !aligned4(lse)))
     return SPEC_ERR_INVALID;
-  if ((st = check_quant_ws(d, SPEC_QUANT_DECODE, ws, ws_bytes)) != SPEC_OK) return st;
+  if ((st = check_quant_ws(d, ws, ws_bytes)) != SPEC_OK) return st;
   const hipStream_t s = as_stream(stream);
   if (debug_on() && (st = debug_range(seq_lens, d.B, 0, d.L_cap, s)) != SPEC_OK) return st;
   return finish(hip_status(spec::launch_quant_decode(d, q, c, seq_lens, out, lse, ws, s)), s);
@@ -841,7 +831,7 @@ spec_status spec_quant_sparse_decode_attn(const spec_quant_dims* dm, const uint1
   if (!aligned16(q) || !aligned4(idx) || !aligned4(counts) || !aligned16(out) ||
       (lse && !aligned4(lse)))
     return SPEC_ERR_INVALID;
-  if ((st = check_quant_ws(d, SPEC_QUANT_SPARSE_DECODE, ws, ws_bytes)) != SPEC_OK) return st;
+  if ((st = check_quant_ws(d, ws, ws_bytes)) != SPEC_OK) return st;
   const hipStream_t s = as_stream(stream);
   if (debug_on() &&
       (st = debug_selection(d.B, d.k_max, d.n_sets, idx, counts, d.L_cap, s)) != SPEC_OK)

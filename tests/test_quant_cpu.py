@@ -196,7 +196,8 @@ def test_workspace_sizes(lib):
     assert lib.spec_quant_workspace_size(ctypes.byref(dims()), DECODE, None) == 1
     st, n = size(lib, dims(B=1, n_layers=1), DECODE)
     assert st == 0 and n >= 2 * 32 * 130 * 4 and n % 256 == 0     # in parts
-    assert size(lib, dims(B=64, n_layers=32), DECODE) == (0, 0)   # enough without
+    assert size(lib, dims(B=64, n_layers=32, window=512), DECODE) == (0, 0)   # enough without
+    assert size(lib, dims(B=64, n_layers=32), SPARSE) == (0, 0)
     # one device's plan for every device: the same size however often it is asked
     assert size(lib, dims(B=1, n_layers=1), DECODE)[1] == n
 
@@ -204,7 +205,8 @@ def test_workspace_sizes(lib):
 def test_plans_of_all_sizes(lib):
     """Sizing takes any shape within the limits (a plan exists), and a split is never of more
     parts than there are chunks of 32 tokens: at most rows x ceil(tokens / 32) partial results
-    of 130 floats, in two regions of whole 256 bytes."""
+    of 130 floats, in two regions of whole 256 bytes, and 512 for where up to 64 sequences'
+    parts begin."""
     rng = np.random.default_rng(5)
     for _ in range(3000):
         H_kv = int(rng.integers(1, 17))
@@ -218,7 +220,7 @@ def test_plans_of_all_sizes(lib):
         for op, tokens in ((DECODE, min(cap, w + sink)), (SPARSE, k)):
             st, need = size(lib, d, op)
             assert st == 0
-            assert need <= n * B * H_kv * G * -(-tokens // 32) * 130 * 4 + 512
+            assert need <= n * B * H_kv * G * -(-tokens // 32) * 130 * 4 + 1024
 
 
 # ------------------------------------------------------------------ the binding
