@@ -518,12 +518,13 @@ struct Parts {
     const int lane = threadIdx.x & 63;
     const int P = a.B * a.n_split;
     const int own = lane < a.B ? (Visible(a, lane, most).chunks() + waves - 1) / waves : 0;
-    int start;  // of the lane's sequence
+    int start, end;  // of the lane's sequence; of all
     if (__all(lane >= a.B || own == __builtin_amdgcn_readfirstlane(own))) {
       b = j / a.n_split;
       first = b * a.n_split;
       n = a.n_split;
-      start = min(lane, a.B) * a.n_split;
+      start = lane * a.n_split;
+      end = P;
     } else {
       int64_t total = 0;
       for (int s = 0; s < a.B; ++s) total += __builtin_amdgcn_readlane(own, s);
@@ -549,11 +550,11 @@ struct Parts {
         }
         next += m;
       }
-      if (lane >= a.B) start = next;
+      end = min(next, P);
     }
     if (blockIdx.x == 0 && threadIdx.x < 64) {
-      if (lane <= a.B) a.parts[lane] = min(start, P);
-      if (a.B == 64 && lane == 0) a.parts[64] = P;
+      if (lane < a.B) a.parts[lane] = min(start, P);
+      if (lane == 0) a.parts[a.B] = end;
     }
   }
 };
