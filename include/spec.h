@@ -621,6 +621,11 @@ SPEC_API spec_status spec_evict(const spec_dense_dims* dm, const spec_bounded* c
  * differences of the entry points over caches read in full (any G up to 128, any
  * H_kv, workspaces of the size that spec_quant_workspace_size() gives).  k and v must
  * be 16-byte aligned and scales 8-byte aligned, and their strides multiples of that.
+ * SPEC_DEBUG also reports new rows that lie outside the caches.
+ *
+ * A call divides a batch's work by seq_lens or counts, so that the last bits of a
+ * sequence's results may depend on the lengths of the sequences beside it; the same call
+ * gives the same bits.
  *
  * Sizes beyond a launch give SPEC_ERR_UNSUPPORTED: those of the decode entry points
  * above (B, n_layers or H_kv above 65535; n_layers B H_kv above 2^21; n_layers B H_q above

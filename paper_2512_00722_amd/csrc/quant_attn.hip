@@ -732,8 +732,9 @@ __global__ __launch_bounds__(256) void quant_merge_kernel(MergeArgs a) {
 // sequences and layers of 64 to 131072 tokens, 1 to 16 query heads per KV head, 4 and 8 bits,
 // rows selected or not): on average it is 1.6% slower than the best plan, 12% at most.
 // Between plans: 32 x 8 x 32768 tokens in 4 bits 1344 us with 8 wavefronts and no parts, 1367
-// with 4 and four; 1 x 4096 10.4 with 4 wavefronts to a unit in 24 parts, 13.3 with 8; 1 x 512
-// 8.3 in one part, 10.6 in two.
+// with 4 and four; 1 x 4096 6.2 and 3.9 to join the parts with 4 wavefronts to a unit in 32
+// parts, 7.7 and 2.7 with 8 in 16; 1 x 512 7.6 in one part, 5.4 and 2.6 in four, where
+// programs that launch one call after another wait 8.1 and 10.6.
 QuantPlan make_plan(const QuantDims& d, int k_max, bool ragged) {
   const int heads_groups = d.G / group_heads(d.G);
   const int64_t lb = (int64_t)d.n_layers * d.B, rows = lb * d.H_q;

@@ -27,6 +27,20 @@ def dev():
 @pytest.mark.parametrize("G", (2, 6, 16))
 @pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "n{}_b{}_l{}_h{}".format(*s))
 def test_plans(dev, shape, G, bits):
+    check_plan(dev, shape, G, bits)
+
+
+@pytest.mark.parametrize("bits", (4, 8))
+@pytest.mark.parametrize("G", (1, 17, 20, 48))
+@pytest.mark.parametrize("shape", [(1, 1, 200, 3), (1, 16, 700, 8), (4, 64, 96, 4), (8, 3, 8192, 2)],
+                         ids=lambda s: "n{}_b{}_l{}_h{}".format(*s))
+def test_column_groups(dev, shape, G, bits):
+    """One query head per KV head, and several groups of them: as many as there are, where
+    their number has no divisor up to 16."""
+    check_plan(dev, shape, G, bits)
+
+
+def check_plan(dev, shape, G, bits):
     n, B, L, H_kv = shape
     announce(f"plans {shape} {G} {bits}")
     cap = L + 5
