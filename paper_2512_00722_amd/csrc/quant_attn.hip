@@ -122,8 +122,9 @@ __device__ __forceinline__ void quant_unit_by_token(const QuantUnit& u, int h, f
   l_run = quad_sum(l_run);
 }
 
-// The matrix cores' 16 columns hold 16 / GW copies of the GW query heads of a KV head.
-// S^T comes out the same in every copy; of a lane's eight tokens copy L takes numbers
+// The matrix cores' 16 columns are 16 / GW copies of the GW query heads of a KV head.
+// S^T is worked out in the first (the others' queries are zeros, which cost less power: 1372
+// us for 1385 at the sizes below); of a lane's eight tokens copy L takes numbers
 // 8 GW / 16 L .., so that the softmax of a token is worked out once.  In the second
 // product a copy's column then has the tokens of its own as its lanes made them, and in
 // the places of the others', which it would leave empty, their weights' lower parts: the
@@ -142,21 +143,27 @@ struct Columns {
     return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)v, ROT == 0 ? 0xE4 : 0x120 + ROT,
                                                  0xf, MASK, false);
   }
-  template <int MASK>
+  template <int ROT, int MASK>
   static __device__ __forceinline__ float choose(float old, float v) {
-    return __uint_as_float(put<0, MASK>(__float_as_uint(old), __float_as_uint(v)));
+    return __uint_as_float(put<ROT, MASK>(__float_as_uint(old), __float_as_uint(v)));
   }
-  // A lane's own values of its eight.
+  // The first copy's v.
+  static __device__ __forceinline__ float first(float v) {
+    if constexpr (GW == 4) v = choose<12, 8>(choose<8, 4>(choose<4, 2>(v, v), v), v);
+    else if constexpr (GW == 8) v = choose<8, 12>(v, v);
+    return v;
+  }
+  // A lane's own values of the first copy's eight.
   static __device__ __forceinline__ void own(const float (&p)[8], float (&q)[OWN]) {
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
       q[i] = p[i];
       if constexpr (GW == 4) {
-        q[i] = choose<2>(q[i], p[2 + i]);
-        q[i] = choose<4>(q[i], p[4 + i]);
-        q[i] = choose<8>(q[i], p[6 + i]);
+        q[i] = choose<4, 2>(q[i], p[2 + i]);
+        q[i] = choose<8, 4>(q[i], p[4 + i]);
+        q[i] = choose<12, 8>(q[i], p[6 + i]);
       } else if constexpr (GW == 8) {
-        q[i] = choose<12>(q[i], p[4 + i]);
+        q[i] = choose<8, 12>(q[i], p[4 + i]);
       }
     }
   }
@@ -241,7 +248,6 @@ __device__ __forceinline__ uint32_t quant_unit(const QuantUnit& u, WaveTile<NH>&
   const int lane = threadIdx.x & 63;
   const int r16 = lane & 15;  // column of this lane; token of a K tile row
   const int kg = lane >> 4;
-  const int head = r16 % GW;
   const int lrow = lane / P, lpiece = lane % P;   // of a load
   const int lhead = lpiece / BITS, lpart = lpiece % BITS;
   bf16x8 qf[NH][4];  // Q^T: column r16, dimensions 32 kg + 8 s ..
@@ -249,9 +255,9 @@ __device__ __forceinline__ uint32_t quant_unit(const QuantUnit& u, WaveTile<NH>&
   for (int h = 0; h < NH; ++h)
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const uint4 w = head < u.heads ? ldg16(u.q + h * u.q_stride + head * kHeadDim + kGroup * kg +
-                                             8 * s)
-                                     : make_uint4(0, 0, 0, 0);
+      const uint4 w = r16 < u.heads ? ldg16(u.q + h * u.q_stride + r16 * kHeadDim + kGroup * kg +
+                                            8 * s)
+                                    : make_uint4(0, 0, 0, 0);
       qf[h][s] = __builtin_bit_cast(bf16x8, w);
     }
   uint4 kr[NI], vr[NI];
@@ -430,7 +436,7 @@ __device__ __forceinline__ uint32_t quant_unit(const QuantUnit& u, WaveTile<NH>&
       mx[h] = -INFINITY;
 #pragma unroll
       for (int i = 0; i < 8; ++i) mx[h] = fmaxf(mx[h], p[h][i]);
-      mx[h] = quad_max(mx[h]) * u.scale_log2;
+      mx[h] = C::first(quad_max(mx[h])) * u.scale_log2;
       more |= mx[h] > m_run[h];
     }
     if (__any(more)) {  // seldom but in the first chunks
