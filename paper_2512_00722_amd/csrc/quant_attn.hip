@@ -74,11 +74,21 @@ __device__ __forceinline__ int64_t token_of(const QuantUnit& u, int h, int j) {
   return j + (j < u.n_sink ? 0 : u.shift);
 }
 
+// Log2-unit logits from here on are 2 and more apart in 32 bits.  A weight 2^(s c - m) by one
+// fused multiply-add is that of the unrounded product s c, m that of the rounded one: below,
+// the greatest token weighs 1/2 to 2, which goes out in the division by the weights' sum; from
+// 2^31 on it could weigh 0 or infinity.
+constexpr float kFusedMost = 0x1p24f;
+
 // A wavefront's share token by token, without the matrix cores, for the rare sums that
-// hold an infinity or a NaN, as unit_by_token() has it for bf16 caches.
+// hold an infinity or a NaN, as unit_by_token() has it for bf16 caches, and for logits beyond
+// kFusedMost: there the logits are rounded before the maximum is taken off, so that the
+// greatest token weighs 1.  Below, weights are those of quant_unit(): equal logits weigh the
+// same in every wavefront, whichever way it went.
 template <int BITS, bool INDEXED>
 __device__ __forceinline__ void quant_unit_by_token(const QuantUnit& u, int h, float& m_run,
                                                     float& l_run, floatx4 (&acc)[8]) {
+#pragma clang fp contract(off)  // a logit's product and difference stay two roundings
   const int lane = threadIdx.x & 63, r16 = lane & 15, kg = lane >> 4;
   const uint16_t* q = u.q + h * u.q_stride + (r16 < u.heads ? r16 : 0) * kHeadDim + 4 * kg;
   const uint8_t* k = u.k + h * row_bytes(BITS);
@@ -105,9 +115,12 @@ __device__ __forceinline__ void quant_unit_by_token(const QuantUnit& u, int h, f
         s = fmaf(bf16lo(x.y), y[2], s);
         s = fmaf(bf16hi(x.y), y[3], s);
       }
-      s = quad_sum(s) * u.scale_log2;
+      const float sum = quad_sum(s);
+      s = sum * u.scale_log2;
       const float mn = fmaxf(m_run, s);
-      const float alpha = exp2_fast(m_run - mn), p = exp2_fast(s - mn);
+      const float alpha = exp2_fast(m_run - mn);
+      const float p =
+          exp2_fast(fabsf(mn) < kFusedMost ? fmaf(sum, u.scale_log2, -mn) : s - mn);
       m_run = mn;
       l_run = l_run * alpha + (kg == 0 ? p : 0.f);
 #pragma unroll
@@ -234,8 +247,8 @@ struct WaveTile {
 // through LDS as it is held, V as bf16 (from where it is read transposed); both by the
 // wavefront itself, so that none waits for another.  Lane (r16, kg) then has dimensions
 // 32 kg .. of K of tokens r16 and 16 + r16.  Results as decode_unit's, for each head; returns
-// the heads (bits) whose sums hold an infinity or a NaN, which quant_unit_by_token() has yet
-// to work out.
+// the heads (bits) whose sums hold an infinity or a NaN or whose logits go beyond kFusedMost,
+// which quant_unit_by_token() has yet to work out.
 template <int BITS, int NH, int GW, bool INDEXED>
 __device__ __forceinline__ uint32_t quant_unit(const QuantUnit& u, WaveTile<NH>& T,
                                                float (&m_run)[NH], float (&l_run)[NH],
@@ -488,7 +501,10 @@ __device__ __forceinline__ uint32_t quant_unit(const QuantUnit& u, WaveTile<NH>&
         odd[i] = fmaf(acc[h][db][i], 0.f, odd[i]);
       }
     const float any = (odd[0] + odd[1]) + (odd[2] + odd[3]);
-    if (__any(any != any)) odd_heads |= 1u << h;
+    // Maxima only rise: smaller ones than -kFusedMost before the last have weights of 0, or
+    // sums that the last one makes a NaN of.
+    const bool far = u.part < chunks && fabsf(m_run[h]) >= kFusedMost;
+    if (__any(any != any || far)) odd_heads |= 1u << h;
   }
   return odd_heads;
 }
