@@ -98,9 +98,12 @@ constexpr int tile_elems(bool half) { return half ? kTileElems / 2 : kTileElems;
 // hold an infinity or a NaN: an infinity times a weight's parts is not that times the
 // weight, and a token whose logit is -inf counts for nothing, whatever its row of V holds
 // (in a part of nothing but such tokens as well, which joins leave out).  As decode_unit
-// leaves them, l_run not yet added up over a head's lanes.
+// leaves them, l_run not yet added up over a head's lanes, and with its weights: a logit is
+// rounded before the maximum is taken off.  (By one fused operation a large one would weigh
+// something else than its equals in other wavefronts, from 2^31 on 0 or infinity.)
 __device__ __forceinline__ void unit_by_token(const DecodeUnit& u, float& m_run, float& l_run,
                                               floatx4 (&acc)[8]) {
+#pragma clang fp contract(off)
   const int lane = threadIdx.x & 63, r16 = lane & 15, kg = lane >> 4;
   const uint16_t* q = u.q + (r16 < u.heads ? r16 : 0) * kHeadDim + 4 * kg;
   auto four = [](const uint16_t* p) {

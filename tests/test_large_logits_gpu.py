@@ -11,7 +11,9 @@ that join in any order take no more.  The log-sum-exp is scale times that logit 
 the scale, log2(e), their product, that with the logit, the sum with log2(m), ln(2) and the
 product with it are a rounding each, 7 U of it, and log2(m) is off by less than 2^-18: 8 U are
 allowed and 2^-18 more.  Where the greatest logits are 0, they are the same with a
-log-sum-exp of log(m)."""
+log-sum-exp of log(m).  Weights that enter the products rounded to bf16 are off by 2^-8 of
+themselves, as two bf16 numbers by 2^-17, and an output in bf16 by 2^-8 of itself."""
+import itertools
 import math
 
 import numpy as np
@@ -57,9 +59,9 @@ def keys(kind, shape, seed, dev):
     return K
 
 
-def check(what, out, lse, q, k, v, skip=()):
+def check(what, out, lse, q, k, v, skip=(), more=0.0):
     """out [D], lse of one query q [D] over rows k, v [n][D] (float64); dimensions `skip` of
-    the output are not looked at."""
+    the output are not looked at; more: what weights and output are off by beside fp32."""
     if len(k) == 0:
         assert (out == 0).all() and lse == -math.inf, what
         return
@@ -68,11 +70,11 @@ def check(what, out, lse, q, k, v, skip=()):
     near = s == top
     rest = s[~near]
     assert len(rest) == 0 or rest.max() < top - 1000, what   # the inputs are as described
+    dims = [d for d in range(D) if d not in skip]
     rows = v[near]
     m = len(rows)
-    dims = [d for d in range(D) if d not in skip]
     err = np.abs(out - rows.mean(0))[dims]
-    tol = (m + 2) * db.U * np.abs(rows).mean(0)[dims]
+    tol = ((m + 2) * db.U + more) * np.abs(rows).mean(0)[dims]
     assert (err <= tol).all(), (what, m, top, out[dims][:4], rows.mean(0)[dims][:4])
     want = top + math.log(m)
     assert abs(lse - want) <= 8 * db.U * abs(want) + 2.0 ** -18, (what, m, lse, want)
@@ -136,3 +138,48 @@ def test_quantised_caches_beside_a_nan(dev, e, bits):
         for h in range(G * H_kv):
             check((b, h), out[0, b, h], lse[0, b, h], f64(q[0, b, h]), Kh[0, b, :m, h // G],
                   Vh[0, b, :m, h // G], skip=range(32, 64))
+
+
+# ------------------------------------------------------------------ caches in bf16
+
+# layers, KV heads, query heads of each, tokens, lengths
+BF16 = [(1, 2, 4, 40, [40, 1, 33]), (2, 3, 8, 300, [300, 65, 0]), (1, 1, 16, 1500, [1500, 999])]
+
+
+def bf16_case(case, j, kind, odd, dev):
+    """K, V; odd: an infinity in dimension 40 of V, which sends the sums the way of the rare
+    ones."""
+    n, H_kv, _, L, lens = BF16[case]
+    K = keys(kind, (n, len(lens), L, H_kv), 520 + 10 * case + j, dev)
+    V = normal((n, len(lens), L, H_kv, D), 620 + 10 * case + j, dev)
+    if odd:
+        V[:, :, 0, :, 40] = math.inf
+    Vh = f64(V)
+    return K, V, f64(K), np.where(np.isfinite(Vh), Vh, 0)
+
+
+@pytest.mark.parametrize("odd", (False, True), ids=("finite", "inf"))
+@pytest.mark.parametrize("e", EXPONENTS)
+def test_a_decode_step(dev, e, odd):
+    """Over all rows, and over selected ones."""
+    skip = (40,) if odd else ()
+    for case, (n, H_kv, G, L, lens) in enumerate(BF16):
+        q = queries((n, len(lens), G * H_kv, D), e, dev)
+        for j, kind in enumerate(("all", "some", "first")):
+            announce(f"large logits bf16 2^{e} {BF16[case]} {kind} {skip}")
+            K, V, Kh, Vh = bf16_case(case, j, kind, odd, dev)
+            rng = np.random.default_rng(720 + case)
+            idx = np.full((len(lens), L), 0)
+            for b, m in enumerate(lens):
+                idx[b, :m] = np.sort(rng.choice(L, m, replace=False))
+            dense = [f64(t) for t in spec.window_decode_attn(q, K, V, i32(lens, dev), window=L)]
+            sparse = [f64(t) for t in spec.sparse_decode_attn(q, K, V, i32(lens, dev),
+                                                              idx=i32(idx, dev))]
+            qh = f64(q)
+            for layer, b, h in itertools.product(range(n), range(len(lens)), range(G * H_kv)):
+                for what, (out, lse), rows, more in (
+                        ("dense", dense, np.arange(lens[b]), 0.0),
+                        ("sparse", sparse, idx[b, :lens[b]], 2.0 ** -17)):
+                    check((what, BF16[case], kind, layer, b, h), out[layer, b, h],
+                          lse[layer, b, h], qh[layer, b, h], Kh[layer, b, rows, h // G],
+                          Vh[layer, b, rows, h // G], skip, more)
