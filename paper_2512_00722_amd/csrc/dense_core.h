@@ -19,6 +19,12 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // weigh nothing from the first tile on.
 constexpr float kNoMax = -FLT_MAX;
 
+// Log2-unit logits from here on are 2 and more apart in 32 bits.  A weight 2^(s c - m) by one
+// fused multiply-add is that of the unrounded product s c, m that of the rounded one: below,
+// the greatest token weighs 1/2 to 2, which goes out in the division by the weights' sum; from
+// 2^31 on it could weigh 0 or infinity.
+constexpr float kFusedMost = 0x1p24f;
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Transposing LDS read: within each 16-lane group, lane i receives element

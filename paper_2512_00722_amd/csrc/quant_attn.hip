@@ -74,12 +74,6 @@ __device__ __forceinline__ int64_t token_of(const QuantUnit& u, int h, int j) {
   return j + (j < u.n_sink ? 0 : u.shift);
 }
 
-// Log2-unit logits from here on are 2 and more apart in 32 bits.  A weight 2^(s c - m) by one
-// fused multiply-add is that of the unrounded product s c, m that of the rounded one: below,
-// the greatest token weighs 1/2 to 2, which goes out in the division by the weights' sum; from
-// 2^31 on it could weigh 0 or infinity.
-constexpr float kFusedMost = 0x1p24f;
-
 // A wavefront's share token by token, without the matrix cores, for the rare sums that
 // hold an infinity or a NaN, as unit_by_token() has it for bf16 caches, and for logits beyond
 // kFusedMost: there the logits are rounded before the maximum is taken off, so that the

@@ -76,15 +76,18 @@ __device__ __forceinline__ Range window_range(const TileArgs& a, int p0, int i0,
 }
 
 // The same token by token, for the rare sums that hold infinities or NaNs: of rows that
-// a query does not see, or whose logit is -inf, they are selected away.  The wavefront's
-// tokens are j0 .. j0 + run - 1 and those `step` further on, up to j1.  A lane has the
-// dimensions 32 db + 8 e + 4 kg .. + 3 of its row, as the accumulators do.
+// a query does not see, or whose logit is -inf, they are selected away; and for logits
+// beyond kFusedMost, which are rounded before the maximum is taken off (below, weights are
+// those of the matrix cores' path).  The wavefront's tokens are j0 .. j0 + run - 1 and those
+// `step` further on, up to j1.  A lane has the dimensions 32 db + 8 e + 4 kg .. + 3 of its
+// row, as the accumulators do.
 template <bool WINDOW, class TokenOf>
 __device__ __forceinline__ void attend_by_token(const TileArgs& a, const uint16_t* q,
                                                 const uint16_t* k, const uint16_t* v, int64_t rs,
                                                 int kg, int j0, int j1, int run, int step, int pos,
                                                 TokenOf&& token_of, float& m_run, float& l_run,
                                                 floatx16 (&acc)[4]) {
+#pragma clang fp contract(off)  // a logit's product and difference stay two roundings
   auto four = [](const uint16_t* p, float (&f)[4]) {
     const uint2 x = *reinterpret_cast<const uint2*>(p);
     f[0] = bf16lo(x.x);
@@ -110,10 +113,11 @@ __device__ __forceinline__ void attend_by_token(const TileArgs& a, const uint16_
       for (int i = 0; i < 4; ++i) s = fmaf(x[i], y[i], s);
     }
     const bool see = !WINDOW || (t <= pos && (t < a.n_sink || t > pos - a.window));
-    s = pair_sum(s) * a.scale_log2;
-    s = see ? s : -INFINITY;
+    const float all = pair_sum(s), sum = see ? all : -INFINITY;
+    s = see ? all * a.scale_log2 : -INFINITY;
     const float mn = fmaxf(m_run, s);
-    const float alpha = exp2_fast(m_run - mn), p = exp2_fast(s - mn);
+    const float alpha = exp2_fast(m_run - mn);
+    const float p = exp2_fast(fabsf(mn) < kFusedMost ? fmaf(sum, a.scale_log2, -mn) : s - mn);
     m_run = mn;
     l_run = l_run * alpha + (kg == 0 ? p : 0.f);
 #pragma unroll
@@ -396,14 +400,15 @@ void tile_attn_kernel(TileArgs a) {
   // Where an infinity or a NaN got into the sums, they are taken again without the matrix
   // cores: a weight of 0 does not keep one of a row that this query does not see, or whose
   // logit is -inf, out of them (0 x NaN), nor is an infinity of one that it sees the
-  // product with a weight's parts.
+  // product with a weight's parts.  So they are where a row's logits go beyond kFusedMost
+  // (maxima only rise: those of before weigh 0, or leave a NaN).
   {
     float odd = 0.f;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
       for (int i = 0; i < 16; ++i) odd = fmaf(acc[db][i], 0.f, odd);
-    if (__any(odd != odd))
+    if (__any(odd != odd || (fabsf(m_run) >= kFusedMost && m_run != kNoMax)))
       attend_by_token<WINDOW>(a, a.q + orow * kD, a.k + base, a.v + base, rs, kg,
                               v0 + tw * NB * 32, v1, NB * 32, TOK, pos, token_of, m_run, l_run,
                               acc);

@@ -183,3 +183,53 @@ def test_a_decode_step(dev, e, odd):
                     check((what, BF16[case], kind, layer, b, h), out[layer, b, h],
                           lse[layer, b, h], qh[layer, b, h], Kh[layer, b, rows, h // G],
                           Vh[layer, b, rows, h // G], skip, more)
+
+
+@pytest.mark.parametrize("odd", (False, True), ids=("finite", "inf"))
+@pytest.mark.parametrize("e", EXPONENTS)
+def test_a_chunk_of_queries(dev, e, odd):
+    skip, T = (40,) if odd else (), 5
+    for case, (n, H_kv, G, L, lens) in enumerate(BF16):
+        q = queries((n, len(lens), T, G * H_kv, D), e, dev)
+        for j, kind in enumerate(("all", "some", "first")):
+            announce(f"large logits chunk 2^{e} {BF16[case]} {kind} {skip}")
+            K, V, Kh, Vh = bf16_case(case, j, kind, odd, dev)
+            own = [min(T, m) for m in lens]
+            out, lse = (f64(t) for t in spec.window_attn(q, K, V, i32(lens, dev), window=L,
+                                                         q_lens=i32(own, dev)))
+            qh = f64(q)
+            for layer, b, h in itertools.product(range(n), range(len(lens)), range(G * H_kv)):
+                for i in range(own[b]):
+                    p = lens[b] - own[b] + i + 1
+                    check((BF16[case], kind, layer, b, i, h), out[layer, b, i, h],
+                          lse[layer, b, i, h], qh[layer, b, i, h], Kh[layer, b, :p, h // G],
+                          Vh[layer, b, :p, h // G], skip, 2.0 ** -7)   # weights and output
+
+
+@pytest.mark.parametrize("odd", (False, True), ids=("finite", "inf"))
+@pytest.mark.parametrize("e", EXPONENTS)
+def test_a_shared_prefix(dev, e, odd):
+    """Levels of the prefix from 1, of the own tokens from 2: the greatest logits are
+    those of the one or the other."""
+    skip = (40,) if odd else ()
+    for n, H_kv, G, P, L, lens in ((1, 2, 4, 700, 90, [90, 0, 33]), (2, 1, 16, 100, 50, [50] * 6)):
+        announce(f"large logits prefix 2^{e} {P} {L} {skip}")
+        B = len(lens)
+        q = queries((n, B, G * H_kv, D), e, dev)
+        Kp, Vp = keys("all", (n, 1, P, H_kv), 541, dev)[:, 0], normal((n, P, H_kv, D), 641, dev)
+        K, V = keys("all", (n, B, L, H_kv), 542, dev), normal((n, B, L, H_kv, D), 642, dev)
+        K[..., 0] *= 2
+        if odd:
+            Vp[:, 3, :, 40] = math.inf
+            V[:, :, 2, :, 40] = -math.inf
+        out, lse = (f64(t) for t in spec.prefix_decode_attn(q, Kp.contiguous(), Vp, K, V,
+                                                            i32(lens, dev)))
+        ph, qh, oh = (f64(Kp), f64(Vp)), f64(q), (f64(K), f64(V))
+        for layer in range(n):
+            for b, m in enumerate(lens):
+                for h in range(G * H_kv):
+                    g = h // G
+                    k, v = (np.concatenate([x[layer, :, g], y[layer, b, :m, g]])
+                            for x, y in zip(ph, oh))
+                    check((P, layer, b, h), out[layer, b, h], lse[layer, b, h], qh[layer, b, h],
+                          k, v, skip, 2.0 ** -17)
