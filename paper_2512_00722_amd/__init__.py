@@ -1335,6 +1335,8 @@ def quant_read(cache: QuantCache, counts: torch.Tensor, idx: Optional[torch.Tens
         if st is not None:
             _check(st, "spec_quant_read")
             return tuple(out)
+    if out is not None and (len(out) != 2 or out[0] is None or out[1] is None):
+        raise ValueError("out must be two tensors (K, V)")
     dims = _quant_dims(cache)
     _i32(counts, "counts", dims.B)
     if idx is not None:
