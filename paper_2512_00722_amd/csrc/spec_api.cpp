@@ -502,14 +502,15 @@ spec_status resolve_quant(const spec_quant_dims* dm, spec_quant_op op, spec::Qua
   return SPEC_OK;
 }
 
-// New tokens' rows inside the caches: pos[b] in [0, L_cap - n_new[b]] (null: T).
+// New tokens' rows inside the caches: pos[b] in [0, L_cap - n_new[b]] (null: T); a sequence
+// without new ones has none outside.
 spec_status debug_append(const spec::QuantDims& d, const int32_t* pos, const int32_t* n_new,
                          hipStream_t s) {
   std::vector<int32_t> p, n((size_t)d.B, d.T);
   if (!d2h(p, pos, (size_t)d.B, s) || (n_new && !d2h(n, n_new, (size_t)d.B, s)))
     return SPEC_ERR_HIP;
   for (int b = 0; b < d.B; ++b)
-    if (p[b] < 0 || (int64_t)p[b] + n[b] > d.L_cap) return SPEC_ERR_INVALID;
+    if (n[b] > 0 && (p[b] < 0 || (int64_t)p[b] + n[b] > d.L_cap)) return SPEC_ERR_INVALID;
   return SPEC_OK;
 }
 
