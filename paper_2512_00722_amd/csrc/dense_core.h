@@ -78,11 +78,9 @@ __device__ __forceinline__ float quad_sum(float v) {
 }
 
 // Decode attention of up to 16 query heads of one KV head over a contiguous cache,
-// by some wavefronts: chunk c of 32 tokens belongs to wavefront c mod n_parts,
+// by some wavefronts: chunk c of kDecodeChunk tokens belongs to wavefront c mod n_parts,
 // whatever the length, so that it divides evenly and nothing but the length has to
 // arrive before the first rows are requested.
-constexpr int kDecodeChunk = 32;
-
 struct DecodeUnit {
   const uint16_t* q;    // the unit's first query head; heads are d apart
   const uint16_t* k;    // the sequence's rows of the KV head

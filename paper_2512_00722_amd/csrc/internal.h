@@ -244,6 +244,7 @@ struct DenseDims {
   float scale;
 };
 constexpr int kHeadDim = 128;
+constexpr int kDecodeChunk = 32;  // tokens that a wavefront of decode attention takes at a time
 // Query heads of a column group: all of a KV head's where there are at most 16, else
 // their largest divisor up to 16.
 inline int group_heads(int G) {
@@ -292,6 +293,8 @@ struct QuantPlan {
   int nh, w, ub_log2, n_split;
   bool deal;  // n_split on average: sequences have parts by their lengths
 };
+constexpr int kScaleBytes = 8;  // of a token and head: K's four groups, V's four
+constexpr int row_bytes(int bits) { return kHeadDim * bits / 8; }
 // Dimensions of their entry points after validation.
 struct QuantDims {
   int B, L_cap, n_layers, H_q, H_kv, G, bits, T, window, n_sink, k_max, n_sets;

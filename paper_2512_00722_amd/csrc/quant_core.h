@@ -15,13 +15,11 @@ namespace spec {
 
 // A row of a head: 4 lanes' parts of 32 elements, one group each.
 constexpr int kGroup = 32;
-constexpr int kScaleBytes = 8;  // of a token and head: K's four groups, V's four
 template <int BITS>
 struct RowPart {                // 32 elements
   uint4 w[BITS / 4];
 };
 constexpr int part_bytes(int bits) { return kGroup * bits / 8; }
-constexpr int row_bytes(int bits) { return kHeadDim * bits / 8; }
 
 // Byte i of `bytes`, as a scale operand: 2^(byte - 127), NaN for 255.
 __device__ __forceinline__ float scale_of(uint32_t bytes, int i) {
