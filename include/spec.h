@@ -608,10 +608,13 @@ SPEC_API spec_status spec_evict(const spec_dense_dims* dm, const spec_bounded* c
  * magnitude of a group,
  *     x^ = 2^X e(x 2^-X),  X the least integer with A <= 7 2^X (4 bits) or 448 2^X (8),
  * where e() rounds to the nearest element, ties to the even one, and beyond the
- * largest, 6 or 448, gives that: no element is off by more than half the spacing of
- * the elements at its magnitude.  X is clamped to [-111, 125] (8 bits: [-111, 119]).  A
- * group that holds a NaN or an infinity is NaN throughout.  Every x^ is a bf16 number (bytes
- * that spec_quant_append does not write may stand for others: they are rounded to bf16).
+ * largest, 6 or 448, gives that.  X is clamped to [-111, 125] (8 bits: [-111, 119]).
+ * In groups of A <= 7 2^125 (448 2^119) no element is off by more than half the spacing
+ * of the elements at its magnitude (in 4 bits beyond 6: of the two below it); what is
+ * beyond the largest element in greater, finite groups becomes 6 2^125 (448 2^119).  A
+ * group that holds a NaN or an infinity is NaN throughout.  Every x^ is a bf16 number
+ * (bytes that spec_quant_append does not write may stand for others: they are rounded to
+ * bf16).
  *     k, v    uint8 [n_layers][B][L_cap][H_kv][d bits / 8]: byte i of 4-bit rows holds
  *             dimension 2 i in its low half (sign, two bits of exponent, one of mantissa)
  *             and 2 i + 1 in its high half;
