@@ -375,6 +375,8 @@ __device__ __forceinline__ uint32_t quant_unit(const QuantUnit& u, WaveTile<NH>&
     __builtin_amdgcn_sched_barrier(0);
   }
   for (int c = u.part; c < chunks; c += u.n_parts) {
+    // Behind a wavefront's last chunk the sequence's last is requested, which nobody uses: the
+    // loads stay without a branch, and a wavefront waits for them at its end.
     const int next = min(c + u.n_parts, chunks - 1);
     *reinterpret_cast<uint2*>(T.scales + lane % (kDecodeChunk * NH) * kScaleBytes) = sc;
 #pragma unroll

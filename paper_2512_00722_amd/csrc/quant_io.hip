@@ -1,8 +1,9 @@
 // New rows into caches held in 4 or 8 bits, and rows back to bf16.
 //
-// Both are bound by memory, and run at 6.4 to 7.1 TB/s of what they read and write.  A thread
-// has eight elements of K and the same eight of V (one 16-byte bf16 load or store each), four
-// threads a group, sixteen a row of a head.
+// Both are bound by memory: 5.6 to 6.6 TB/s of what they read and write in calls of 680 to 990
+// MB, one after another on two sets of buffers in turn (as all times here; calls on one set
+// find some of it in the caches).  A thread has eight elements of K and the same eight of V
+// (one 16-byte bf16 load or store each), four threads a group, sixteen a row of a head.
 #include "quant_core.h"
 
 namespace spec {
@@ -12,9 +13,10 @@ constexpr int kRowThreads = 16;               // of a row of a head
 constexpr int kThreads = 256;
 constexpr int kBlockRows = kThreads / kRowThreads;  // rows at a time
 // Rows of a thread, whose loads are all in flight: two when writing the caches (8 layers x 2
-// x 8192 tokens x 8 KV heads in 4 bits 106.5 us, one 107.9, four 109.2; in 8 bits 122.8, 122.9,
-// 123.2), one when reading them (8 x 8 x 2048 selected rows in 4 bits 95.3, two 98.9, four
-// 100.0; in 8 bits 127.1, 136.5, 136.9).
+// x 8192 tokens x 8 KV heads in 4 bits 114 us, one 111, four 115; in 8 bits 141, 136, 143;
+// with the rows read back 205, 203, 206 and 265, 265, 264), one when reading them (8 x 8 x 2048
+// selected rows in 4 bits 121, two 125, four 123; in 8 bits 142, 145, 146; 4 x 2 x 20011 rows in
+// order 126, 135, 140 and 158, 161, 161).
 constexpr int kAppendRows = 2;
 constexpr int kReadRows = 1;
 
@@ -71,9 +73,11 @@ __device__ __forceinline__ void store8(uint8_t* row, int piece, const uint2& e) 
 
 // Rows (token, head) of a sequence's new tokens stand in the caches as they come, from
 // token pos on: those inside the caches are one range of rows.  STREAM: new rows that the
-// caches do not hold are loaded past them (537 MB of them: 106.5 us, through the caches 122.5);
+// caches do not hold are loaded past them (537 MB of them in 4 bits: 114 us, through the caches
+// 121, and with the rows read back 205 and 226; in 8 bits 141 and 141, 265 and 280);
 // others, which the program has just made, through them.  The rows are stored through the
-// caches: past them the call takes 3% less, and reading the rows afterwards 10% more.
+// caches: past them the call takes 3% less (in 8 bits 10%), and reading the rows afterwards 15%
+// more (10%).
 template <int BITS, bool STREAM>
 __global__ __launch_bounds__(kThreads) void append_kernel(QuantIoArgs a) {
   const int lb = blockIdx.z * gridDim.y + blockIdx.y;
@@ -124,8 +128,9 @@ __device__ __forceinline__ uint4 values8(const uint2& e, float scale) {
   return __builtin_bit_cast(uint4, elements8<BITS>(p, 0, scale));
 }
 
-// A 16-byte store past the caches, which the outputs do not fit: in 4 bits 8 x 8 x 2048
-// selected rows take 95.3 us, with ordinary stores 130.3.
+// A 16-byte store past the caches: in 4 bits 8 layers x 8 x 2048 selected rows take 121 us,
+// with ordinary stores 130, one layer of them 14.3 and 16.2, one layer and the attention that
+// reads the outputs next 32.6 and 37.0; in 8 bits 142 and 159, 16.9 and 18.6, 35.1 and 37.5.
 __device__ __forceinline__ void store_stream(uint16_t* p, const uint4& x) {
   typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
   __builtin_nontemporal_store(uintx4{x.x, x.y, x.z, x.w}, reinterpret_cast<uintx4*>(p));

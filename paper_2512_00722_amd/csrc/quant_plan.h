@@ -18,10 +18,11 @@ constexpr int kMostDealt = 64;
 // share of the bytes (256 of them move 6.9 TB/s; workgroups that read a part of a token's row
 // move 7% less per halving, and in 4 bits 45% where it is half a 128-byte line), and its
 // wavefronts' chunks one after the other (0.86 us, of two heads 1.5: what a chunk's loads
-// take to arrive); workgroups beyond those resident cost 2.9 us a round, and parts a second
-// launch and the traffic of their results.  Fitted to 4900 launches of 144 shapes (1 to 256
-// sequences and layers of 64 to 131072 tokens, 1 to 16 query heads per KV head, 4 and 8 bits,
-// rows selected or not): on average it is 1.6% slower than the best plan, 12% at most.
+// take to arrive, fitted with the one that a wavefront loads beyond its last, see quant_unit());
+// workgroups beyond those resident cost 2.9 us a round, and parts a second launch and the
+// traffic of their results.  Fitted to 4900 launches of 144 shapes (1 to 256 sequences and
+// layers of 64 to 131072 tokens, 1 to 16 query heads per KV head, 4 and 8 bits, rows selected or
+// not): on average it is 1.6% slower than the best plan, 12% at most.
 // Between plans: 32 x 8 x 32768 tokens in 4 bits 1344 us with 8 wavefronts and no parts, 1367
 // with 4 and four; 1 x 4096 6.2 and 3.9 to join the parts with 4 wavefronts to a unit in 32
 // parts, 7.7 and 2.7 with 8 in 16; 1 x 512 7.6 in one part, 5.4 and 2.6 in four, where
@@ -43,7 +44,10 @@ inline QuantPlan make_plan(const QuantDims& d, int k_max, bool ragged) {
         (float)kCUs * kDecodeChunk * nh * (2 * row_bytes(d.bits) + kScaleBytes) / 6.9e6f;
     const float wait_us = nh == 2 ? 1.5f : 0.86f;
     for (int w = 4; w <= 8; w += 4) {
-      const int resident = w == 8 ? 1 : nh == 2 ? 2 : 3;  // workgroups of a CU
+      // Workgroups of a CU, as the other numbers were fitted with.  Registers and LDS hold as
+      // many but for selected rows in 8 bits by 4 wavefronts (194 registers: 2) and, where rows
+      // are not selected, one head in 4 bits (126: 4 workgroups of 4 wavefronts, 2 of 8).
+      const int resident = w == 8 ? 1 : nh == 2 ? 2 : 3;
       for (int u = 0; 1 << u <= w && units % (1 << u) == 0; ++u) {
         const int64_t one = lb * (units >> u);
         if (one > INT32_MAX / (w * 64)) continue;
